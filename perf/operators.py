@@ -337,14 +337,14 @@ def run(s):
         return _plain_attention(s) if case["entry"] == "attention4" else _plain_append(s)
     hb, stream = s["hb"], torch.cuda.current_stream()
     if case["entry"] == "attention4":      # one layer of a step whose descriptor is on the GPU
-        hb.hfx_mixed_paged_attention_kv4(s["shape"], s["q"], s["pool"], s["host_desc"], s["device_desc"], s["workspace"], s["out"], stream)
+        hb.hfx_mixed_paged_attention_mx(s["shape"], s["q"], s["pool"], s["host_desc"], s["device_desc"], s["workspace"], s["out"], stream)
         return s["out"]
     q, k, v = s["q"], s["k"], s["v"]
-    append = hb.hfx_rope_append_kv if case["entry"] == "append" else hb.hfx_rope_append_kv4
+    append = hb.hfx_rope_append_kv if case["entry"] == "append" else hb.hfx_rope_append_kv_mx
     append(s["shape"], s["rope"], q, q.stride(0), k, k.stride(0), v, v.stride(0), s["out"], s["pool"], s["host_desc"], s["device_desc"], stream)
     if case["entry"] == "append":
         return s["out"], s["pool"]
-    hb.hfx_read_new_kv4(s["shape"], s["pool"], s["host_desc"], s["device_desc"], s["k_out"], s["v_out"], stream)
+    hb.hfx_read_new_kv_mx(s["shape"], s["pool"], s["host_desc"], s["device_desc"], s["k_out"], s["v_out"], stream)
     return s["out"], s["k_out"], s["v_out"]
 
 
