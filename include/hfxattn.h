@@ -288,6 +288,81 @@ hfx_status hfx_copy_pages(const hfx_shape* shape, const void* src_pool, void* ds
                           size_t stage_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Position rotation on the way into the cache, and the cache held in 4 bits.
+ * ---------------------------------------------------------------------------------------- */
+
+/* Rotary position embedding.  cos_sin is a table [num_positions][rot_dim] of fp32: the cosines of a position's rot_dim / 2 angles, then their
+ * sines.  Dimensions past rot_dim are left as they are. */
+typedef struct {
+  const float* cos_sin;   /* [device], 16-byte aligned                                                       */
+  int32_t num_positions;  /* rows of the table; every context of the step must fit                            */
+  int32_t rot_dim;        /* a multiple of 16, at most head_dim                                              */
+  int32_t interleaved;    /* pairs are 0: dimensions i and i + rot_dim / 2; 1: dimensions 2 i and 2 i + 1     */
+} hfx_rope;
+
+/*
+ * hfx_append_kv with the step's position rotation and its queries: takes queries, keys and values as a projection leaves them, rotates the
+ * queries and the keys, writes the queries to q_out packed as hfx_mixed_paged_attention takes them, and the keys and values into their
+ * pages.  (The step of the execution loop of Section 3.4 between a layer's projection and its attention.)  Chunk row i of request r is at position
+ * ctx_len[r] - q_len[r] + i; a pair (a, b) with the angle's cosine c and sine s becomes (a c - b s, b c + a s), every product and sum
+ * rounded to fp32 and the result to bf16, nearest-even.  Values, and dimensions that are not rotated, go through unchanged.
+ *   rope         [host]   NULL: nothing is rotated
+ *   q            [device] bf16, token t's heads [Hq][D] at q + t * q_stride; NULL (with q_out NULL): the step's queries are not touched
+ *   k_new, v_new [device] bf16, token t's heads [Hkv][D] at t * k_stride, t * v_stride
+ *   q_stride ..           elements between tokens, multiples of 8, no less than the heads take.  Rows of all three may lie in one buffer
+ *   q_out        [device] bf16 [T][Hq][D].  May be q itself if q is packed (q_stride == Hq * D), and overlaps nothing else
+ *   kv_pool      [device] the bf16 page pool, written in place
+ * Everything else as for hfx_append_kv.  Asynchronous on `stream`; allocates nothing.
+ * Errors: HFX_ERR_NULL, HFX_ERR_SHAPE (also: a stride too small, rot_dim or interleaved not as above), HFX_ERR_LEN (a context is longer than the
+ * table), HFX_ERR_DESC, HFX_ERR_ALIGN (also: a stride that is no multiple of 8), HFX_ERR_DEVICE.
+ */
+hfx_status hfx_rope_append_kv(const hfx_shape* shape, const hfx_rope* rope, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                              void* kv_pool, const void* host_desc, const void* device_desc, void* stream);
+
+/*
+ * The 4-bit page pool (one device allocation of hfx_mx_pool_bytes, 16-byte aligned): a token's keys and values of a kv-head are cut into blocks of 32
+ * dimensions, each with a scale 2^(e - 127), e a byte, and 32 codes of four bits, sign and magnitude out of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1).  4.25
+ * bits a value; a page of 16 tokens takes Hkv * 17 * D bytes, 0.27 of the bf16 one.
+ *
+ *   pool[num_pages][Hkv][17 * D], of which
+ *     [16 tokens][D/32][16]                 key codes: byte b of a block has dimensions 2 b (low four bits) and 2 b + 1
+ *     [2][D/64][16][2][8 tokens]            value codes: [8 tokens of the page][64 dimensions][i][32 of those][token], with dimensions i (low) and i + 16
+ *     [16 tokens][D/32]                     key scales e
+ *     [2][D/64][8 tokens][2]                value scales e
+ *
+ * The order in which the matrix cores take codes and scales.  Pages, block tables, shared pages and unused slots are as in the bf16 pool; the unused ones may hold
+ * anything.  One descriptor serves pools of both kinds.
+ */
+hfx_status hfx_mx_pool_bytes(const hfx_shape* shape, size_t* bytes);
+
+/*
+ * hfx_rope_append_kv into a 4-bit pool.  The rotated keys, in fp32, and the values are quantised: e is the smallest power of two's under which the
+ * block's largest magnitude is nearest to one of at most 6 (it is less than 7), kept within [2, 252]; codes are nearest, ties to the
+ * even one.  A block with a value that is not finite gets e = 255 and stands for NaN.  Tokens of the page that are not in the step keep their bytes.
+ * Arguments and errors as above.
+ */
+hfx_status hfx_rope_append_kv_mx(const hfx_shape* shape, const hfx_rope* rope, const void* q, int64_t q_stride,
+                               const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                               void* mx_pool, const void* host_desc, const void* device_desc, void* stream);
+
+/*
+ * The step's tokens as the 4-bit pool holds them: bf16 rows [T][Hkv][D] of keys and of values, packed like Q, exact (every value that a block can hold
+ * is a bf16 number).  The paging check hook of this pool; a descriptor whose chunks are whole contexts (q_len == ctx_len) reads whole contexts.
+ * Errors: HFX_ERR_NULL, HFX_ERR_SHAPE, HFX_ERR_DESC, HFX_ERR_ALIGN, HFX_ERR_DEVICE.
+ */
+hfx_status hfx_read_new_kv_mx(const hfx_shape* shape, const void* mx_pool, const void* host_desc, const void* device_desc,
+                            void* k_out, void* v_out, void* stream);
+
+/*
+ * hfx_mixed_paged_attention over a 4-bit pool: the same result as over a bf16 pool that holds the values that this one stands for, to rounding (scores
+ * against the bf16 queries and the weighted sum accumulate in fp32, softmax weights are rounded to bf16).  Same descriptor, workspace, arguments and errors.
+ */
+hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, const void* mx_pool, const void* host_desc,
+                                         void* device_desc, void* workspace, size_t workspace_bytes, void* out,
+                                         void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Step composition (host only): the closed forms of Section 3.3.1 that decide how many
  * prompt tokens a step may carry, and a one-instance form of the dispatching steps that
  * turns a waiting queue into the arrays hfx_build_batch_desc takes.

@@ -24,13 +24,22 @@ HFX_DECODE, HFX_PREFILL = 0, 1
 
 EXPORTS = ["hfx_status_string", "hfx_version", "hfx_batch_desc_sizes", "hfx_build_batch_desc",
            "hfx_fill_batch_desc", "hfx_mixed_paged_attention", "hfx_mixed_paged_attention_static", "hfx_gather_kv", "hfx_append_kv",
-           "hfx_copy_pages", "hfx_token_budget", "hfx_maturity_time", "hfx_fit_latency_model", "hfx_compose_step"]
+           "hfx_copy_pages", "hfx_rope_append_kv", "hfx_mx_pool_bytes", "hfx_rope_append_kv_mx", "hfx_read_new_kv_mx", "hfx_mixed_paged_attention_mx",
+           "hfx_token_budget", "hfx_maturity_time", "hfx_fit_latency_model", "hfx_compose_step"]
 
 
 class hfx_shape(ctypes.Structure):
     _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("num_pages", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class hfx_rope(ctypes.Structure):
+    """Keeps the table it was made with alive (see make_rope)."""
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+    def data_ptr(self):
+        return ctypes.addressof(self)
 
 
 class hfx_latency_model(ctypes.Structure):
@@ -86,6 +95,16 @@ def load() -> ctypes.CDLL:
         lib.hfx_copy_pages.argtypes = [shp, vp, vp, ctypes.c_int32, ctypes.c_int32, ints, ints, vp, vp,
                                        ctypes.c_size_t, vp]
         lib.hfx_copy_pages.restype = ctypes.c_int32
+        rope, i64 = ctypes.POINTER(hfx_rope), ctypes.c_int64
+        for f in (lib.hfx_rope_append_kv, lib.hfx_rope_append_kv_mx):
+            f.argtypes = [shp, rope, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+            f.restype = ctypes.c_int32
+        lib.hfx_mx_pool_bytes.argtypes = [shp, szp]
+        lib.hfx_mx_pool_bytes.restype = ctypes.c_int32
+        lib.hfx_read_new_kv_mx.argtypes = [shp, vp, vp, vp, vp, vp, vp]
+        lib.hfx_read_new_kv_mx.restype = ctypes.c_int32
+        lib.hfx_mixed_paged_attention_mx.argtypes = [shp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp]
+        lib.hfx_mixed_paged_attention_mx.restype = ctypes.c_int32
         dbl, dblp = ctypes.c_double, ctypes.POINTER(ctypes.c_double)
         i64p, lmp = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(hfx_latency_model)
         lib.hfx_token_budget.argtypes = [dbl, dbl, lmp, i64p]
@@ -121,7 +140,9 @@ def _serving() -> types.SimpleNamespace:
         _calls = types.SimpleNamespace(
             build=caller(lib.hfx_build_batch_desc, "SKAAAaBBs"), attention=caller(lib.hfx_mixed_paged_attention, "SPPPPBPs"),
             attention_static=caller(lib.hfx_mixed_paged_attention_static, "SPPPPPs"), gather=caller(lib.hfx_gather_kv, "SPPPiPPs"),
-            append=caller(lib.hfx_append_kv, "SPPPPPs"), copy_pages=caller(lib.hfx_copy_pages, "SPPikaPPzs"))
+            append=caller(lib.hfx_append_kv, "SPPPPPs"), copy_pages=caller(lib.hfx_copy_pages, "SPPikaPPzs"),
+            rope_append=caller(lib.hfx_rope_append_kv, "SPPzPzPzPPPPs"), rope_append4=caller(lib.hfx_rope_append_kv_mx, "SPPzPzPzPPPPs"),
+            read_new4=caller(lib.hfx_read_new_kv_mx, "SPPPPPs"), attention4=caller(lib.hfx_mixed_paged_attention_mx, "SPPPPBPs"))
     return _calls
 
 
@@ -168,6 +189,15 @@ def _nbytes(x) -> int:
 def make_shape(num_q_heads, num_kv_heads, head_dim, num_pages, softmax_scale=0.0, page_size=16) -> hfx_shape:
     return hfx_shape(int(num_q_heads), int(num_kv_heads), int(head_dim), int(page_size), int(num_pages),
                      float(softmax_scale))
+
+
+def make_rope(cos_sin, rot_dim: int, interleaved: bool = False) -> hfx_rope:
+    """The rotation by a table [positions, rot_dim] of fp32 on the GPU: the cosines of a position's angles, then their sines."""
+    if cos_sin.dim() != 2 or cos_sin.shape[1] != rot_dim or cos_sin.element_size() != 4 or not cos_sin.is_floating_point() or not cos_sin.is_contiguous():
+        raise ValueError("cos_sin is a contiguous fp32 table [positions, rot_dim]")
+    rope = hfx_rope(cos_sin.data_ptr(), cos_sin.shape[0], int(rot_dim), int(bool(interleaved)))
+    rope.table = cos_sin
+    return rope
 
 
 def hfx_status_string(code: int) -> str:
@@ -250,6 +280,40 @@ def hfx_copy_pages(shape: hfx_shape, src_pool, dst_pool, dst_num_pages: int, src
         raise HfxError(rc, "hfx_copy_pages")
 
 
+def hfx_rope_append_kv(shape: hfx_shape, rope, q, q_stride: int, k_new, k_stride: int, v_new, v_stride: int, q_out, kv_pool, host_desc, device_desc,
+                       stream=None) -> None:
+    rc = (_calls or _serving()).rope_append(shape, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, kv_pool, host_desc, device_desc, stream)
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_rope_append_kv")
+
+
+def hfx_mx_pool_bytes(shape: hfx_shape) -> int:
+    n = ctypes.c_size_t()
+    rc = load().hfx_mx_pool_bytes(ctypes.byref(shape), ctypes.byref(n))
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_mx_pool_bytes")
+    return n.value
+
+
+def hfx_rope_append_kv_mx(shape: hfx_shape, rope, q, q_stride: int, k_new, k_stride: int, v_new, v_stride: int, q_out, mx_pool, host_desc, device_desc,
+                        stream=None) -> None:
+    rc = (_calls or _serving()).rope_append4(shape, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, mx_pool, host_desc, device_desc, stream)
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_rope_append_kv_mx")
+
+
+def hfx_read_new_kv_mx(shape: hfx_shape, mx_pool, host_desc, device_desc, k_out, v_out, stream=None) -> None:
+    rc = (_calls or _serving()).read_new4(shape, mx_pool, host_desc, device_desc, k_out, v_out, stream)
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_read_new_kv_mx")
+
+
+def hfx_mixed_paged_attention_mx(shape: hfx_shape, q, mx_pool, host_desc, device_desc, workspace, out, stream=None) -> None:
+    rc = (_calls or _serving()).attention4(shape, q, mx_pool, host_desc, device_desc, workspace, out, stream)
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_mixed_paged_attention_mx")
+
+
 def hfx_token_budget(ttft: float, tpot: float, model: hfx_latency_model) -> int:
     n = ctypes.c_int64(-1)
     rc = load().hfx_token_budget(ttft, tpot, ctypes.byref(model), ctypes.byref(n))
@@ -323,7 +387,7 @@ class DescHeader(ctypes.Structure):
                 ("n_units", ctypes.c_int32), ("off_units", ctypes.c_uint32), ("n_runs", ctypes.c_int32),
                 ("off_runs", ctypes.c_uint32), ("queue_classes", ctypes.c_uint32),
                 ("deal_balanced", ctypes.c_uint32), ("off_queue", ctypes.c_uint32),
-                ("die_items", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+                ("die_items", ctypes.c_uint32), ("off_run_pos", ctypes.c_uint32)]
 
 
 ITEM_DTYPE = np.dtype([(n, np.int32) for n in ("type", "req", "group", "slot_row", "h0", "hn", "row0", "nrows",
@@ -351,6 +415,8 @@ def parse_desc(host_desc: np.ndarray) -> dict:
         "units": buf[h.off_units:h.off_units + 8 * h.n_units].view(np.int32).reshape(-1, 2),
         # append runs: (first packed row, tokens, physical page, first slot)
         "runs": buf[h.off_runs:h.off_runs + 16 * h.n_runs].view(np.int32).reshape(-1, 4),
+        # logical position of each run's first token
+        "run_pos": buf[h.off_run_pos:h.off_run_pos + 4 * h.n_runs].view(np.int32),
     }
 
 

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhfxattn.so")
 # The name says for which Python it was built, so that another one does not load it.
 CALL_LIB = os.path.join(HERE, "_hfxcall" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["hfx_kernels.hip", "hfx_api.cpp", "hfx_plan.cpp", "hfx_sched.cpp"]
+SOURCES = ["hfx_kernels.hip", "hfx_append.hip", "hfx_mx.hip", "hfx_api.cpp", "hfx_plan.cpp", "hfx_sched.cpp"]
 # -fno-honor-nans: no floating-point operation in the kernels is ever fed a NaN (possibly-NaN scores
 # are masked through integer selects first), and without it every max carries a canonicalising twin.
 # Device code only: the host side validates its floating-point arguments with NaN tests.

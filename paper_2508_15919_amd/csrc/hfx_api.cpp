@@ -31,18 +31,19 @@ hfx_status check_header(const hfx_shape* shape, const void* host_desc, HfxHeader
 // Workgroups of the persistent launch on the current device: what fits on the chip at once (cached per
 // device), but never more than the width the planner laid the queue out for -- its first rounds deal
 // queue positions b and b + HFX_PLAN_WGS to workgroup b.
-hfx_status persistent_grid(int head_dim, int* grid) {
+hfx_status persistent_grid(int head_dim, bool four, int* grid) {
   static std::mutex mu;
-  static int cache[HFX_MAX_DEVICES][2];
+  static int cache[HFX_MAX_DEVICES][4];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return HFX_ERR_DEVICE;
   if (dev < 0 || dev >= HFX_MAX_DEVICES) return HFX_ERR_DEVICE;
-  const int slot = head_dim == 128 ? 1 : 0;
+  const int slot = (head_dim == 128 ? 1 : 0) + (four ? 2 : 0);
   std::lock_guard<std::mutex> lock(mu);
   if (cache[dev][slot] == 0) {
     int cus = 0, per_cu = 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return HFX_ERR_DEVICE;
-    if (hfx::max_resident_workgroups(head_dim, &per_cu) != hipSuccess) return HFX_ERR_DEVICE;
+    if ((four ? hfx::max_resident_workgroups_mx(head_dim, &per_cu) : hfx::max_resident_workgroups(head_dim, &per_cu)) != hipSuccess)
+      return HFX_ERR_DEVICE;
     if (cus < 1 || per_cu < 1) return HFX_ERR_DEVICE;
     cache[dev][slot] = cus * per_cu < HFX_PLAN_WGS ? cus * per_cu : HFX_PLAN_WGS;
   }
@@ -54,8 +55,8 @@ hfx_status persistent_grid(int head_dim, int* grid) {
 
 namespace {
 
-// The attention call proper; `h` is the descriptor's header, already checked against the shape.
-hfx_status run_attention(const HfxHeader& h, const void* q, const void* kv_pool, void* device_desc, void* workspace,
+// The attention call proper, over a bf16 pool or (four) a 4-bit one; `h` is the descriptor's header, already checked against the shape.
+hfx_status run_attention(const HfxHeader& h, bool four, const void* q, const void* kv_pool, void* device_desc, void* workspace,
                          size_t workspace_bytes, void* out, void* stream) {
   hfx_status st;
   if (h.workspace_bytes > 0 && !workspace) return HFX_ERR_NULL;
@@ -68,13 +69,50 @@ hfx_status run_attention(const HfxHeader& h, const void* q, const void* kv_pool,
   // positions that belong to dies: the kernel hands them out without looking at the end of the queue
   if (h.die_items > (uint32_t)h.n_items || h.die_items % HFX_QUEUE_CLASSES != 0) return HFX_ERR_DESC;
   int grid = 0;
-  st = persistent_grid(h.head_dim, &grid);
+  st = persistent_grid(h.head_dim, four, &grid);
   if (st != HFX_OK) return st;
   if (grid > h.n_items) grid = h.n_items;
-  if (hfx::launch_mixed_attention(h, grid, device_desc, q, kv_pool, workspace, out, static_cast<hipStream_t>(stream)) !=
-      hipSuccess)
+  if ((four ? hfx::launch_mixed_attention_mx : hfx::launch_mixed_attention)(h, grid, device_desc, q, kv_pool, workspace, out,
+                                                                             static_cast<hipStream_t>(stream)) != hipSuccess)
     return HFX_ERR_DEVICE;
   return HFX_OK;
+}
+
+// Checks what the two rotating appends take, and enqueues the one asked for.
+hfx_status rope_append(const hfx_shape* shape, const hfx_rope* rope, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                       const void* v_new, int64_t v_stride, void* q_out, void* pool, const void* host_desc, const void* device_desc, bool four,
+                       void* stream) {
+  if (!k_new || !v_new || !pool || !device_desc || (q == nullptr) != (q_out == nullptr)) return HFX_ERR_NULL;
+  HfxHeader h;
+  hfx_status st = check_header(shape, host_desc, &h);
+  if (st != HFX_OK) return st;
+  const int64_t q_row = (int64_t)h.num_q_heads * h.head_dim, kv_row = (int64_t)h.num_kv_heads * h.head_dim;
+  if ((q && q_stride < q_row) || k_stride < kv_row || v_stride < kv_row) return HFX_ERR_SHAPE;
+  hfx::RopeAppend a = {};
+  if (rope) {
+    if (!rope->cos_sin) return HFX_ERR_NULL;
+    if (rope->rot_dim < 16 || rope->rot_dim > h.head_dim || rope->rot_dim % 16 != 0 || (rope->interleaved != 0 && rope->interleaved != 1))
+      return HFX_ERR_SHAPE;
+    if (!aligned16(rope->cos_sin)) return HFX_ERR_ALIGN;
+    const HfxReq* reqs = reinterpret_cast<const HfxReq*>(static_cast<const char*>(host_desc) + h.off_req);
+    for (int r = 0; r < h.num_requests; ++r)
+      if (reqs[r].ctx_len > rope->num_positions) return HFX_ERR_LEN;
+    a.rot = rope->rot_dim;
+    a.interleaved = rope->interleaved;
+    a.cos_sin = rope->cos_sin;
+  }
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned16(pool) || !aligned16(device_desc) ||
+      ((q ? q_stride : 0) | k_stride | v_stride) % 8 != 0)
+    return HFX_ERR_ALIGN;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k_new);
+  a.v = static_cast<const uint16_t*>(v_new);
+  a.q_stride = (long)q_stride;
+  a.k_stride = (long)k_stride;
+  a.v_stride = (long)v_stride;
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.pool = pool;
+  return hfx::launch_rope_append(h, device_desc, a, four, static_cast<hipStream_t>(stream)) == hipSuccess ? HFX_OK : HFX_ERR_DEVICE;
 }
 
 }  // namespace
@@ -160,7 +198,7 @@ hfx_status hfx_mixed_paged_attention(const hfx_shape* shape, const void* q, cons
   HfxHeader h;
   hfx_status st = check_header(shape, host_desc, &h);
   if (st != HFX_OK) return st;
-  return run_attention(h, q, kv_pool, device_desc, workspace, workspace_bytes, out, stream);
+  return run_attention(h, false, q, kv_pool, device_desc, workspace, workspace_bytes, out, stream);
 }
 
 hfx_status hfx_mixed_paged_attention_static(const hfx_shape* shape, const void* q, const void* kv_pool,
@@ -173,7 +211,7 @@ hfx_status hfx_mixed_paged_attention_static(const hfx_shape* shape, const void* 
   if (h.workspace_bytes > (uint64_t)HFX_STATIC_WS_BYTES) return HFX_ERR_BUFSIZE;
   void* ws = nullptr;
   if (hfx::static_workspace(&ws) != hipSuccess) return HFX_ERR_DEVICE;
-  return run_attention(h, q, kv_pool, device_desc, ws, (size_t)HFX_STATIC_WS_BYTES, out, stream);
+  return run_attention(h, false, q, kv_pool, device_desc, ws, (size_t)HFX_STATIC_WS_BYTES, out, stream);
 }
 
 hfx_status hfx_gather_kv(const hfx_shape* shape, const void* kv_pool, const void* host_desc,
@@ -200,6 +238,46 @@ hfx_status hfx_append_kv(const hfx_shape* shape, const void* k_new, const void* 
   if (hfx::launch_append_kv(h, device_desc, k_new, v_new, kv_pool, static_cast<hipStream_t>(stream)) != hipSuccess)
     return HFX_ERR_DEVICE;
   return HFX_OK;
+}
+
+hfx_status hfx_rope_append_kv(const hfx_shape* shape, const hfx_rope* rope, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                              const void* v_new, int64_t v_stride, void* q_out, void* kv_pool, const void* host_desc, const void* device_desc,
+                              void* stream) {
+  return rope_append(shape, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, kv_pool, host_desc, device_desc, false, stream);
+}
+
+hfx_status hfx_rope_append_kv_mx(const hfx_shape* shape, const hfx_rope* rope, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                               const void* v_new, int64_t v_stride, void* q_out, void* mx_pool, const void* host_desc, const void* device_desc,
+                               void* stream) {
+  return rope_append(shape, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, mx_pool, host_desc, device_desc, true, stream);
+}
+
+hfx_status hfx_mx_pool_bytes(const hfx_shape* shape, size_t* bytes) {
+  if (!bytes) return HFX_ERR_NULL;
+  hfx_status st = hfx::check_shape(shape);
+  if (st != HFX_OK) return st;
+  *bytes = (size_t)shape->num_pages * (size_t)shape->num_kv_heads * 17u * (size_t)shape->head_dim;
+  return HFX_OK;
+}
+
+hfx_status hfx_read_new_kv_mx(const hfx_shape* shape, const void* mx_pool, const void* host_desc, const void* device_desc, void* k_out, void* v_out,
+                            void* stream) {
+  if (!mx_pool || !device_desc || !k_out || !v_out) return HFX_ERR_NULL;
+  HfxHeader h;
+  hfx_status st = check_header(shape, host_desc, &h);
+  if (st != HFX_OK) return st;
+  if (!aligned16(mx_pool) || !aligned16(device_desc) || !aligned16(k_out) || !aligned16(v_out)) return HFX_ERR_ALIGN;
+  if (hfx::launch_read_new_kv_mx(h, device_desc, mx_pool, k_out, v_out, static_cast<hipStream_t>(stream)) != hipSuccess) return HFX_ERR_DEVICE;
+  return HFX_OK;
+}
+
+hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, const void* mx_pool, const void* host_desc, void* device_desc,
+                                         void* workspace, size_t workspace_bytes, void* out, void* stream) {
+  if (!q || !mx_pool || !device_desc || !out) return HFX_ERR_NULL;
+  HfxHeader h;
+  hfx_status st = check_header(shape, host_desc, &h);
+  if (st != HFX_OK) return st;
+  return run_attention(h, true, q, mx_pool, device_desc, workspace, workspace_bytes, out, stream);
 }
 
 hfx_status hfx_copy_pages(const hfx_shape* shape, const void* src_pool, void* dst_pool, int32_t dst_num_pages,

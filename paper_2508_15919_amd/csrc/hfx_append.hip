@@ -1,0 +1,273 @@
+// Rotary position embedding on the way into the page pool: one launch takes the step's queries, keys and values out of the projection's
+// output, rotates queries and keys by their logical positions, writes the queries packed for the attention call, and keys and values into their
+// pages, in bf16 or quantised to 4 bits; and the way back, from the 4-bit pages of the step's tokens to bf16 rows.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "hfx_desc.h"
+#include "hfx_device.h"
+#include "hfx_mx.h"
+#include "hfx_launch.h"
+
+namespace hfx {
+
+// Rotates eight values (dimensions 8 piece .. 8 piece + 7 of a head) by the angles of their position.  A pair (a, b) turns into (a c - b s, b c + a s); every
+// product and sum is rounded to fp32 by itself, so that what is quantised afterwards does not depend on how a compiler contracts them.
+struct Turn {
+  float c[8], s[8];
+  bool on, second;       // the piece is rotated; and holds the b's of its pairs, its partner the a's
+  int partner;           // lane that holds the other value of each pair
+};
+
+template <bool Interleaved>
+__device__ __forceinline__ Turn turn_of(const float* __restrict__ row, int rot, int piece, int lane) {
+  Turn t;
+  const int pieces = rot / 8, half = pieces / 2;
+  t.on = piece < pieces;
+  t.second = !Interleaved && piece >= half;
+  t.partner = !t.on || Interleaved ? lane : t.second ? lane - half : lane + half;
+  if (t.on) {
+    if constexpr (Interleaved) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 c = reinterpret_cast<const float2*>(row + 4 * piece)[i], s = reinterpret_cast<const float2*>(row + rot / 2 + 4 * piece)[i];
+        t.c[2 * i] = c.x;
+        t.c[2 * i + 1] = c.y;
+        t.s[2 * i] = s.x;
+        t.s[2 * i + 1] = s.y;
+      }
+    } else {
+      const int at = 8 * (t.second ? piece - half : piece);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 c = reinterpret_cast<const f32x4*>(row + at)[i], s = reinterpret_cast<const f32x4*>(row + rot / 2 + at)[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          t.c[4 * i + e] = c[e];
+          t.s[4 * i + e] = s[e];
+        }
+      }
+    }
+  }
+  return t;
+}
+
+__device__ __forceinline__ void widen(const u32x4& v, float* x) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    x[2 * w] = __builtin_bit_cast(float, v[w] << 16);
+    x[2 * w + 1] = __builtin_bit_cast(float, v[w] & 0xffff0000u);
+  }
+}
+
+// All lanes of a wavefront take part (the partner's values come by a lane exchange).
+template <bool Interleaved>
+__device__ __forceinline__ void turn(const Turn& t, bool any, const u32x4& v, float* y) {
+#pragma clang fp contract(off)
+  float x[8];
+  widen(v, x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = x[e];
+  if (!any) return;
+  if constexpr (Interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = x[2 * i], b = x[2 * i + 1];
+      const float ac = a * t.c[i], bs = b * t.s[i], bc = b * t.c[i], as = a * t.s[i];
+      y[2 * i] = t.on ? ac - bs : a;
+      y[2 * i + 1] = t.on ? bc + as : b;
+    }
+  } else {
+    u32x4 p;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) p[w] = (uint32_t)__shfl((int)v[w], t.partner, 64);
+    float z[8];
+    widen(p, z);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float xc = x[e] * t.c[e], zs = z[e] * t.s[e];
+      y[e] = !t.on ? x[e] : t.second ? xc + zs : xc - zs;
+    }
+  }
+}
+
+__device__ __forceinline__ u32x4 narrow(const float* x) {
+  u32x4 v;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const bf16x2 r = {(__bf16)x[2 * w], (__bf16)x[2 * w + 1]};
+    v[w] = __builtin_bit_cast(unsigned, r);
+  }
+  return v;
+}
+
+// Largest magnitude, as its bits, of the 32 values that four neighbouring lanes hold (a NaN has larger bits than any number).
+__device__ __forceinline__ unsigned block_top(const float* x) {
+  unsigned top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(unsigned, x[e]) & 0x7fffffffu);
+  top = max(top, (unsigned)__builtin_amdgcn_mov_dpp((int)top, 0xb1, 0xf, 0xf, true));      // lane ^ 1
+  return max(top, (unsigned)__builtin_amdgcn_mov_dpp((int)top, 0x4e, 0xf, 0xf, true));     // lane ^ 2
+}
+
+// One workgroup of 2 D threads per (run, kv-head), a run being the new tokens of one request in one page (at most 16).  A thread has one
+// 16-byte piece of one token: of its key row, of its value row, and of the rows of the q-heads that share the kv-head, all of which take the
+// same angles.
+template <int D, bool Four, bool Interleaved>
+__global__ __launch_bounds__(2 * D) void rope_append_kernel(const RopeAppend a) {
+  constexpr int LD = D + 8;                       // LDS row stride in elements
+  __shared__ __attribute__((aligned(16))) uint16_t sv[Four ? 1 : HFX_PAGE * LD];
+  __shared__ __attribute__((aligned(16))) uint8_t s4[Four ? 9 * D : 16];      // value codes, key scales, value scales as in the block
+  const int Hkv = a.num_kv_heads, G = a.num_q_heads / Hkv;
+  const unsigned block = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+  const int index = (int)(block / (unsigned)Hkv), g = (int)(block - (unsigned)index * Hkv), tid = threadIdx.x;
+  if (index >= a.n_runs) return;
+  const HfxRun run = a.runs[index];
+  const int tok = tid / (D / 8), piece = tid % (D / 8), lane = tid & 63;
+  const bool live = tok < run.n;
+  const bool any = a.rot > 0;
+  Turn t;
+  if (any) t = turn_of<Interleaved>(a.cos_sin + (long)(a.run_pos[index] + min(tok, run.n - 1)) * a.rot, a.rot, piece, lane);
+  const long row = (long)run.row0 + tok;
+  u32x4 kv = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
+  if (live) {
+    kv = *reinterpret_cast<const u32x4*>(a.k + row * a.k_stride + g * D + piece * 8);
+    vv = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + g * D + piece * 8);
+  }
+  if (a.q) {
+    for (int h = g * G; h < (g + 1) * G; ++h) {
+      u32x4 qv = {0, 0, 0, 0};
+      if (live) qv = *reinterpret_cast<const u32x4*>(a.q + row * a.q_stride + h * D + piece * 8);
+      float y[8];
+      turn<Interleaved>(t, any, qv, y);
+      if (live) *reinterpret_cast<u32x4*>(a.q_out + (row * a.num_q_heads + h) * D + piece * 8) = narrow(y);
+    }
+  }
+  float y[8];
+  turn<Interleaved>(t, any, kv, y);
+  const int slot = run.slot0 + tok;
+  if constexpr (!Four) {
+    uint16_t* kblk = reinterpret_cast<uint16_t*>(a.pool) + (((long)run.page * Hkv + g) * 2) * (16L * D);
+    if (live) {
+      *reinterpret_cast<u32x4*>(kblk + ((piece >> 1) * HFX_PAGE + slot) * 16 + (piece & 1) * 8) = any ? narrow(y) : kv;
+      *reinterpret_cast<u32x4*>(sv + slot * LD + piece * 8) = vv;
+    }
+    __syncthreads();
+    store_value_columns<D>(kblk + 16L * D, sv, LD, tid, run.slot0, run.n);
+  } else {
+    constexpr int kG = D / 32;
+    char* blk = reinterpret_cast<char*>(a.pool) + ((long)run.page * Hkv + g) * Mx<D>::kBlock;
+    const int group = piece >> 2, part = piece & 3;
+    const unsigned ke = scale_byte(block_top(y));
+    const unsigned kc = to_fp4(y, ke);
+    float x[8];
+    widen(vv, x);
+    const unsigned ve = scale_byte(block_top(x));
+    const unsigned vc = to_fp4(x, ve);
+    // a byte of value codes holds dimensions i and i + 16: lanes part and part ^ 2 join theirs, each for four of the eight
+    const unsigned other = (unsigned)__builtin_amdgcn_mov_dpp((int)vc, 0x4e, 0xf, 0xf, true);
+    const unsigned low = part < 2 ? vc : other >> 16, high = part < 2 ? other : vc >> 16;
+    if (live) {
+      *reinterpret_cast<unsigned*>(blk + (slot * kG + group) * 16 + part * 4) = kc;
+      const int half = slot >> 3, at = slot & 7, tp = group >> 1, w = group & 1;
+      const int i0 = 8 * (part & 1) + (part < 2 ? 0 : 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        s4[half * Mx<D>::kHalf + ((tp * 16 + i0 + i) * 2 + w) * 8 + at] = (uint8_t)((low >> (4 * i) & 15u) | (high >> (4 * i) & 15u) << 4);
+      if (part == 0) {
+        s4[8 * D + slot * kG + group] = (uint8_t)ke;
+        s4[8 * D + D / 2 + half * Mx<D>::kHalfScales + (tp * 8 + at) * 2 + w] = (uint8_t)ve;
+      }
+    }
+    __syncthreads();
+    // four bytes at a time where the run has all of their tokens, else those of its tokens
+    for (int i = tid; i < 9 * D / 4; i += 2 * D) {
+      const int b = 4 * i;
+      int first, step;          // token of byte b, and 4 / how many bytes a token has in a row
+      if (b < 8 * D) {
+        first = b / Mx<D>::kHalf * 8 + (b & 7);
+        step = 1;
+      } else if (b < 8 * D + D / 2) {
+        first = (b - 8 * D) / kG;
+        step = -kG;
+      } else {
+        const int r = b - 8 * D - D / 2;
+        first = r / Mx<D>::kHalfScales * 8 + (r & 15) / 2;
+        step = -2;
+      }
+      const int last = step > 0 ? first + 3 : first + 3 / -step;
+      const int lo = run.slot0, hi = run.slot0 + run.n;
+      if (first >= lo && last < hi) {
+        *reinterpret_cast<unsigned*>(blk + Mx<D>::kValues + b) = *reinterpret_cast<const unsigned*>(s4 + b);
+      } else if (last >= lo && first < hi) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int token = step > 0 ? first + e : first + e / -step;
+          if (token >= lo && token < hi) blk[Mx<D>::kValues + b + e] = (char)s4[b + e];
+        }
+      }
+    }
+  }
+}
+
+// The way back: bf16 rows [T][Hkv][D] of the values that the 4-bit pages hold for the step's tokens, one workgroup of 2 D threads per (run, kv-head).
+template <int D>
+__global__ __launch_bounds__(2 * D) void read_new_kv_mx_kernel(const HfxRun* __restrict__ runs, int n_runs, int Hkv, const char* __restrict__ pool,
+                                                             uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out) {
+  __shared__ __attribute__((aligned(16))) uint8_t s4[9 * D];
+  constexpr int kG = D / 32;
+  const unsigned block = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+  const int index = (int)(block / (unsigned)Hkv), g = (int)(block - (unsigned)index * Hkv), tid = threadIdx.x;
+  if (index >= n_runs) return;
+  const HfxRun run = runs[index];
+  const char* blk = pool + ((long)run.page * Hkv + g) * Mx<D>::kBlock;
+  for (int i = tid; i < 9 * D / 4; i += 2 * D) *reinterpret_cast<unsigned*>(s4 + 4 * i) = *reinterpret_cast<const unsigned*>(blk + Mx<D>::kValues + 4 * i);
+  __syncthreads();
+  const int tok = tid / (D / 8), piece = tid % (D / 8);
+  if (tok >= run.n) return;
+  const int slot = run.slot0 + tok, group = piece >> 2, part = piece & 3;
+  const unsigned kc = *reinterpret_cast<const unsigned*>(blk + (slot * kG + group) * 16 + part * 4);
+  const int half = slot >> 3, at = slot & 7, tp = group >> 1, w = group & 1;
+  unsigned vc = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const unsigned b = s4[half * Mx<D>::kHalf + ((tp * 16 + 8 * (part & 1) + i) * 2 + w) * 8 + at];
+    vc |= (part < 2 ? b & 15u : b >> 4) << (4 * i);
+  }
+  const unsigned ke = scale_at<0>(s4[8 * D + slot * kG + group]);
+  const unsigned ve = scale_at<0>(s4[8 * D + D / 2 + half * Mx<D>::kHalfScales + (tp * 8 + at) * 2 + w]);
+  const long to = (((long)run.row0 + tok) * Hkv + g) * D + piece * 8;
+  *reinterpret_cast<u32x4*>(k_out + to) = u32x4{from_fp4<0>(kc, ke), from_fp4<1>(kc, ke), from_fp4<2>(kc, ke), from_fp4<3>(kc, ke)};
+  *reinterpret_cast<u32x4*>(v_out + to) = u32x4{from_fp4<0>(vc, ve), from_fp4<1>(vc, ve), from_fp4<2>(vc, ve), from_fp4<3>(vc, ve)};
+}
+
+// A workgroup for each (run, kv-head); the runs fill the two slower dimensions, the first of which holds at most 65535.
+static dim3 run_grid(const HfxHeader& h) {
+  const unsigned per_z = (unsigned)std::min(h.n_runs, 32768);
+  return dim3((unsigned)h.num_kv_heads, per_z, ((unsigned)h.n_runs + per_z - 1) / per_z);
+}
+
+hipError_t launch_rope_append(const HfxHeader& h, const void* desc, RopeAppend a, bool four, hipStream_t stream) {
+  if (h.n_runs <= 0) return hipSuccess;
+  a.runs = reinterpret_cast<const HfxRun*>(static_cast<const char*>(desc) + h.off_runs);
+  a.run_pos = reinterpret_cast<const int*>(static_cast<const char*>(desc) + h.off_run_pos);
+  a.n_runs = h.n_runs;
+  a.num_q_heads = h.num_q_heads;
+  a.num_kv_heads = h.num_kv_heads;
+  const unsigned threads = 2u * (unsigned)h.head_dim;
+  void (*const kernels[])(RopeAppend) = {rope_append_kernel<64, false, false>,  rope_append_kernel<64, false, true>,  rope_append_kernel<64, true, false>,
+                                         rope_append_kernel<64, true, true>,    rope_append_kernel<128, false, false>, rope_append_kernel<128, false, true>,
+                                         rope_append_kernel<128, true, false>,  rope_append_kernel<128, true, true>};
+  return launch(kernels[(h.head_dim == 128 ? 4 : 0) + (four ? 2 : 0) + (a.interleaved ? 1 : 0)], run_grid(h), threads, stream, a);
+}
+
+hipError_t launch_read_new_kv_mx(const HfxHeader& h, const void* desc, const void* pool, void* k_out, void* v_out, hipStream_t stream) {
+  if (h.n_runs <= 0) return hipSuccess;
+  const HfxRun* runs = reinterpret_cast<const HfxRun*>(static_cast<const char*>(desc) + h.off_runs);
+  return launch(h.head_dim == 128 ? read_new_kv_mx_kernel<128> : read_new_kv_mx_kernel<64>, run_grid(h), 2u * (unsigned)h.head_dim, stream, runs, h.n_runs,
+                h.num_kv_heads, static_cast<const char*>(pool), static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out));
+}
+
+}  // namespace hfx

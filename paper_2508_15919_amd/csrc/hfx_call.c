@@ -140,7 +140,8 @@ static int int32_array(const Caller* self, PyObject* o, Held* held, uint64_t* ad
   return 0;
 }
 
-typedef int32_t (*Function)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t);
+typedef int32_t (*Function)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t,
+                            uint64_t);
 
 static PyObject* call(PyObject* callable, PyObject* const* args, size_t nargsf, PyObject* kwnames) {
   const Caller* self = (const Caller*)callable;
@@ -200,7 +201,7 @@ static PyObject* call(PyObject* callable, PyObject* const* args, size_t nargsf, 
   if (!bad) {
     // Integers and pointers travel alike, in order, and a function takes no notice of what is behind its own (System V, x86-64).
     Py_BEGIN_ALLOW_THREADS
-    status = ((Function)(uintptr_t)self->function)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11]);
+    status = ((Function)(uintptr_t)self->function)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12]);
     Py_END_ALLOW_THREADS
   }
   release(&held);
@@ -224,8 +225,8 @@ static int caller_init(PyObject* o, PyObject* args, PyObject* kwargs) {
     held += strchr("SKAka", kinds[n]) != NULL;
     self->kinds[n] = kinds[n];
   }
-  if (kinds[n] || words > 12 || held > MAX_HELD || address == 0) {
-    PyErr_SetString(PyExc_ValueError, "kinds of at most 12 arguments out of SPBKAkaizs, at most 8 of them SKAka, and an address");
+  if (kinds[n] || words > 13 || held > MAX_HELD || address == 0) {
+    PyErr_SetString(PyExc_ValueError, "kinds of at most 13 arguments out of SPBKAkaizs, at most 8 of them SKAka, and an address");
     return -1;
   }
   self->n_kinds = n;

@@ -1,0 +1,755 @@
+// Attention of a scheduled step over a page pool held in 4 bits (see hfx_mx.h for the format): the same work items, queue and split merge as over
+// the bf16 pool, with kernels of their own for both kinds of items.
+//
+//   S^T = K . Q^T   on the scaled 4-bit matrix instructions: the keys' codes and scale bytes go into them as they lie in the cache.  Their other
+//                   operand has 8 bits, so a query is taken as the sum of two 8-bit numbers, each with a scale for 32 dimensions: a bf16 value has 8
+//                   significant bits, the first number (e4m3) has 4 of them and the rest, rounded nowhere, fits the second.  Two products at twice the
+//                   rate of a bf16 one: the same matrix time, and no key is ever converted.
+//   O^T = V^T . P^T on the bf16 matrix instructions: a scale belongs to a token, which is the contracted index here, so the values are widened to bf16
+//                   (every code times every scale is a bf16 number).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "hfx_desc.h"
+#include "hfx_device.h"
+#include "hfx_mx.h"
+#include "hfx_launch.h"
+
+namespace hfx {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// Operand formats of the scaled matrix instructions.
+constexpr int kFp8 = 0, kFp4 = 4;
+
+// The 4-bit operand takes four registers of the eight that the builtins ask for.
+__device__ __forceinline__ i32x8 fp4_operand(const u32x4& c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
+
+// Scale byte for query values whose largest magnitude has the bits `top`: that value comes into [128, 256) of e4m3's 448.  The remainder is
+// at most 8 there and has a scale 2^4 times finer.  Values 2^-13 of the largest and more are taken exactly, smaller ones to 2^-22 of it.
+__device__ __forceinline__ unsigned query_scale(unsigned top) { return (unsigned)max((int)(top >> 23) - 7, 5); }
+constexpr unsigned kRestScale = 4;
+
+// Eight query values as 8 + 8 numbers of 8 bits under scale byte e: two registers of first numbers, two of remainders.
+__device__ __forceinline__ void split_query(const bf16x8& q, unsigned e, int* first, int* rest) {
+  const float up = __builtin_bit_cast(float, (254 - e) << 23);
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)q[i] * up;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    int f = 0, r = 0;
+    f = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w], x[4 * w + 1], f, false);
+    f = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2], x[4 * w + 3], f, true);
+    const float r0 = (x[4 * w] - __builtin_amdgcn_cvt_f32_fp8(f, 0)) * 16.f, r1 = (x[4 * w + 1] - __builtin_amdgcn_cvt_f32_fp8(f, 1)) * 16.f;
+    const float r2 = (x[4 * w + 2] - __builtin_amdgcn_cvt_f32_fp8(f, 2)) * 16.f, r3 = (x[4 * w + 3] - __builtin_amdgcn_cvt_f32_fp8(f, 3)) * 16.f;
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(r0, r1, r, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(r2, r3, r, true);
+    first[w] = f;
+    rest[w] = r;
+  }
+}
+
+// Bits of the largest magnitude of eight values.
+__device__ __forceinline__ unsigned top_of(const bf16x8& q) {
+  const u32x4 u = __builtin_bit_cast(u32x4, q);
+  unsigned top = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = max(top, max(u[w] & 0x7fff0000u, u[w] << 16 & 0x7fff0000u));
+  return top;
+}
+
+// Values of eight tokens and two dimensions, i and i + 16 of 32, out of eight codes bytes (a, b) and the tokens' scale bytes: token 2k's is byte
+// `At` of scales[k], token 2k + 1's byte At + 2.  lo and hi are the operand registers of the two dimensions: eight tokens in a row each.
+template <int At>
+__device__ __forceinline__ void widen_values(unsigned a, unsigned b, const u32x4& scales, u32x4& lo, u32x4& hi) {
+  const unsigned t0 = from_fp4<0>(a, scale_at<At>(scales[0])), t1 = from_fp4<1>(a, scale_at<At + 2>(scales[0]));
+  const unsigned t2 = from_fp4<2>(a, scale_at<At>(scales[1])), t3 = from_fp4<3>(a, scale_at<At + 2>(scales[1]));
+  const unsigned t4 = from_fp4<0>(b, scale_at<At>(scales[2])), t5 = from_fp4<1>(b, scale_at<At + 2>(scales[2]));
+  const unsigned t6 = from_fp4<2>(b, scale_at<At>(scales[3])), t7 = from_fp4<3>(b, scale_at<At + 2>(scales[3]));
+  constexpr unsigned kLow = 0x05040100u, kHigh = 0x07060302u;
+  lo = u32x4{__builtin_amdgcn_perm(t1, t0, kLow), __builtin_amdgcn_perm(t3, t2, kLow), __builtin_amdgcn_perm(t5, t4, kLow),
+             __builtin_amdgcn_perm(t7, t6, kLow)};
+  hi = u32x4{__builtin_amdgcn_perm(t1, t0, kHigh), __builtin_amdgcn_perm(t3, t2, kHigh), __builtin_amdgcn_perm(t5, t4, kHigh),
+             __builtin_amdgcn_perm(t7, t6, kHigh)};
+}
+
+// ----------------------------------------------------------------------------------------------
+// Decode item: as over the bf16 pool one wavefront per kv-head (hn of them), the others interleave over page pairs.  Per pair (32 tokens) and kv-head a
+// wavefront takes 4352 bytes (D = 128).
+//   S^T[token][head]: 16x16x128, a lane has 32 dimensions of one key (a group) with their scale; D = 64: lanes of the upper half have the
+//                     same keys again, and the queries' remainders there, so that one instruction does both products.
+//   O^T[d][head]    : 16x16x32 bf16, a lane has eight tokens of dimension n of each tile.
+// ----------------------------------------------------------------------------------------------
+template <int D>
+struct PairRegs4 {
+  u32x4 ka, kb;                          // key codes of the two score tiles
+  unsigned sa, sb;                       // and scale bytes
+  u32x4 v[D / 64], vs[D / 64];           // value codes and scales of 64 dimensions
+};
+
+// Lane's parts of the addresses inside a block.
+struct DecodeLane4 {
+  int key, key_scale, value, value_scale;
+  bool key_second, value_second;         // page of the pair
+};
+
+template <int D>
+__device__ __forceinline__ void decode_load4(PairRegs4<D>& r, const char* pool, int pg0, int pg1, int Hkv, int g, const DecodeLane4& a) {
+  const char* kp = pool + ((long)(a.key_second ? pg1 : pg0) * Hkv + g) * Mx<D>::kBlock;
+  const char* vp = pool + ((long)(a.value_second ? pg1 : pg0) * Hkv + g) * Mx<D>::kBlock;
+  r.ka = *reinterpret_cast<const u32x4*>(kp + a.key);
+  r.kb = *reinterpret_cast<const u32x4*>(kp + a.key + 4 * (D / 2));
+  r.sa = *reinterpret_cast<const uint8_t*>(kp + a.key_scale);
+  r.sb = *reinterpret_cast<const uint8_t*>(kp + a.key_scale + 4 * Mx<D>::kGroups);
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    r.v[i] = *reinterpret_cast<const u32x4*>(vp + a.value + i * 256);
+    r.vs[i] = *reinterpret_cast<const u32x4*>(vp + a.value_scale + i * 16);
+  }
+}
+
+template <int D>
+struct DecodeQuery4 {
+  i32x8 q[D / 64];        // D = 128: first numbers, remainders; D = 64: both in one
+  unsigned scale;         // bytes: of q[0], of q[1]
+};
+
+template <int D>
+__device__ __forceinline__ f32x4 decode_scores4(const u32x4& k, unsigned ks, const DecodeQuery4<D>& q) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), q.q[0], s, kFp4, kFp8, 0, (int)ks, 0, (int)q.scale);
+  if constexpr (D == 128) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), q.q[1], s, kFp4, kFp8, 0, (int)ks, 1, (int)q.scale);
+  return s;
+}
+
+template <int D>
+__device__ __forceinline__ void decode_compute4(PairRegs4<D>& r, const DecodeQuery4<D>& q, f32x4* o, float& m, float& l, float sl2, int nv) {
+  const f32x4 sa = decode_scores4<D>(r.ka, r.sa, q), sb = decode_scores4<D>(r.kb, r.sb, q);
+  float s[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    s[e] = sa[e] * sl2;
+    s[4 + e] = sb[e] * sl2;
+  }
+  if (nv < 8) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = keep_or_neg_inf(s[e], e < nv);
+  }
+  float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+  const float mn = fmaxf(m, mx);
+  const float alpha = fast_exp2(m - mn);
+  float ps = 0.f;
+  bf16x8 pb;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float p = fast_exp2(s[e] - mn);
+    ps += p;
+    pb[e] = (__bf16)p;
+  }
+  l = l * alpha + ps;
+  m = mn;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) {
+    u32x4 lo, hi;
+    if (t % 2 == 0) widen_values<0>(r.v[t / 2][0], r.v[t / 2][1], r.vs[t / 2], lo, hi);
+    else widen_values<1>(r.v[t / 2][2], r.v[t / 2][3], r.vs[t / 2], lo, hi);
+    bf16x8 v0 = __builtin_bit_cast(bf16x8, lo), v1 = __builtin_bit_cast(bf16x8, hi);
+    if (nv < 8) {          // unused slots hold anything
+      v0 = keep_first(v0, nv);
+      v1 = keep_first(v1, nv);
+    }
+    o[2 * t] *= alpha;
+    o[2 * t + 1] *= alpha;
+    o[2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pb, o[2 * t], 0, 0, 0);
+    o[2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pb, o[2 * t + 1], 0, 0, 0);
+  }
+}
+
+// Query operand of a kv-head's q-heads (column n), zero past the group.  The 8-bit operand of 16x16x128 has dimensions 16j .. 16j + 15 and 64 + 16j ..
+// in lane group j, and lane group i names the scale of dimensions 32i ...
+template <int D>
+__device__ __forceinline__ DecodeQuery4<D> decode_query4(const __bf16* q, const HfxItem& item, int g, int Hq, int G, int n, int j) {
+  const int hh = n < G ? n : G - 1;
+  const __bf16* row = q + ((long)item.rq.q_start * Hq + g * G + hh) * D + j * 16;
+  bf16x8 x[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) x[i] = keep_first(ld16(row + (i >> 1) * 64 + (i & 1) * 8), n < G ? 8 : 0);
+  DecodeQuery4<D> r;
+  unsigned e[D / 64];
+#pragma unroll
+  for (int p = 0; p < D / 64; ++p) {
+    unsigned top = max(top_of(x[2 * p]), top_of(x[2 * p + 1]));
+    top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));        // the two lanes that share 32 dimensions
+    e[p] = query_scale(top);
+  }
+  const int from = (j & 1) * 32 + n;                               // of lane groups 0 and 1 (and 2, 3): the first 32 dimensions of 64, and the second
+  if constexpr (D == 128) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int f[2], s[2];
+      split_query(x[i], e[i >> 1], f, s);
+      r.q[0][2 * i] = f[0];
+      r.q[0][2 * i + 1] = f[1];
+      r.q[1][2 * i] = s[0];
+      r.q[1][2 * i + 1] = s[1];
+    }
+    const unsigned e0 = (unsigned)__shfl((int)e[0], from, 64), e1 = (unsigned)__shfl((int)e[D / 64 - 1], from, 64);
+    const unsigned own = j < 2 ? e0 : e1;
+    r.scale = own | (own - kRestScale) << 8;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int f[2], s[2];
+      split_query(x[i], e[0], f, s);
+      r.q[0][2 * i] = f[0];
+      r.q[0][2 * i + 1] = f[1];
+      r.q[0][4 + 2 * i] = s[0];
+      r.q[0][4 + 2 * i + 1] = s[1];
+    }
+    const unsigned e0 = (unsigned)__shfl((int)e[0], from, 64);
+    r.scale = j < 2 ? e0 : e0 - kRestScale;
+  }
+  return r;
+}
+
+// Runs the decode item t.cur and carries on for as long as the workgroup's next item is a decode item too, as over the bf16 pool.
+template <int D>
+__device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
+                            char* smem) {
+  const int tid = threadIdx.x;
+  int lane = tid & 63;
+  asm volatile("" : "+v"(lane));     // what follows from it is formed per run, not kept in registers through prefill runs
+  const int wave = uniform(tid >> 6);
+  const int Hq = H->num_q_heads, Hkv = H->num_kv_heads;
+  const int G = Hq / Hkv;
+  const int n = lane & 15, j = lane >> 4;
+  const float sl2 = H->softmax_scale * 1.4426950408889634f;
+  const int* bt = reinterpret_cast<const int*>(a.desc + H->off_bt);
+  const char* pool = reinterpret_cast<const char*>(a.pool);
+  // Row rho of score tile A is token ((rho>>2)&1)*8 + (rho&3) of page rho>>3, of tile B the token 4 further on; so a lane holds the scores of 8
+  // tokens in a row, (j&1)*8.. of page j>>1, which are the ones it takes of the values.
+  constexpr int kG = Mx<D>::kGroups;
+  const int token = ((n >> 2) & 1) * 8 + (n & 3), group = j & (kG - 1);
+  DecodeLane4 la;
+  la.key_second = (n >> 3) != 0;
+  la.key = (token * kG + group) * 16;
+  la.key_scale = Mx<D>::kKeyScales + token * kG + group;
+  la.value_second = (j >> 1) != 0;
+  la.value = Mx<D>::kValues + (j & 1) * Mx<D>::kHalf + n * 16;
+  la.value_scale = Mx<D>::kValueScales + (j & 1) * Mx<D>::kHalfScales;
+  const int tok_lane = (j >> 1) * 16 + (j & 1) * 8;   // first of this lane's 8 tokens inside the pair
+
+  HfxItem it = items[t.cur];
+  DecodeWave d = decode_wave(bt, it, wave);
+  PairRegs4<D> r0, r1;
+  if (d.pp < d.pe) decode_load4<D>(r0, pool, d.a0, d.a1, Hkv, d.g, la);
+  DecodeQuery4<D> qf = decode_query4<D>(a.q, it, d.g, Hq, G, n, j);
+
+  for (;;) {
+    // the record of the next item and, if it is a decode item, this wavefront's share of it
+    const HfxItem nx = items[t.nxt < n_items ? t.nxt : t.cur];
+    const bool carry_on = t.nxt < n_items && nx.type == HFX_ITEM_DECODE;
+    const DecodeWave dn = decode_wave(bt, nx, wave);
+
+    f32x4 o[D / 16];
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = NEG_INF, l = 0.f;
+    const int step = d.step, pe = d.pe, tend = d.tend, g = d.g;
+    int pp = d.pp;
+    int a0 = d.a0, a1 = d.a1, b0 = d.b0, b1 = d.b1;
+    bool reserved = false;
+    int pending = 0;
+    // page ids are fetched one pair ahead of the loads that need them
+    while (pp < pe) {
+      if (!reserved && pp + 4 * step >= pe) {   // a few pairs before the end (thread 0 sits in the first wavefront, which always has pairs)
+        tickets_reserve(t, pending, ctrl);
+        reserved = true;
+      }
+      if (pp + step < pe) decode_load4<D>(r1, pool, b0, b1, Hkv, g, la);
+      if (pp + 2 * step < pe) {
+        a0 = decode_page(bt, d, pp + 2 * step);
+        a1 = decode_page(bt, d, pp + 2 * step + 1);
+      }
+      {
+        const int nv = tend - (pp * HFX_PAGE + tok_lane);
+        if ((pp + 2) * HFX_PAGE <= tend) decode_compute4<D>(r0, qf, o, m, l, sl2, 8);
+        else decode_compute4<D>(r0, qf, o, m, l, sl2, nv);
+      }
+      pp += step;
+      if (pp >= pe) break;
+      if (pp + step < pe) decode_load4<D>(r0, pool, a0, a1, Hkv, g, la);
+      if (pp + 2 * step < pe) {
+        b0 = decode_page(bt, d, pp + 2 * step);
+        b1 = decode_page(bt, d, pp + 2 * step + 1);
+      }
+      {
+        const int nv = tend - (pp * HFX_PAGE + tok_lane);
+        if ((pp + 2) * HFX_PAGE <= tend) decode_compute4<D>(r1, qf, o, m, l, sl2, 8);
+        else decode_compute4<D>(r1, qf, o, m, l, sl2, nv);
+      }
+      pp += step;
+    }
+    tickets_publish(t, pending, s_tk, ctrl, H);
+    // both register sets and the query operand are free now: start on the next item
+    if (carry_on) {
+      if (dn.pp < dn.pe) decode_load4<D>(r0, pool, dn.a0, dn.a1, Hkv, dn.g, la);
+      qf = decode_query4<D>(a.q, nx, dn.g, Hq, G, n, j);
+    }
+    decode_store<D>(a, H, it, o, m, l, Hq, G, tid, wave, n, j, smem);
+    __syncthreads();                  // frees the LDS partials; the ticket was published before the barrier in decode_store
+    tickets_take(t, s_tk, n_items);
+    if (!carry_on) break;
+    it = nx;
+    d = dn;
+  }
+}
+
+// ----------------------------------------------------------------------------------------------
+// Prefill item: four wavefronts, each with 32 chunk rows of one q-head, all sharing the kv-head.  Keys arrive in steps of 64 (four pages, one a
+// wavefront): the wavefront copies its page's block into a ring of raw slots with direct-to-LDS loads, two to three steps ahead of its use; key codes are
+// read from there as operands by all four, and the value codes are widened to bf16 by the wavefront that copied them, a step ahead of
+// their use, into one of two slots in operand order.  So each value is widened once a workgroup, not once a wavefront.
+//   S^T[key][row]  = K . Q^T     32x32x64 scaled, keys' codes against the two numbers of the queries
+//   O^T[d][row]   += V^T . P^T   32x32x16 bf16, as over the bf16 pool
+// ----------------------------------------------------------------------------------------------
+template <int D>
+struct Smem4 {
+  static constexpr int kRawPage = 16 * D + 256;        // key codes [group][16 keys][16 bytes], value codes, then the scales as in the block (the copy of them writes 256 bytes)
+  static constexpr int kRawStep = 4 * kRawPage;
+  static constexpr int kRawSteps = 3;
+  static constexpr int kValuePage = 32 * D;            // [D / 32][32 dimensions][2 halves of 8 tokens] bf16, halves of rows 8-15 and 24-31 swapped
+  static constexpr int kValueStep = 4 * kValuePage;
+  static constexpr int kRing = kRawSteps * kRawStep;
+  static constexpr int kBytes = kRing + 2 * kValueStep > decode_part_bytes(D) ? kRing + 2 * kValueStep : decode_part_bytes(D);
+  static constexpr int kCopies = D == 128 ? 3 : 2;     // instructions that copy a page
+};
+constexpr int kStepKeys = 64;
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// The block of one page: base (scalar), offsets of the lane's 16 bytes of keys, of values and 4 bytes of scales, LDS destination.
+template <int D>
+__device__ __forceinline__ void raw_copy(const char* base, unsigned keys, unsigned values, unsigned scales, unsigned lds) {
+  if constexpr (D == 128)
+    asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %3\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024\n\t"
+                 "global_load_lds_dword %2, %3 offset:2048"
+                 :: "v"(keys), "v"(values), "v"(scales), "s"(base), "s"(lds) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dword %1, %2 offset:1024"
+                 :: "v"(keys), "v"(scales), "s"(base), "s"(lds) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int D>
+struct PrefillWave4 {
+  f32x16 o[D / 32];            // O^T accumulators per 32-dimension block
+  i32x8 q[D / 64][2];          // of 64 dimensions: first numbers, remainders
+  unsigned qs;                 // their scale bytes, in that order
+  float m, l;                  // reference exponent (base-2 domain) and running sum
+};
+
+// Operand registers of a stage's 32 keys.
+template <int D>
+struct Keys4 {
+  u32x4 k[D / 64];
+  unsigned scale;              // byte 2i: of k[i]
+};
+
+template <int D>
+__device__ __forceinline__ Keys4<D> read_keys4(const char* stage, int k_lane, int s_lane, int j) {
+  Keys4<D> r;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) r.k[i] = *reinterpret_cast<const u32x4*>(stage + k_lane + i * 512);
+  if constexpr (D == 128) r.scale = *reinterpret_cast<const unsigned*>(stage + s_lane) >> (8 * j);
+  else r.scale = (unsigned)*reinterpret_cast<const uint16_t*>(stage + s_lane) >> (8 * j);
+  return r;
+}
+
+// Matrix instruction number i of a stage's scores: 64 dimensions i / 2, the first numbers or the remainders.
+template <int D>
+__device__ __forceinline__ f32x16 score_product(const PrefillWave4<D>& w, const Keys4<D>& k, int i, f32x16 s) {
+  if (i == 0) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[0]), w.q[0][0], s, kFp4, kFp8, 0, (int)k.scale, 0, (int)w.qs);
+  if (i == 1) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[0]), w.q[0][1], s, kFp4, kFp8, 0, (int)k.scale, 1, (int)w.qs);
+  if (i == 2) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[D / 64 - 1]), w.q[D / 64 - 1][0], s, kFp4, kFp8, 2, (int)k.scale, 2, (int)w.qs);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[D / 64 - 1]), w.q[D / 64 - 1][1], s, kFp4, kFp8, 2, (int)k.scale, 3, (int)w.qs);
+}
+
+// Scores of an item's first stage; the accumulators are cleared between the instructions.
+template <int D>
+__device__ __forceinline__ f32x16 first_scores4(PrefillWave4<D>& w, const Keys4<D>& k) {
+  f32x16 s;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    s = score_product<D>(w, k, i, s);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      float zero = 0.f;
+      asm volatile("" : "+v"(zero));
+      w.o[i][v] = zero;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  return s;
+}
+
+template <int D>
+__device__ __forceinline__ bf16x8 value_fragment4(const char* values, int i, int v_lane) {
+  constexpr int B = D / 32;
+  return *reinterpret_cast<const bf16x8*>(values + (i / B) * Smem4<D>::kValuePage + (i % B) * 1024 + v_lane);
+}
+
+// First phase of a stage: scores of the next one, the second half of the weights of the present one (scores cur) between them, and the present
+// stage's value fragments.
+template <int D>
+__device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, const Keys4<D>& k, bf16x8* frag, const f32x16& cur, Weighing& wt, float sl2,
+                                                const char* values, int v_lane) {
+  constexpr int S = D / 16;
+  f32x16 acc;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+#pragma unroll
+  for (int i = 0; i < S / 2; ++i) {
+    acc = score_product<D>(w, k, i, acc);
+#pragma unroll
+    for (int h = 2 * i; h < 2 * i + 2; ++h) {
+      frag[h] = value_fragment4<D>(values, h, v_lane);
+      wt.portion(h == 0 ? Share<D>::values[S - 1] : Share<D>::scores[h - 1], Share<D>::scores[h], Share<D>::scores[h + 1], cur, sl2, w.m);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  wt.portion(Share<D>::scores[S - 1], 16, 16, cur, sl2, w.m);
+  return acc;
+}
+
+// Second phase: weighted values of the present stage, the first half of the weights of the next one (scores next) between them, and the keys of the
+// stage after next.
+template <int D>
+__device__ __forceinline__ void values_phase4(PrefillWave4<D>& w, const bf16x8* frag, const bf16x8* pb, const f32x16& next, Weighing& wt, float sl2) {
+  constexpr int B = D / 32, S = 2 * B;
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    w.o[i % B] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i], pb[i / B], w.o[i % B], 0, 0, 0);
+    wt.portion(i == 0 ? 0 : Share<D>::values[i - 1], Share<D>::values[i], Share<D>::values[i + 1], next, sl2, w.m);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// Query operands of this lane's row (rows past the chunk read the last row and are never stored).  The 8-bit operand of 32x32x64 has dimensions
+// 16j .. 16j + 15 and 32 + 16j .. of 64 in lane group j, and lane group i names the scale of dimensions 32i ...
+template <int D>
+__device__ __forceinline__ void query_rows4(PrefillWave4<D>& w, const bf16x8 (*x)[4]) {
+  w.qs = 0;
+  const int j = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    unsigned e[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const unsigned top = max(top_of(x[i][2 * p]), top_of(x[i][2 * p + 1]));
+      const Pair32 both = swap32(__builtin_bit_cast(float, top));
+      e[p] = query_scale(max(__builtin_bit_cast(unsigned, both.lo), __builtin_bit_cast(unsigned, both.hi)));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int f[2], r[2];
+        split_query(x[i][2 * p + h], e[p], f, r);
+        w.q[i][0][4 * p + 2 * h] = f[0];
+        w.q[i][0][4 * p + 2 * h + 1] = f[1];
+        w.q[i][1][4 * p + 2 * h] = r[0];
+        w.q[i][1][4 * p + 2 * h + 1] = r[1];
+      }
+    }
+    const unsigned own = j ? e[1] : e[0];
+    w.qs |= (own | (own - kRestScale) << 8) << (16 * i);
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void query_load4(bf16x8 (*x)[4], const __bf16* q, int row0, int last, int Hq, int n, int j) {
+  const __bf16* qp = q + (long)min(row0 + n, last) * Hq * D + j * 16;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+    for (int p = 0; p < 4; ++p) x[i][p] = ld16(qp + i * 64 + (p >> 1) * 32 + (p & 1) * 8);
+}
+
+__device__ __forceinline__ int item_steps(const HfxItem& it) { return (int)((unsigned)(it.ke - it.kb + kStepKeys - 1) / kStepKeys); }
+
+// What the loop over an item's steps needs to know of the item after it.
+struct NextItem4 {
+  int left, bt, last, head;
+};
+
+template <int D>
+__device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
+                             char* smem, char* o_stage) {
+  typedef Smem4<D> L;
+  constexpr int SK = HFX_STAGE_KEYS, S = D / 16;
+  const int tid = threadIdx.x;
+  int lane = tid & 63;
+  asm volatile("" : "+v"(lane));     // what follows from it is formed per run, not kept in registers through decode runs
+  const int wave = uniform(tid >> 6);
+  const int Hq = H->num_q_heads, Hkv = H->num_kv_heads;
+  const int G = Hq / Hkv;
+  const int n = lane & 31, j = lane >> 5;
+  char* stage = o_stage + wave * 2048;
+  const float sl2 = H->softmax_scale * 1.4426950408889634f;
+  const int* __restrict__ bt = reinterpret_cast<const int*>(a.desc + H->off_bt);
+  const char* pool = reinterpret_cast<const char*>(a.pool);
+  // row of this lane's key inside a stage's 32 keys (as over the bf16 pool)
+  const int krow = (n >> 4) * 16 + ((n >> 2) & 1) * 8 + ((n >> 3) & 1) * 4 + (n & 3);
+  const int k_lane = (krow >> 4) * L::kRawPage + j * 256 + (krow & 15) * 16;
+  const int s_lane = (krow >> 4) * L::kRawPage + Mx<D>::kKeyScales + (krow & 15) * Mx<D>::kGroups;
+  const int v_lane = (n * 2 + (j ^ ((n >> 3) & 1))) * 16;   // V^T rows 32b + n, keys 8j.. of a page
+  char* const values = smem + L::kRing;
+  // copies: a page's keys change their order from [key][group] to [group][key]
+  constexpr int kG = Mx<D>::kGroups;
+  const unsigned c_keys = D == 128 || lane < 32 ? (unsigned)(((lane & 15) * kG + ((lane >> 4) & (kG - 1))) * 16) : (unsigned)lane * 16;
+  const unsigned c_values = (unsigned)lane * 16, c_scales = (unsigned)(lane & (D / 4 - 1)) * 4;
+  const unsigned lds_raw = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * L::kRawPage;
+  // widening: this lane's value codes in the raw page, their scales, and where its dimensions go
+  const int half = lane >> 5;
+  const int w_codes = Mx<D>::kValues + lane * (D / 8);
+  const int w_scales = Mx<D>::kValueScales + (D == 128 ? (lane >> 4) * 16 : half * 16);
+  const int w_i = D == 128 ? lane & 15 : (lane >> 1) & 15;
+  const int w_to = (D == 128 ? ((lane >> 4) & 1) * 2048 : (lane & 1) * 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
+
+  HfxItem it = items[t.cur];
+  HfxItem item1 = items[t.nxt < n_items ? t.nxt : t.cur];
+  bool next_ok = t.nxt < n_items && item1.type == HFX_ITEM_PREFILL;
+  auto source = [&](const HfxItem& item) {
+    NextItem4 x;
+    x.left = item_steps(item);
+    x.bt = item.rq.bt_start + (int)((unsigned)item.kb / HFX_PAGE) + wave;
+    x.last = item.rq.bt_start + item.rq.n_pages - 1;
+    x.head = item.h0 / G;
+    return x;
+  };
+  // The stream of page copies: the steps of the current item and then those of the next.  Page ids, one a lane, for up to 64 steps at a time;
+  // the next lot is asked for as soon as one is begun.
+  NextItem4 from = source(it), nx = source(item1);
+  bool in_next = false;
+  int ids = 0, at = 0, have = 0, ids_head = 0;
+  int ids2 = 0, have2 = 0, head2 = 0;
+  int fed = 0, widened = 0;            // steps whose copies have been issued, whose values have been widened, over all items of the run
+  int g_st = 0;                        // step at work, likewise
+  auto ask = [&]() {
+    if (from.left <= 0 && !in_next && next_ok) {
+      in_next = true;
+      from = nx;
+    }
+    if (have2 == 0 && from.left > 0) {
+      ids2 = bt[min(from.bt + 4 * lane, from.last)];
+      have2 = min(from.left, 64);
+      head2 = from.head;
+      from.left -= have2;
+      from.bt += 4 * 64;
+    }
+  };
+  // copies steps up to `limit` as far as they are known
+  auto feed = [&](int limit) {
+    while (fed < limit) {
+      if (at == have) {
+        if (have2 == 0) break;
+        ids = ids2;
+        have = have2;
+        ids_head = head2;
+        at = have2 = 0;
+        ask();
+      }
+      const int page = __builtin_amdgcn_readlane(ids, at);
+      ++at;
+      raw_copy<D>(pool + ((long)page * Hkv + ids_head) * Mx<D>::kBlock, c_keys, c_values, c_scales, (unsigned)uniform((int)(lds_raw + (unsigned)(fed % L::kRawSteps) * L::kRawStep)));
+      ++fed;
+    }
+  };
+  auto raw_slot = [&](int step) { return smem + (unsigned)(step % L::kRawSteps) * L::kRawStep; };
+  auto value_slot = [&](int step) { return values + (step & 1) * L::kValueStep; };
+  // this wavefront's page of a step's values goes to its slot in bf16
+  auto widen = [&](int step) {
+    const char* raw = raw_slot(step) + wave * L::kRawPage;
+    char* to = value_slot(step) + wave * L::kValuePage + w_to;
+    u32x4 scales = *reinterpret_cast<const u32x4*>(raw + w_scales);
+    u32x4 lo, hi;
+    if constexpr (D == 128) {
+      const u32x4 codes = *reinterpret_cast<const u32x4*>(raw + w_codes);
+      widen_values<0>(codes[0], codes[1], scales, lo, hi);
+      *reinterpret_cast<u32x4*>(to) = lo;
+      *reinterpret_cast<u32x4*>(to + 512) = hi;
+      widen_values<1>(codes[2], codes[3], scales, lo, hi);
+      *reinterpret_cast<u32x4*>(to + 1024) = lo;
+      *reinterpret_cast<u32x4*>(to + 1536) = hi;
+    } else {
+      const uint2 codes = *reinterpret_cast<const uint2*>(raw + w_codes);
+      const int w = lane & 1;          // which 32 dimensions
+#pragma unroll
+      for (int k = 0; k < 4; ++k) scales[k] >>= 8 * w;
+      widen_values<0>(codes.x, codes.y, scales, lo, hi);
+      *reinterpret_cast<u32x4*>(to) = lo;
+      *reinterpret_cast<u32x4*>(to + 512) = hi;
+    }
+    widened = step + 1;
+  };
+  ask();
+
+  PrefillWave4<D> w;
+  WaveRows wr = wave_rows(it, wave);
+  bf16x8 qx[D / 64][4];
+  auto q_rows = [&](const HfxItem& item, const WaveRows& r) { return a.q + ((long)item.rq.q_start * Hq + r.head) * D; };
+  query_load4<D>(qx, q_rows(it, wr), wr.row0, it.rq.q_len - 1, Hq, n, j);
+
+  for (;;) {
+    // Start of an item: its first step's keys have landed for everybody and its values are widened, or that is done now.
+    ask();
+    if (widened <= g_st) {
+      feed(g_st + L::kRawSteps);
+      HFX_WAIT_VMCNT(0);
+      ring_barrier();
+      widen(g_st);
+    }
+    query_rows4<D>(w, qx);
+    w.l = 0.f;
+    const int wave_end = wr.wave_kend, unmasked_upto = wr.wave_pmin, ctx_len = it.rq.ctx_len;
+    const int steps = item_steps(it);
+    int kt = it.kb;
+    auto mask_stage = [&](f32x16& s, int key0) {     // keys past this lane's row's horizon (rows past the chunk: its last row's)
+      if (key0 + SK - 1 > unmasked_upto) mask_scores(s, min(wr.wave_pmin + n, ctx_len - 1), key0 + j * 8);
+    };
+    bf16x8 frag[S];
+    f32x16 s0, s1;
+    Weighing wt;
+    Keys4<D> keys = read_keys4<D>(raw_slot(g_st), k_lane, s_lane, j);
+    s0 = first_scores4<D>(w, keys);
+    keys = read_keys4<D>(raw_slot(g_st) + 2 * L::kRawPage, k_lane, s_lane, j);
+    mask_stage(s0, kt);
+    w.m = fmaxf(HFX_M_NONE, row_max(s0, sl2));
+    wt.portion(0, 0, 4, s0, sl2, w.m);
+    wt.portion(0, 4, 8, s0, sl2, w.m);
+    wt.portion(4, Share<D>::values[S - 1], Share<D>::values[S - 1], s0, sl2, w.m);
+    auto mask_values = [&](int key0) {               // unused slots may hold anything
+      if (key0 + SK > ctx_len) {
+#pragma unroll
+        for (int i = 0; i < S; ++i) frag[i] = keep_first(frag[i], ctx_len - (key0 + i / (D / 32) * 16 + j * 8));
+      }
+    };
+    for (int left = steps; left > 0; --left) {
+      // Synchronisation point: the values of this step are widened, the next one's raw pages have landed, and nobody reads the slots any more that are
+      // filled next.  In the item's last step the next ticket is asked for and published.
+      if (left == 1) {
+        int reply = 0;
+        tickets_reserve(t, reply, ctrl);
+        HFX_WAIT_VMCNT(0);
+        tickets_publish(t, reply, s_tk, ctrl, H);
+      } else if (fed == g_st + L::kRawSteps) {
+        HFX_WAIT_VMCNT(L::kCopies);
+      } else {
+        HFX_WAIT_VMCNT(0);
+      }
+      ring_barrier();
+      const bool landed = fed > g_st + 1;       // the next step's pages; copies issued now have not
+      feed(g_st + 1 + L::kRawSteps);
+      ask();
+      if (landed) widen(g_st + 1);
+      bf16x8 pb[2];
+      if (kt < wave_end) {
+        s1 = scores_phase4<D>(w, keys, frag, s0, wt, sl2, value_slot(g_st), v_lane);
+        pb[0] = wt.fragment(0);
+        pb[1] = wt.fragment(1);
+        settle_weights<D>(w, s0, pb, wt.sum(), sl2);
+        mask_stage(s1, kt + SK);
+        mask_values(kt);
+        if (left > 1) keys = read_keys4<D>(raw_slot(g_st + 1), k_lane, s_lane, j);
+        __builtin_amdgcn_sched_barrier(0);
+        values_phase4<D>(w, frag, pb, s1, wt, sl2);
+      }
+      if (kt + SK < wave_end) {
+        if (left > 1) {
+          s0 = scores_phase4<D>(w, keys, frag, s1, wt, sl2, value_slot(g_st) + 2 * L::kValuePage, v_lane);
+        } else {
+#pragma unroll
+          for (int i = 0; i < S; ++i) frag[i] = value_fragment4<D>(value_slot(g_st) + 2 * L::kValuePage, i, v_lane);
+          wt.portion(Share<D>::values[S - 1], 8, 12, s1, sl2, w.m);
+          wt.portion(8, 12, 16, s1, sl2, w.m);
+          wt.portion(12, 16, 16, s1, sl2, w.m);
+        }
+        pb[0] = wt.fragment(0);
+        pb[1] = wt.fragment(1);
+        settle_weights<D>(w, s1, pb, wt.sum(), sl2);
+        if (left > 1) mask_stage(s0, kt + 2 * SK);
+        mask_values(kt + SK);
+        if (left > 1) keys = read_keys4<D>(raw_slot(g_st + 1) + 2 * L::kRawPage, k_lane, s_lane, j);
+        __builtin_amdgcn_sched_barrier(0);
+        values_phase4<D>(w, frag, pb, s0, wt, sl2);
+      }
+      kt += kStepKeys;
+      ++g_st;
+    }
+    // hand-over
+    tickets_take(t, s_tk, n_items);
+    if (!next_ok) {
+      prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
+      break;
+    }
+    const HfxItem item_c = items[t.cur];
+    const HfxItem item_n = items[t.nxt < n_items ? t.nxt : t.cur];
+    const WaveRows wr_c = wave_rows(item_c, wave);
+    query_load4<D>(qx, q_rows(item_c, wr_c), wr_c.row0, item_c.rq.q_len - 1, Hq, n, j);
+    if (!in_next) from = nx;
+    in_next = false;
+    nx = source(item_n);
+    next_ok = t.nxt < n_items && item_n.type == HFX_ITEM_PREFILL;
+    prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
+    it = item_c;
+    wr = wr_c;
+  }
+  __syncthreads();     // every wavefront is done with the ring before the LDS is used for anything else
+}
+
+template <int D>
+__global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(const HfxHeader hdr, const char* __restrict__ desc, int* __restrict__ ctrl,
+                                                                                const __bf16* __restrict__ q, const __bf16* __restrict__ pool,
+                                                                                float* __restrict__ ws, __bf16* __restrict__ out) {
+  KArgs a;
+  a.desc = desc;
+  a.q = q;
+  a.pool = pool;
+  a.ws = ws;
+  a.out = out;
+  __shared__ __attribute__((aligned(1024))) char smem[Smem4<D>::kBytes];
+  __shared__ int s_tk[2];
+  __shared__ __attribute__((aligned(128))) char s_ostage[4 * 2048];      // result rows on their way out (prefill_store)
+  const HfxHeader* H = &hdr;
+  const HfxItem* items = reinterpret_cast<const HfxItem*>(a.desc + H->off_items);
+  const int n_items = H->n_items;
+  Tickets t = tickets_start(H, a.desc);
+  while (t.cur < n_items) {
+    if (items[t.cur].type == HFX_ITEM_DECODE) decode_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem);
+    else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ostage);
+  }
+  queue_done(H, ctrl);
+}
+
+hipError_t max_resident_workgroups_mx(int head_dim, int* per_cu) {
+  if (head_dim == 128) return hipOccupancyMaxActiveBlocksPerMultiprocessor(per_cu, mixed_attention_mx_kernel<128>, HFX_WG_THREADS, 0);
+  return hipOccupancyMaxActiveBlocksPerMultiprocessor(per_cu, mixed_attention_mx_kernel<64>, HFX_WG_THREADS, 0);
+}
+
+hipError_t launch_mixed_attention_mx(const HfxHeader& h, int grid, void* desc, const void* q, const void* pool, void* ws, void* out, hipStream_t stream) {
+  const HfxHeader hk = launch_header(h, grid);
+  const char* d = static_cast<const char*>(desc);
+  int* ctrl = reinterpret_cast<int*>(static_cast<char*>(desc) + h.off_ctrl);
+  const __bf16* qp = static_cast<const __bf16*>(q);
+  const __bf16* pp = static_cast<const __bf16*>(pool);
+  float* wp = static_cast<float*>(ws);
+  __bf16* op = static_cast<__bf16*>(out);
+  const hipError_t e = launch(h.head_dim == 128 ? mixed_attention_mx_kernel<128> : mixed_attention_mx_kernel<64>, dim3(grid), HFX_WG_THREADS, stream, hk, d,
+                              ctrl, qp, pp, wp, op);
+  return e != hipSuccess ? e : launch_merge(h, desc, ws, out, stream);
+}
+
+}  // namespace hfx

@@ -1060,7 +1060,9 @@ void layout_blob(const hfx_shape* shape, const Plan& P, HfxHeader* h) {
   off = align_up(off + sizeof(HfxUnit) * P.units.size(), 64);
   h->off_runs = (uint32_t)off;
   h->n_runs = P.n_runs;
-  off = align_up(off + sizeof(HfxRun) * (uint64_t)P.n_runs, 256);
+  off = align_up(off + sizeof(HfxRun) * (uint64_t)P.n_runs, 64);
+  h->off_run_pos = (uint32_t)off;
+  off = align_up(off + 4ull * (uint64_t)P.n_runs, 256);
   h->total_bytes = off;
   uint64_t acc_bytes = align_up((uint64_t)P.n_partial_rows * shape->head_dim * 4ull, 256);
   h->ws_off_ml = acc_bytes;
@@ -1126,6 +1128,7 @@ hfx_status fill_blob(const hfx_shape* shape, Plan& P, const int32_t* bt_indptr, 
   put(h.off_units, P.units.data(), sizeof(HfxUnit) * P.units.size(), h.off_runs);
   // append runs: each request's new tokens, cut at page boundaries
   HfxRun* run = (HfxRun*)(base + h.off_runs);
+  int32_t* run_pos = (int32_t*)(base + h.off_run_pos);
   for (int r = 0; r < R; ++r) {
     const HfxReq& q = P.reqs[(size_t)r];
     const int32_t* pages = bt + q.bt_start;
@@ -1134,10 +1137,12 @@ hfx_status fill_blob(const hfx_shape* shape, Plan& P, const int32_t* bt_indptr, 
       const int32_t slot0 = t % HFX_PAGE;
       const int32_t n = std::min<int32_t>(HFX_PAGE - slot0, q.ctx_len - t);
       *run++ = HfxRun{q.q_start + (t - (q.ctx_len - q.q_len)), n, pages[t / HFX_PAGE], slot0};
+      *run_pos++ = t;
       t += n;
     }
   }
-  put(h.off_runs + sizeof(HfxRun) * (uint64_t)P.n_runs, nullptr, 0, h.total_bytes);
+  put(h.off_runs + sizeof(HfxRun) * (uint64_t)P.n_runs, nullptr, 0, h.off_run_pos);
+  put(h.off_run_pos + 4ull * (uint64_t)P.n_runs, nullptr, 0, h.total_bytes);
   return HFX_OK;
 }
 

@@ -1,0 +1,476 @@
+"""Position rotation on the way into the cache, and the cache held in 4 bits, on the GPU against plain forms in 64 bits.
+
+Oracles (numpy, 64 bits, written from the definitions): the rotation; the 4-bit format, quantised to and read from token by token in the page layout of the
+header; dense attention over the values that a page stands for.
+
+Tolerances, from the arithmetic:
+ * rotation, 4-bit codes and scales: the operator fixes every rounding (products and sums to fp32, then bf16 or the 4-bit format), so bits are equal
+   to those of the oracle with the same roundings; its distance from 64 bits without them is bounded in a test of its own.
+ * attention: the project's own for bf16 outputs, max-abs <= 2e-2 and mean-abs <= 2e-3 (weights rounded to bf16, 2^-9 each, output rounded to bf16; values of
+   order 1).
+"""
+import numpy as np
+import pytest
+
+from paper_2508_15919_amd import synth
+from paper_2508_15919_amd.synth import DECODE, PREFILL, bf16_bits_to_f32, bf16_bits_to_f64, f32_to_bf16_bits
+
+MAGNITUDES = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6], np.float64)
+MAX_ABS, MEAN_ABS = 2e-2, 2e-3
+
+
+# ------------------------------------------------------------------ oracles
+def quantise(x):
+    """fp64 values [..., D] -> codes and scale bytes [..., D / 32], by the definition."""
+    x = np.asarray(x, np.float64)
+    b = x.reshape(*x.shape[:-1], -1, 32)
+    top = np.abs(b).max(-1)
+    finite = np.isfinite(top)
+    safe = np.where(finite & (top > 0), top, 1.0)
+    e = np.floor(np.log2(safe)).astype(np.int64)
+    e = np.where(2.0 ** e > safe, e - 1, e)                   # log2 may round up to the next power
+    e = e - 2 + (safe >= 1.75 * 2.0 ** e)                     # nearest to 6 at most: less than 7 = 1.75 * 4
+    e = np.where(top > 0, e, -1000)
+    byte = np.clip(e + 127, 2, 252)
+    y = np.abs(np.where(finite[..., None], b, 0.0)) / 2.0 ** (byte - 127.0)[..., None]
+    code = np.zeros(y.shape, np.int64)
+    for i in range(1, 8):                                     # above the middle, or on it if the upper code is even
+        middle = (MAGNITUDES[i - 1] + MAGNITUDES[i]) / 2
+        code[(y > middle) | ((y == middle) & (i % 2 == 0))] = i
+    code += 8 * np.signbit(b)
+    return code.reshape(x.shape).astype(np.uint8), np.where(finite, byte, 255).astype(np.uint8)
+
+
+def value(code, e):
+    with np.errstate(invalid="ignore"):
+        size = np.where(e == 255, np.nan, 2.0 ** (e.astype(np.float64) - 127))
+    v = MAGNITUDES[code & 7] * np.where(code & 8, -1.0, 1.0)
+    return (v.reshape(*code.shape[:-1], -1, 32) * size[..., None]).reshape(code.shape)
+
+
+def places(slot, dim, D):
+    """Byte and shift of a key's code, of a value's code, and the bytes of their scales, inside a block of 17 D bytes."""
+    w, i = divmod(dim, 32)
+    key = (slot * (D // 32) + w) * 16 + i // 2, 4 * (i % 2)
+    tp, t = divmod(w, 2)
+    val = 8 * D + (((slot // 8 * (D // 64) + tp) * 16 + i % 16) * 2 + t) * 8 + slot % 8, 4 * (i // 16)
+    return key, val, 16 * D + slot * (D // 32) + w, 16 * D + D // 2 + ((slot // 8 * (D // 64) + tp) * 8 + slot % 8) * 2 + t
+
+
+def place_tables(D):
+    t = [[places(s, d, D) for d in range(D)] for s in range(16)]
+    pick = lambda f: np.array([[f(c) for c in row] for row in t])       # noqa: E731
+    return (pick(lambda c: c[0][0]), pick(lambda c: c[0][1]), pick(lambda c: c[1][0]), pick(lambda c: c[1][1]),
+            pick(lambda c: c[2])[:, ::32], pick(lambda c: c[3])[:, ::32])
+
+
+def put_token(block, slot, k, v, D, tables):
+    """Keys and values [heads, D] in fp64 go to a slot of a page's blocks [heads, 17 D], byte by byte."""
+    kb, ks, vb, vs, ke, ve = tables
+    for x, byte, shift, scale in ((k, kb, ks, ke), (v, vb, vs, ve)):
+        code, e = quantise(x)
+        for d in range(D):
+            at, sh = byte[slot, d], shift[slot, d]
+            block[:, at] = (block[:, at] & (0xF0 if sh == 0 else 0x0F)) | (code[:, d] << sh)
+        block[:, scale[slot]] = e
+
+
+def get_page(block, D, tables):
+    """Values of a page: [heads, 16, D] of keys and of values."""
+    kb, ks, vb, vs, ke, ve = tables
+    k = value((block[:, kb] >> ks) & 15, block[:, ke])
+    v = value((block[:, vb] >> vs) & 15, block[:, ve])
+    return k, v
+
+
+def rotate(x, position, table, rot, interleaved, steps):
+    """x [T, H, D] in fp64.  steps: the roundings to fp32 of the operator."""
+    y = np.array(x, np.float64)
+    r = (lambda z: z.astype(np.float32).astype(np.float64)) if steps else (lambda z: z)
+    m = rot // 2
+    for i in range(m):
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + m)
+        c, s = table[position, i][:, None].astype(np.float64), table[position, m + i][:, None].astype(np.float64)
+        y[:, :, a] = r(r(x[:, :, a] * c) - r(x[:, :, b] * s))
+        y[:, :, b] = r(r(x[:, :, b] * c) + r(x[:, :, a] * s))
+    return y
+
+
+def angles(positions, rot):
+    t = np.arange(positions)[:, None] * 10000.0 ** (-np.arange(rot // 2) / (rot // 2))
+    return np.concatenate((np.cos(t), np.sin(t)), 1).astype(np.float32)
+
+
+def test_rotation_oracle_against_64_bits():
+    """Three roundings of at most 2^-24 of what they round, which is at most |a| + |b|."""
+    g = np.random.default_rng(1)
+    x = bf16_bits_to_f64(f32_to_bf16_bits(g.standard_normal((500, 2, 64)).astype(np.float32)))
+    position, table = g.integers(0, 4000, 500), angles(4000, 48)
+    for interleaved in (False, True):
+        a, b = (rotate(x, position, table, 48, interleaved, steps) for steps in (True, False))
+        assert (np.abs(a - b) <= 3 * 2.0 ** -24 * 2 * np.abs(x).max(-1, keepdims=True)).all() and not np.array_equal(a, b)
+        assert np.array_equal(a[..., 48:], x[..., 48:])
+        y = np.linalg.norm(b, axis=-1) / np.linalg.norm(x, axis=-1)             # a rotation
+        assert np.abs(y - 1).max() < 1e-6
+
+
+def test_quantiser_oracle_on_values_that_can_be_said():
+    x = np.zeros((4, 32))
+    x[0, :16] = [7.0, .25, .75, 1.25, 1.75, 2.5, 3.5, 5, -.25, -.75, -1.25, -1.75, -2.5, -3.5, -5, -6]     # 7 takes the next scale, 2: half of each
+    x[1, :8] = [6.99, .25, .75, 1.25, 1.75, 2.5, 3.5, 5]
+    x[2, 0] = np.inf
+    code, e = quantise(x)
+    assert e[:, 0].tolist() == [128, 127, 255, 2]
+    assert code[0, :8].tolist() == [6, 0, 1, 1, 2, 2, 4, 4] and code[1, :8].tolist() == [7, 0, 2, 2, 4, 4, 6, 6]
+    assert not value(code, e)[3].any() and np.isnan(value(code, e)[2]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_bit_of_a_block_has_one_place(D):
+    seen = set()
+    for slot in range(16):
+        for d in range(D):
+            (kb, ks), (vb, vs), ke, ve = places(slot, d, D)
+            for bit in range(4):
+                seen |= {8 * kb + ks + bit, 8 * vb + vs + bit}
+            seen |= {8 * b + bit for b in (ke, ve) for bit in range(8)}
+    assert seen == set(range(8 * 17 * D))
+    assert len(seen) == 16 * D * 4 * 2 + 16 * (D // 32) * 8 * 2
+
+
+# ------------------------------------------------------------------ on the GPU
+@pytest.fixture(scope="module")
+def hb():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2508_15919_amd import binding
+    binding.load()
+    return binding
+
+
+class Step:
+    """A step's descriptor and block table; contexts of the given lengths, chunks of the given lengths at their ends."""
+
+    def __init__(self, hb, hq, hkv, d, q_len, ctx_len, seed, extra=3, scale=0.0):
+        import torch
+        g = np.random.default_rng(seed)
+        self.g, self.torch, self.hb, self.hq, self.hkv, self.d = g, torch, hb, hq, hkv, d
+        self.q_len, self.ctx_len = np.array(q_len, np.int32), np.array(ctx_len, np.int32)
+        self.kind = np.where((self.q_len == 1) & (g.random(len(q_len)) < 0.7), DECODE, PREFILL).astype(np.int32)
+        n = (self.ctx_len + 15) // 16
+        self.indptr = np.concatenate(([0], np.cumsum(n))).astype(np.int32)
+        self.num_pages = int(n.sum()) + extra
+        self.pages = g.permutation(self.num_pages)[:int(n.sum())].astype(np.int32)
+        self.tokens = int(self.q_len.sum())
+        self.shape = hb.make_shape(hq, hkv, d, self.num_pages, scale)
+        nb, _, ws = hb.hfx_batch_desc_sizes(self.shape, self.kind, self.q_len, self.ctx_len)
+        self.host = torch.empty(nb, dtype=torch.uint8, pin_memory=True)
+        self.dev = torch.empty(nb, dtype=torch.uint8, device="cuda")
+        self.ws = torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None
+        hb.hfx_build_batch_desc(self.shape, self.kind, self.q_len, self.ctx_len, self.indptr, self.pages, self.host, self.dev, torch.cuda.current_stream())
+        self.position = np.concatenate([np.arange(c - q, c) for q, c in zip(self.q_len.tolist(), self.ctx_len.tolist())])
+        self.request = np.repeat(np.arange(len(q_len)), self.q_len)
+        self.page = self.pages[self.indptr[self.request] + self.position // 16]
+        self.slot = self.position % 16
+
+    def bits(self, *shape, scale=1.0):
+        return f32_to_bf16_bits((self.g.standard_normal(shape) * scale).astype(np.float32))
+
+    def up(self, bits):
+        return self.torch.from_numpy(bits.view(np.int16)).cuda()
+
+
+def down(t):
+    return t.cpu().numpy().view(np.uint16)
+
+
+def random_pool(step):
+    """Quantised keys and values of order one in every slot that a context has; every other slot of the pool any bytes, NaN scales among them."""
+    D = step.d
+    tables = place_tables(D)
+    pool = step.g.integers(0, 256, (step.num_pages, step.hkv, 17 * D), dtype=np.uint8)
+    pool[:, :, 16 * D:][step.g.random((step.num_pages, step.hkv, D)) < 0.3] = 255
+    kb, ks, vb, vs, ke, ve = tables
+    for r, c in enumerate(step.ctx_len.tolist()):
+        for i in range(-(-c // 16)):
+            used = min(16, c - 16 * i)
+            block = pool[step.pages[step.indptr[r] + i]]
+            for byte, shift, scale in ((kb, ks, ke), (vb, vs, ve)):
+                code, e = quantise(step.g.standard_normal((step.hkv, used, D)))
+                for sh in (0, 4):
+                    at = shift[:used] == sh
+                    block[:, byte[:used][at]] = (block[:, byte[:used][at]] & (0xF0 if sh == 0 else 0x0F)) | (code[:, at] << sh)
+                block[:, scale[:used]] = e
+    return pool
+
+
+def dense(step, q, pool):
+    """softmax(Q K^T * scale + causal mask) V in fp64 over the values of the pool."""
+    D, G = step.d, step.hq // step.hkv
+    tables = place_tables(D)
+    scale = step.shape.softmax_scale if step.shape.softmax_scale > 0 else 1 / np.sqrt(D)
+    out = np.zeros((step.tokens, step.hq, D))
+    t0 = 0
+    for r, (n, c) in enumerate(zip(step.q_len.tolist(), step.ctx_len.tolist())):
+        kv = [get_page(pool[p], D, tables) for p in step.pages[step.indptr[r]:step.indptr[r] + -(-c // 16)]]
+        k, v = (np.concatenate([x[i] for x in kv], 1)[:, :c] for i in (0, 1))
+        hidden = np.arange(c)[None, :] > np.arange(c - n, c)[:, None]
+        for h in range(step.hq):
+            s = q[t0:t0 + n, h] @ k[h // G].T * scale
+            s[hidden] = -np.inf
+            s = np.exp(s - s.max(1, keepdims=True))
+            out[t0:t0 + n, h] = s / s.sum(1, keepdims=True) @ v[h // G]
+        t0 += n
+    return out
+
+
+def attend(step, q_bits, pool):
+    torch, hb = step.torch, step.hb
+    out = torch.full((step.tokens, step.hq, step.d), 0x7FC0, dtype=torch.int16, device="cuda")
+    hb.hfx_mixed_paged_attention_mx(step.shape, step.up(q_bits), pool, step.host, step.dev, step.ws, out, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    return down(out)
+
+
+ATTENTION = [
+    # hq, hkv, d, q_len, ctx_len
+    (4, 2, 64, [1, 1, 1, 32], [37, 64, 129, 32]),
+    (32, 8, 128, [1] * 9, [1, 2, 15, 16, 17, 31, 33, 500, 2100]),
+    (8, 1, 128, [1, 1, 5, 1], [4097, 1, 777, 63]),
+    (8, 2, 128, [65, 1, 130], [65, 40, 700]),
+    (8, 8, 64, [1, 33, 2, 1], [700, 33, 1, 16][:2] + [64, 16]),
+    (16, 1, 64, [1, 97], [333, 97]),
+    (24, 8, 128, [1, 31, 64, 63, 1], [16, 31, 64, 128, 95]),
+    (32, 4, 64, [300, 1, 129], [301, 1025, 640]),
+    (4, 4, 128, [1] * 40 + [3] * 5, list(range(1, 41)) + [3, 16, 17, 48, 66]),
+    (8, 1, 128, [200, 17], [3000, 1500]),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(ATTENTION)))
+def test_attention_over_the_4_bit_cache(hb, case):
+    hq, hkv, d, q_len, ctx = ATTENTION[case]
+    step = Step(hb, hq, hkv, d, q_len, ctx, 100 + case, scale=0.2 if case == 3 else 0.0)
+    pool = random_pool(step)
+    q = step.bits(step.tokens, hq, d)
+    got = bf16_bits_to_f64(attend(step, q, step.torch.from_numpy(pool).cuda()))
+    err = np.abs(got - dense(step, bf16_bits_to_f64(q), pool))
+    print(f"max-abs {np.nanmax(err):.3e} mean-abs {np.nanmean(err):.3e}")
+    assert np.isfinite(got).all()
+    assert err.max() <= MAX_ABS and err.mean() <= MEAN_ABS
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (8, 8, 64)])
+def test_attention_with_queries_of_many_sizes(hb, hq, hkv, d):
+    """Queries whose dimensions differ by many powers of two, whole heads that are tiny or zero: they are taken as sums of two 8-bit numbers with a scale
+    for 32 dimensions.  Scores stay of order one by the softmax scale, so the bound is the usual one."""
+    step = Step(hb, hq, hkv, d, [1, 40, 1], [333, 200, 90], 7)
+    pool = random_pool(step)
+    sizes = 2.0 ** step.g.integers(-30, 1, (step.tokens, hq, d))
+    sizes[:, 1] = 2.0 ** -60
+    sizes[0, 0] = 0.0
+    q = f32_to_bf16_bits((step.g.standard_normal(sizes.shape) * sizes * 3).astype(np.float32))
+    got = bf16_bits_to_f64(attend(step, q, step.torch.from_numpy(pool).cuda()))
+    err = np.abs(got - dense(step, bf16_bits_to_f64(q), pool))
+    assert np.isfinite(got).all() and err.max() <= MAX_ABS and err.mean() <= MEAN_ABS
+
+
+@pytest.mark.gpu
+def test_a_context_of_one_token_returns_its_values(hb):
+    step = Step(hb, 8, 2, 128, [1, 1, 1], [1, 1, 1], 11)
+    pool = random_pool(step)
+    got = bf16_bits_to_f64(attend(step, step.bits(3, 8, 128), step.torch.from_numpy(pool).cuda()))
+    for r in range(3):
+        _, v = get_page(pool[step.pages[step.indptr[r]]], 128, place_tables(128))
+        assert np.array_equal(got[r], np.repeat(v[:, 0], 4, axis=0))
+
+
+APPEND = [
+    # hq, hkv, d, rot, interleaved, packed, q_len, ctx_len
+    (32, 8, 128, 128, False, True, [1] * 16 + [5, 40, 64, 17], [40 + i for i in range(16)] + [5, 90, 64, 33]),
+    (8, 1, 64, 64, True, True, [1, 1, 70, 16], [1, 17, 333, 16]),
+    (8, 2, 128, 32, False, False, [3, 1, 129], [3, 16, 140]),
+    (8, 8, 64, 48, False, False, [15, 1, 2], [47, 31, 2]),
+    (4, 4, 128, 96, True, False, [33, 1], [1000, 8]),
+    (12, 12, 128, 0, False, True, [9, 1], [70, 5]),
+    (32, 4, 64, 16, True, False, [1, 18], [15, 40]),
+]
+
+
+def projected(step, packed):
+    """Queries, keys and values: rows of one buffer or apart, the latter with rows further apart than they are long."""
+    hq, hkv, d, n = step.hq, step.hkv, step.d, step.tokens
+    q, k, v = step.bits(n, hq, d), step.bits(n, hkv, d, scale=2.0), step.bits(n, hkv, d)
+    q[0, 0] = 0
+    if packed:
+        rows = step.up(np.concatenate([x.reshape(n, -1) for x in (q, k, v)], 1))
+        return (q, k, v), rows.split((hq * d, hkv * d, hkv * d), 1)
+    wide = [step.torch.zeros((n, x.shape[1] * d + 8 * (i + 1)), dtype=step.torch.int16, device="cuda") for i, x in enumerate((q, k, v))]
+    for w, x in zip(wide, (q, k, v)):
+        w[:, :x.shape[1] * d] = step.up(x.reshape(n, -1))
+    return (q, k, v), wide
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("case", range(len(APPEND)))
+def test_rotating_append(hb, case, four):
+    hq, hkv, d, rot, interleaved, packed, q_len, ctx = APPEND[case]
+    step = Step(hb, hq, hkv, d, q_len, ctx, 200 + case)
+    torch, stream = step.torch, step.torch.cuda.current_stream()
+    (q, k, v), (qd, kd, vd) = projected(step, packed)
+    table = angles(int(max(ctx)), max(rot, 16))
+    rope = hb.make_rope(torch.from_numpy(table).cuda(), rot, interleaved) if rot else None
+    out = torch.full((step.tokens, hq, d), 0x7FC0, dtype=torch.int16, device="cuda")
+    if four:
+        pool = step.g.integers(0, 256, (step.num_pages, hkv, 17 * d), dtype=np.uint8)
+        dev = torch.from_numpy(pool).cuda()
+        assert dev.nbytes == hb.hfx_mx_pool_bytes(step.shape)
+        append = hb.hfx_rope_append_kv_mx
+    else:
+        pool = step.bits(step.num_pages, hkv, 2, 16 * d)
+        dev = step.up(pool)
+        append = hb.hfx_rope_append_kv
+    append(step.shape, rope, qd, qd.stride(0), kd, kd.stride(0), vd, vd.stride(0), out, dev, step.host, step.dev, stream)
+    torch.cuda.synchronize()
+
+    def turned(x):
+        return rotate(bf16_bits_to_f64(x), step.position, table, rot, interleaved, True)
+
+    def same(got, want):
+        assert np.array_equal(got, want), f"{np.count_nonzero(got != want)} of {got.size} differ"
+    same(down(out), f32_to_bf16_bits(turned(q).astype(np.float32)))
+    kr = turned(k)
+    if four:
+        tables = place_tables(d)
+        for t in range(step.tokens):
+            put_token(pool[step.page[t]], step.slot[t], kr[t], bf16_bits_to_f64(v[t]), d, tables)
+        same(dev.cpu().numpy(), pool)
+        k_out, v_out = (torch.full((step.tokens, hkv, d), 0x7FC0, dtype=torch.int16, device="cuda") for _ in range(2))
+        hb.hfx_read_new_kv_mx(step.shape, dev, step.host, step.dev, k_out, v_out, stream)
+        torch.cuda.synchronize()
+        code, e = quantise(kr)
+        assert np.array_equal(bf16_bits_to_f64(down(k_out)), value(code, e))
+        code, e = quantise(bf16_bits_to_f64(v))
+        assert np.array_equal(bf16_bits_to_f64(down(v_out)), value(code, e))
+    else:
+        keys = f32_to_bf16_bits(kr.astype(np.float32))
+        wk = pool.reshape(step.num_pages, hkv, 2, d // 16, 16, 16)
+        wv = pool.reshape(step.num_pages, hkv, 2, d, 16)
+        for t in range(step.tokens):
+            wk[step.page[t], :, 0, :, step.slot[t]] = keys[t].reshape(hkv, d // 16, 16)
+            wv[step.page[t], :, 1, :, step.slot[t]] = v[t]
+        same(down(dev), pool)
+
+
+@pytest.mark.gpu
+def test_rotation_in_place_and_without_queries(hb):
+    step = Step(hb, 8, 2, 128, [1, 20], [7, 50], 31)
+    torch, stream = step.torch, step.torch.cuda.current_stream()
+    (q, k, v), _ = projected(step, False)
+    rope = hb.make_rope(torch.from_numpy(angles(64, 128)).cuda(), 128)
+    qd, kd, vd = step.up(q), step.up(k), step.up(v)
+    pools = [torch.zeros((step.num_pages, 2, 17 * 128), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    out = torch.empty_like(qd)
+    hb.hfx_rope_append_kv_mx(step.shape, rope, qd, 8 * 128, kd, 256, vd, 256, out, pools[0], step.host, step.dev, stream)
+    hb.hfx_rope_append_kv_mx(step.shape, rope, qd, 8 * 128, kd, 256, vd, 256, qd, pools[1], step.host, step.dev, stream)
+    torch.cuda.synchronize()
+    assert torch.equal(out, qd) and torch.equal(pools[0], pools[1])
+    pools[1].zero_()
+    hb.hfx_rope_append_kv_mx(step.shape, rope, None, 0, kd, 256, vd, 256, None, pools[1], step.host, step.dev, stream)
+    torch.cuda.synchronize()
+    assert torch.equal(pools[0], pools[1])
+
+
+@pytest.mark.gpu
+def test_numbers_at_the_ends_of_the_range_and_not_finite_ones(hb):
+    """Blocks of zeros, of the smallest and the largest bf16 numbers, with an infinity, with a NaN; without rotation, so that they arrive as they are."""
+    D, hkv = 128, 4
+    step = Step(hb, 4, hkv, D, [18], [21], 5)
+    torch, stream = step.torch, step.torch.cuda.current_stream()
+    bits = step.bits(18, hkv, D)
+    x = bits.reshape(-1, 32)
+    x[0] = 0
+    x[1] = 0x8000
+    x[2] = 0x0001
+    x[3, 3] = 0x7F7F
+    x[4] = 0x7F7F
+    x[5, 31] = 0x7F80
+    x[6, 0] = 0xFF80
+    x[7, 9] = 0x7FC0
+    x[8] = f32_to_bf16_bits(np.full(32, 7 * 2.0 ** -40, np.float32))
+    x[9] = 0x0080
+    k = bits
+    v = np.ascontiguousarray(bits[::-1])
+    pool = np.zeros((step.num_pages, hkv, 17 * D), np.uint8)
+    dev = torch.from_numpy(pool).cuda()
+    hb.hfx_rope_append_kv_mx(step.shape, None, None, 0, step.up(k), hkv * D, step.up(v), hkv * D, None, dev, step.host, step.dev, stream)
+    k_out, v_out = (torch.zeros((18, hkv, D), dtype=torch.int16, device="cuda") for _ in range(2))
+    hb.hfx_read_new_kv_mx(step.shape, dev, step.host, step.dev, k_out, v_out, stream)
+    torch.cuda.synchronize()
+    for got, was in ((k_out, k), (v_out, v)):
+        code, e = quantise(bf16_bits_to_f64(was))
+        want = value(code, e)
+        got = bf16_bits_to_f64(down(got))
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.nan_to_num(got), np.nan_to_num(want))
+
+
+# ------------------------------------------------------------------ refusals (no GPU needed: nothing is enqueued)
+def test_what_is_refused():
+    import ctypes
+    from paper_2508_15919_amd import binding as hb
+    lib = hb.load()
+    shape = hb.make_shape(8, 2, 128, 16)
+    kind, q, c, indptr, pages = [PREFILL], [20], [50], [0, 4], [3, 1, 0, 7]
+    host = np.zeros(hb.hfx_batch_desc_sizes(shape, kind, q, c)[0], np.uint8)
+    hb.hfx_fill_batch_desc(shape, kind, q, c, indptr, pages, host)
+    d = hb.parse_desc(host)
+    assert d["run_pos"].tolist() == [30, 32, 48] and d["runs"][:, 3].tolist() == [14, 0, 0]
+    good = dict(shape=shape, rope=hb.hfx_rope(16, 50, 128, 0), q=16, qs=1024, k=32, ks=256, v=48, vs=256, out=64, pool=16, host=host, dev=16)
+
+    def status(f, **change):
+        a = {**good, **change}
+        return f(ctypes.byref(a["shape"]), ctypes.byref(a["rope"]) if a["rope"] else None, a["q"], a["qs"], a["k"], a["ks"], a["v"], a["vs"], a["out"],
+                 a["pool"], a["host"].ctypes.data if a["host"] is not None else None, a["dev"], None)
+    junk = np.zeros_like(host)
+    for f in (lib.hfx_rope_append_kv, lib.hfx_rope_append_kv_mx):
+        for name in ("k", "v", "pool", "dev", "host"):
+            assert status(f, **{name: None}) == hb.HFX_ERR_NULL, name
+        assert status(f, q=None) == status(f, out=None) == hb.HFX_ERR_NULL
+        assert status(f, rope=hb.hfx_rope(None, 50, 128, 0)) == hb.HFX_ERR_NULL
+        assert status(f, host=junk) == hb.HFX_ERR_DESC
+        assert status(f, shape=hb.make_shape(8, 2, 64, 16)) == status(f, shape=hb.make_shape(8, 3, 128, 16)) == hb.HFX_ERR_SHAPE
+        for rot in (0, 8, 24, 144, -16):
+            assert status(f, rope=hb.hfx_rope(16, 50, rot, 0)) == hb.HFX_ERR_SHAPE, rot
+        assert status(f, rope=hb.hfx_rope(16, 50, 64, 2)) == hb.HFX_ERR_SHAPE
+        assert status(f, qs=1023) == status(f, ks=248) == status(f, vs=0) == status(f, ks=-256) == hb.HFX_ERR_SHAPE
+        assert status(f, rope=hb.hfx_rope(16, 49, 128, 0)) == hb.HFX_ERR_LEN
+        assert status(f, rope=hb.hfx_rope(8, 50, 128, 0)) == hb.HFX_ERR_ALIGN
+        for name in ("q", "k", "v", "out", "pool", "dev"):
+            assert status(f, **{name: 24}) == hb.HFX_ERR_ALIGN, name
+        assert status(f, qs=1028) == status(f, ks=260) == status(f, vs=257) == hb.HFX_ERR_ALIGN
+    sh = ctypes.byref(shape)
+    read, attention = lib.hfx_read_new_kv_mx, lib.hfx_mixed_paged_attention_mx
+    h = host.ctypes.data
+    assert read(sh, None, h, 16, 16, 16, None) == read(sh, 16, None, 16, 16, 16, None) == read(sh, 16, h, 16, None, 16, None) == hb.HFX_ERR_NULL
+    assert read(sh, 16, junk.ctypes.data, 16, 16, 16, None) == hb.HFX_ERR_DESC
+    assert read(sh, 8, h, 16, 16, 16, None) == read(sh, 16, h, 16, 16, 20, None) == hb.HFX_ERR_ALIGN
+    ws = hb.parse_desc(host)["header"].workspace_bytes
+    assert attention(sh, None, 16, h, 16, 16, 1 << 30, 16, None) == attention(sh, 16, 16, None, 16, 16, 1 << 30, 16, None) == hb.HFX_ERR_NULL
+    assert attention(sh, 16, 16, junk.ctypes.data, 16, 16, 1 << 30, 16, None) == hb.HFX_ERR_DESC
+    assert attention(sh, 16, 24, h, 16, 16, 1 << 30, 16, None) == hb.HFX_ERR_ALIGN
+    if ws:
+        assert attention(sh, 16, 16, h, 16, 16, ws - 1, 16, None) == hb.HFX_ERR_BUFSIZE
+    n = ctypes.c_size_t()
+    assert lib.hfx_mx_pool_bytes(sh, None) == hb.HFX_ERR_NULL and lib.hfx_mx_pool_bytes(ctypes.byref(hb.make_shape(8, 3, 128, 4)), ctypes.byref(n)) == hb.HFX_ERR_SHAPE
+    assert hb.hfx_mx_pool_bytes(hb.make_shape(64, 64, 128, 1 << 20)) == (1 << 20) * 64 * 17 * 128
+
+
+def test_tables_that_are_no_tables_are_refused():
+    import torch
+    from paper_2508_15919_amd import binding as hb
+    for t in (torch.zeros(8, 64, dtype=torch.float64), torch.zeros(8, 128), torch.zeros(64), torch.zeros(64, 8).T, torch.zeros(8, 64, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            hb.make_rope(t, 64)
