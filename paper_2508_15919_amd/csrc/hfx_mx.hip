@@ -1,10 +1,9 @@
 // Attention of a scheduled step over a page pool held in 4 bits (see hfx_mx.h for the format): the same work items, queue and split merge as over
 // the bf16 pool, with kernels of their own for both kinds of items.
 //
-//   S^T = K . Q^T   on the scaled 4-bit matrix instructions: the keys' codes and scale bytes go into them as they lie in the cache.  Their other
-//                   operand has 8 bits, so a query is taken as the sum of two 8-bit numbers, each with a scale for 32 dimensions: a bf16 value has 8
-//                   significant bits, the first number (e4m3) has 4 of them and the rest, rounded nowhere, fits the second.  Two products at twice the
-//                   rate of a bf16 one: the same matrix time, and no key is ever converted.
+//   S^T = K . Q^T   on the scaled matrix instructions for 4 to 8 bits: the keys' codes and scale bytes go into them as they lie in the cache.  With their
+//                   other operand in 6 bits they have four times the rate of a bf16 product, and a query is taken as the sum of two 6-bit numbers
+//                   (E2M3, 4 significant bits), each with a scale for 32 dimensions: half the matrix time, and no key is ever converted.
 //   O^T = V^T . P^T on the bf16 matrix instructions: a scale belongs to a token, which is the contracted index here, so the values are widened to bf16
 //                   (every code times every scale is a bf16 number).
 #include <hip/hip_runtime.h>
@@ -19,59 +18,70 @@ namespace hfx {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
+typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
+typedef __bf16 bf16x32 __attribute__((ext_vector_type(32)));
+
 // Operand formats of the scaled matrix instructions.
-constexpr int kFp8 = 0, kFp4 = 4;
+constexpr int kFp6 = 2, kFp4 = 4;
 
-// The 4-bit operand takes four registers of the eight that the builtins ask for.
+// The 4-bit operand takes four registers of the eight that the builtins ask for, the 6-bit one six.
 __device__ __forceinline__ i32x8 fp4_operand(const u32x4& c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
+__device__ __forceinline__ i32x8 fp6_operand(const u32x6& c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], (int)c[4], (int)c[5], 0, 0}; }
 
-// Scale byte for query values whose largest magnitude has the bits `top`: that value comes into [128, 256) of e4m3's 448.  The remainder is
-// at most 8 there and has a scale 2^4 times finer.  Values 2^-13 of the largest and more are taken exactly, smaller ones to 2^-22 of it.
-__device__ __forceinline__ unsigned query_scale(unsigned top) { return (unsigned)max((int)(top >> 23) - 7, 5); }
+// 32 query values as the sum of two sets of 6-bit numbers with scales 2^(e - 127) and 2^(e - 4 - 127).  e brings the largest magnitude into [3.875, 7.75),
+// where the nearest number of E2M3 (4 significant bits, up to 7.5, steps of 1/8 below 2) is at most 1/4 away; a remainder is at most 4 of its own
+// scale's units.  A bf16 value has 8 significant bits: from 1/8 of the largest magnitude's power of two up the two numbers hold all of them; smaller values
+// are off by at most 2^-8 units, 2^-10 of the largest, half of what bf16 itself rounds that one by.
+struct Query6 {
+  u32x6 first, rest;
+  unsigned scale;          // bytes: of first, of rest
+};
 constexpr unsigned kRestScale = 4;
-
-// Eight query values as 8 + 8 numbers of 8 bits under scale byte e: two registers of first numbers, two of remainders.
-__device__ __forceinline__ void split_query(const bf16x8& q, unsigned e, int* first, int* rest) {
-  const float up = __builtin_bit_cast(float, (254 - e) << 23);
-  float x[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)q[i] * up;
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    int f = 0, r = 0;
-    f = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w], x[4 * w + 1], f, false);
-    f = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2], x[4 * w + 3], f, true);
-    const float r0 = (x[4 * w] - __builtin_amdgcn_cvt_f32_fp8(f, 0)) * 16.f, r1 = (x[4 * w + 1] - __builtin_amdgcn_cvt_f32_fp8(f, 1)) * 16.f;
-    const float r2 = (x[4 * w + 2] - __builtin_amdgcn_cvt_f32_fp8(f, 2)) * 16.f, r3 = (x[4 * w + 3] - __builtin_amdgcn_cvt_f32_fp8(f, 3)) * 16.f;
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(r0, r1, r, false);
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(r2, r3, r, true);
-    first[w] = f;
-    rest[w] = r;
-  }
-}
-
-// Bits of the largest magnitude of eight values.
-__device__ __forceinline__ unsigned top_of(const bf16x8& q) {
-  const u32x4 u = __builtin_bit_cast(u32x4, q);
+__device__ __forceinline__ Query6 split_query(const bf16x8* q) {
   unsigned top = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) top = max(top, max(u[w] & 0x7fff0000u, u[w] << 16 & 0x7fff0000u));
-  return top;
+  for (int i = 0; i < 4; ++i) {
+    const u32x4 u = __builtin_bit_cast(u32x4, q[i]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = max(top, max(u[w] & 0x7fff0000u, u[w] << 16 & 0x7fff0000u));
+  }
+  const unsigned e = (unsigned)max((int)((top + 0x80000u) >> 23) - 2, 5);
+  const float scale = __builtin_bit_cast(float, e << 23), rest_scale = __builtin_bit_cast(float, (e - kRestScale) << 23);
+  bf16x32 x, r;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = q[i >> 3][i & 7];
+  Query6 t;
+  t.first = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, scale);
+  const f32x32 f = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(t.first, scale);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) r[i] = (__bf16)((float)x[i] - f[i]);          // (exact)
+  t.rest = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(r, rest_scale);
+  t.scale = e | (e - kRestScale) << 8;
+  return t;
 }
 
-// Values of eight tokens and two dimensions, i and i + 16 of 32, out of eight codes bytes (a, b) and the tokens' scale bytes: token 2k's is byte
-// `At` of scales[k], token 2k + 1's byte At + 2.  lo and hi are the operand registers of the two dimensions: eight tokens in a row each.
+// Values of two tokens in a row and two dimensions, i and i + 16 of 32, out of two bytes of codes (numbers Byte and Byte + 1) and the tokens' scale bytes,
+// numbers At and At + 2 of `scales`: the operand registers of the two dimensions.
+template <int Byte, int At>
+__device__ __forceinline__ void widen_pair(unsigned codes, unsigned scales, unsigned& lo, unsigned& hi) {
+  const unsigned t0 = from_fp4<Byte>(codes, scale_at<At>(scales)), t1 = from_fp4<Byte + 1>(codes, scale_at<At + 2>(scales));
+  lo = __builtin_amdgcn_perm(t1, t0, 0x05040100u);
+  hi = __builtin_amdgcn_perm(t1, t0, 0x07060302u);
+}
+// Number k of the four pairs of eight tokens with codes in a, b.
+template <int At>
+__device__ __forceinline__ void widen_pair(int k, unsigned a, unsigned b, const u32x4& scales, u32x4& lo, u32x4& hi) {
+  unsigned l, h;
+  if (k % 2 == 0) widen_pair<0, At>(k < 2 ? a : b, scales[k], l, h);
+  else widen_pair<2, At>(k < 2 ? a : b, scales[k], l, h);
+  lo[k] = l;
+  hi[k] = h;
+}
 template <int At>
 __device__ __forceinline__ void widen_values(unsigned a, unsigned b, const u32x4& scales, u32x4& lo, u32x4& hi) {
-  const unsigned t0 = from_fp4<0>(a, scale_at<At>(scales[0])), t1 = from_fp4<1>(a, scale_at<At + 2>(scales[0]));
-  const unsigned t2 = from_fp4<2>(a, scale_at<At>(scales[1])), t3 = from_fp4<3>(a, scale_at<At + 2>(scales[1]));
-  const unsigned t4 = from_fp4<0>(b, scale_at<At>(scales[2])), t5 = from_fp4<1>(b, scale_at<At + 2>(scales[2]));
-  const unsigned t6 = from_fp4<2>(b, scale_at<At>(scales[3])), t7 = from_fp4<3>(b, scale_at<At + 2>(scales[3]));
-  constexpr unsigned kLow = 0x05040100u, kHigh = 0x07060302u;
-  lo = u32x4{__builtin_amdgcn_perm(t1, t0, kLow), __builtin_amdgcn_perm(t3, t2, kLow), __builtin_amdgcn_perm(t5, t4, kLow),
-             __builtin_amdgcn_perm(t7, t6, kLow)};
-  hi = u32x4{__builtin_amdgcn_perm(t1, t0, kHigh), __builtin_amdgcn_perm(t3, t2, kHigh), __builtin_amdgcn_perm(t5, t4, kHigh),
-             __builtin_amdgcn_perm(t7, t6, kHigh)};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) widen_pair<At>(k, a, b, scales, lo, hi);
 }
 
 // ----------------------------------------------------------------------------------------------
@@ -111,15 +121,16 @@ __device__ __forceinline__ void decode_load4(PairRegs4<D>& r, const char* pool, 
 
 template <int D>
 struct DecodeQuery4 {
-  i32x8 q[D / 64];        // D = 128: first numbers, remainders; D = 64: both in one
+  u32x6 q[D / 64];        // D = 128: first numbers, remainders; D = 64: both in one
   unsigned scale;         // bytes: of q[0], of q[1]
 };
 
 template <int D>
 __device__ __forceinline__ f32x4 decode_scores4(const u32x4& k, unsigned ks, const DecodeQuery4<D>& q) {
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), q.q[0], s, kFp4, kFp8, 0, (int)ks, 0, (int)q.scale);
-  if constexpr (D == 128) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), q.q[1], s, kFp4, kFp8, 0, (int)ks, 1, (int)q.scale);
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[0]), s, kFp4, kFp6, 0, (int)ks, 0, (int)q.scale);
+  if constexpr (D == 128)
+    s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[1]), s, kFp4, kFp6, 0, (int)ks, 1, (int)q.scale);
   return s;
 }
 
@@ -168,49 +179,25 @@ __device__ __forceinline__ void decode_compute4(PairRegs4<D>& r, const DecodeQue
   }
 }
 
-// Query operand of a kv-head's q-heads (column n), zero past the group.  The 8-bit operand of 16x16x128 has dimensions 16j .. 16j + 15 and 64 + 16j ..
-// in lane group j, and lane group i names the scale of dimensions 32i ...
+// Query operand of a kv-head's q-heads (column n), zero past the group: lane group j has 32 dimensions, group j (D = 128), or group j & 1 (D = 64), whose
+// first numbers go to the lower half of the lanes and whose remainders to the upper.
 template <int D>
 __device__ __forceinline__ DecodeQuery4<D> decode_query4(const __bf16* q, const HfxItem& item, int g, int Hq, int G, int n, int j) {
   const int hh = n < G ? n : G - 1;
-  const __bf16* row = q + ((long)item.rq.q_start * Hq + g * G + hh) * D + j * 16;
-  bf16x8 x[D / 32];
+  const __bf16* row = q + ((long)item.rq.q_start * Hq + g * G + hh) * D + (j & (D / 32 - 1)) * 32;
+  bf16x8 x[4];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) x[i] = keep_first(ld16(row + (i >> 1) * 64 + (i & 1) * 8), n < G ? 8 : 0);
+  for (int i = 0; i < 4; ++i) x[i] = keep_first(ld16(row + i * 8), n < G ? 8 : 0);
+  const Query6 t = split_query(x);
   DecodeQuery4<D> r;
-  unsigned e[D / 64];
-#pragma unroll
-  for (int p = 0; p < D / 64; ++p) {
-    unsigned top = max(top_of(x[2 * p]), top_of(x[2 * p + 1]));
-    top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));        // the two lanes that share 32 dimensions
-    e[p] = query_scale(top);
-  }
-  const int from = (j & 1) * 32 + n;                               // of lane groups 0 and 1 (and 2, 3): the first 32 dimensions of 64, and the second
   if constexpr (D == 128) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      int f[2], s[2];
-      split_query(x[i], e[i >> 1], f, s);
-      r.q[0][2 * i] = f[0];
-      r.q[0][2 * i + 1] = f[1];
-      r.q[1][2 * i] = s[0];
-      r.q[1][2 * i + 1] = s[1];
-    }
-    const unsigned e0 = (unsigned)__shfl((int)e[0], from, 64), e1 = (unsigned)__shfl((int)e[D / 64 - 1], from, 64);
-    const unsigned own = j < 2 ? e0 : e1;
-    r.scale = own | (own - kRestScale) << 8;
+    r.q[0] = t.first;
+    r.q[1] = t.rest;
+    r.scale = t.scale;
   } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      int f[2], s[2];
-      split_query(x[i], e[0], f, s);
-      r.q[0][2 * i] = f[0];
-      r.q[0][2 * i + 1] = f[1];
-      r.q[0][4 + 2 * i] = s[0];
-      r.q[0][4 + 2 * i + 1] = s[1];
-    }
-    const unsigned e0 = (unsigned)__shfl((int)e[0], from, 64);
-    r.scale = j < 2 ? e0 : e0 - kRestScale;
+    for (int i = 0; i < 6; ++i) r.q[0][i] = j < 2 ? t.first[i] : t.rest[i];
+    r.scale = j < 2 ? t.scale : t.scale >> 8;
   }
   return r;
 }
@@ -347,7 +334,7 @@ __device__ __forceinline__ void raw_copy(const char* base, unsigned keys, unsign
 template <int D>
 struct PrefillWave4 {
   f32x16 o[D / 32];            // O^T accumulators per 32-dimension block
-  i32x8 q[D / 64][2];          // of 64 dimensions: first numbers, remainders
+  u32x6 q[D / 64][2];          // of 64 dimensions: first numbers, remainders
   unsigned qs;                 // their scale bytes, in that order
   float m, l;                  // reference exponent (base-2 domain) and running sum
 };
@@ -356,37 +343,45 @@ struct PrefillWave4 {
 template <int D>
 struct Keys4 {
   u32x4 k[D / 64];
-  unsigned scale;              // byte 2i: of k[i]
+  unsigned scale;              // the key's scales; shifted by 8 j (keys_ready), byte 2i is that of k[i]
 };
 
 template <int D>
-__device__ __forceinline__ Keys4<D> read_keys4(const char* stage, int k_lane, int s_lane, int j) {
+__device__ __forceinline__ void keys_ready(Keys4<D>& k, int j) { k.scale >>= 8 * j; }
+
+template <int D>
+__device__ __forceinline__ Keys4<D> read_keys4(const char* stage, int k_lane, int s_lane) {
   Keys4<D> r;
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) r.k[i] = *reinterpret_cast<const u32x4*>(stage + k_lane + i * 512);
-  if constexpr (D == 128) r.scale = *reinterpret_cast<const unsigned*>(stage + s_lane) >> (8 * j);
-  else r.scale = (unsigned)*reinterpret_cast<const uint16_t*>(stage + s_lane) >> (8 * j);
+  if constexpr (D == 128) r.scale = *reinterpret_cast<const unsigned*>(stage + s_lane);
+  else r.scale = (unsigned)*reinterpret_cast<const uint16_t*>(stage + s_lane);
   return r;
 }
 
-// Matrix instruction number i of a stage's scores: 64 dimensions i / 2, the first numbers or the remainders.
+// Matrix instruction number i of a stage's scores: 64 dimensions i / 2, the first numbers or the remainders.  (The empty asm holds it where it is: the
+// compiler takes it for an ordinary function of its operands and moves it down to where the result is used, out of the softmax it is meant to run beside.)
 template <int D>
-__device__ __forceinline__ f32x16 score_product(const PrefillWave4<D>& w, const Keys4<D>& k, int i, f32x16 s) {
-  if (i == 0) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[0]), w.q[0][0], s, kFp4, kFp8, 0, (int)k.scale, 0, (int)w.qs);
-  if (i == 1) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[0]), w.q[0][1], s, kFp4, kFp8, 0, (int)k.scale, 1, (int)w.qs);
-  if (i == 2) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[D / 64 - 1]), w.q[D / 64 - 1][0], s, kFp4, kFp8, 2, (int)k.scale, 2, (int)w.qs);
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(k.k[D / 64 - 1]), w.q[D / 64 - 1][1], s, kFp4, kFp8, 2, (int)k.scale, 3, (int)w.qs);
+__device__ __forceinline__ void score_product(const PrefillWave4<D>& w, const Keys4<D>& k, int i, f32x16& s) {
+  const i32x8 a = fp4_operand(k.k[i / 2]), b = fp6_operand(w.q[i / 2][i % 2]);
+  const int ks = (int)k.scale, qs = (int)w.qs;
+  if (i == 0) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 0, ks, 0, qs);
+  if (i == 1) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 0, ks, 1, qs);
+  if (i == 2) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 2, ks, 2, qs);
+  if (i == 3) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 2, ks, 3, qs);
+  asm volatile("" : "+v"(s));
 }
 
 // Scores of an item's first stage; the accumulators are cleared between the instructions.
 template <int D>
-__device__ __forceinline__ f32x16 first_scores4(PrefillWave4<D>& w, const Keys4<D>& k) {
+__device__ __forceinline__ f32x16 first_scores4(PrefillWave4<D>& w, Keys4<D>& k, int j) {
+  keys_ready<D>(k, j);
   f32x16 s;
 #pragma unroll
   for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
-    s = score_product<D>(w, k, i, s);
+    score_product<D>(w, k, i, s);
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       float zero = 0.f;
@@ -404,18 +399,24 @@ __device__ __forceinline__ bf16x8 value_fragment4(const char* values, int i, int
   return *reinterpret_cast<const bf16x8*>(values + (i / B) * Smem4<D>::kValuePage + (i % B) * 1024 + v_lane);
 }
 
+struct Nothing {
+  __device__ __forceinline__ void operator()(int) const {}
+};
+
 // First phase of a stage: scores of the next one, the second half of the weights of the present one (scores cur) between them, and the present
-// stage's value fragments.
-template <int D>
-__device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, const Keys4<D>& k, bf16x8* frag, const f32x16& cur, Weighing& wt, float sl2,
-                                                const char* values, int v_lane) {
+// stage's value fragments.  between(i) goes behind instruction i.
+template <int D, class Between>
+__device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, Keys4<D>& k, int j, bf16x8* frag, const f32x16& cur, Weighing& wt, float sl2,
+                                                const char* values, int v_lane, Between between) {
   constexpr int S = D / 16;
+  keys_ready<D>(k, j);
   f32x16 acc;
 #pragma unroll
   for (int v = 0; v < 16; ++v) acc[v] = 0.f;
 #pragma unroll
   for (int i = 0; i < S / 2; ++i) {
-    acc = score_product<D>(w, k, i, acc);
+    score_product<D>(w, k, i, acc);
+    between(i);
 #pragma unroll
     for (int h = 2 * i; h < 2 * i + 2; ++h) {
       frag[h] = value_fragment4<D>(values, h, v_lane);
@@ -427,64 +428,96 @@ __device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, const 
   return acc;
 }
 
-// Second phase: weighted values of the present stage, the first half of the weights of the next one (scores next) between them, and the keys of the
-// stage after next.
-template <int D>
-__device__ __forceinline__ void values_phase4(PrefillWave4<D>& w, const bf16x8* frag, const bf16x8* pb, const f32x16& next, Weighing& wt, float sl2) {
+// Second phase: weighted values of the present stage, the first half of the weights of the next one (scores next) between them.
+template <int D, class Between>
+__device__ __forceinline__ void values_phase4(PrefillWave4<D>& w, const bf16x8* frag, const bf16x8* pb, const f32x16& next, Weighing& wt, float sl2,
+                                              Between between) {
   constexpr int B = D / 32, S = 2 * B;
 #pragma unroll
   for (int i = 0; i < S; ++i) {
     w.o[i % B] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i], pb[i / B], w.o[i % B], 0, 0, 0);
+    between(i);
     wt.portion(i == 0 ? 0 : Share<D>::values[i - 1], Share<D>::values[i], Share<D>::values[i + 1], next, sl2, w.m);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// Query operands of this lane's row (rows past the chunk read the last row and are never stored).  The 8-bit operand of 32x32x64 has dimensions
-// 16j .. 16j + 15 and 32 + 16j .. of 64 in lane group j, and lane group i names the scale of dimensions 32i ...
+// Weighted values of an item's last stage.
 template <int D>
-__device__ __forceinline__ void query_rows4(PrefillWave4<D>& w, const bf16x8 (*x)[4]) {
-  w.qs = 0;
-  const int j = (threadIdx.x >> 5) & 1;
+__device__ __forceinline__ void last_values4(PrefillWave4<D>& w, const bf16x8* frag, const bf16x8* pb) {
+  constexpr int B = D / 32;
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    unsigned e[2];
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const unsigned top = max(top_of(x[i][2 * p]), top_of(x[i][2 * p + 1]));
-      const Pair32 both = swap32(__builtin_bit_cast(float, top));
-      e[p] = query_scale(max(__builtin_bit_cast(unsigned, both.lo), __builtin_bit_cast(unsigned, both.hi)));
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        int f[2], r[2];
-        split_query(x[i][2 * p + h], e[p], f, r);
-        w.q[i][0][4 * p + 2 * h] = f[0];
-        w.q[i][0][4 * p + 2 * h + 1] = f[1];
-        w.q[i][1][4 * p + 2 * h] = r[0];
-        w.q[i][1][4 * p + 2 * h + 1] = r[1];
-      }
-    }
-    const unsigned own = j ? e[1] : e[0];
-    w.qs |= (own | (own - kRestScale) << 8) << (16 * i);
-  }
+  for (int i = 0; i < 2 * B; ++i) w.o[i % B] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i], pb[i / B], w.o[i % B], 0, 0, 0);
 }
 
+// Query operands of this lane's row (rows past the chunk read the last row and are never stored): of each 64 dimensions lane group j has 32j .. 32j + 31.
 template <int D>
 __device__ __forceinline__ void query_load4(bf16x8 (*x)[4], const __bf16* q, int row0, int last, int Hq, int n, int j) {
-  const __bf16* qp = q + (long)min(row0 + n, last) * Hq * D + j * 16;
+  const __bf16* qp = q + (long)min(row0 + n, last) * Hq * D + j * 32;
 #pragma unroll
   for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-    for (int p = 0; p < 4; ++p) x[i][p] = ld16(qp + i * 64 + (p >> 1) * 32 + (p & 1) * 8);
+    for (int p = 0; p < 4; ++p) x[i][p] = ld16(qp + i * 64 + p * 8);
+}
+
+template <int D>
+__device__ __forceinline__ void query_rows4(PrefillWave4<D>& w, const bf16x8 (*x)[4]) {
+  w.qs = 0;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const Query6 t = split_query(x[i]);
+    w.q[i][0] = t.first;
+    w.q[i][1] = t.rest;
+    w.qs |= t.scale << (16 * i);
+  }
 }
 
 __device__ __forceinline__ int item_steps(const HfxItem& it) { return (int)((unsigned)(it.ke - it.kb + kStepKeys - 1) / kStepKeys); }
 
-// What the loop over an item's steps needs to know of the item after it.
+// What the loop over an item's steps needs to know of the item after it: how to copy its steps and where its query rows are.
 struct NextItem4 {
   int left, bt, last, head;
+  int q_row0, q_last;
+  const __bf16* q;
 };
 
+// A wavefront's part of widening a step's values, spread over the step.
+template <int D>
+struct Widening {
+  u32x4 codes, scales;
+  u32x4 lo, hi;
+
+  __device__ __forceinline__ void read(const char* raw, int w_codes, int w_scales, int lane) {
+    scales = *reinterpret_cast<const u32x4*>(raw + w_scales);
+    if constexpr (D == 128) {
+      codes = *reinterpret_cast<const u32x4*>(raw + w_codes);
+    } else {
+      const uint2 c = *reinterpret_cast<const uint2*>(raw + w_codes);
+      codes[0] = c.x;
+      codes[1] = c.y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) scales[k] >>= 8 * (lane & 1);          // which 32 dimensions of 64
+    }
+  }
+  // piece i of D / 16; every fourth completes two operands
+  __device__ __forceinline__ void piece(int i, char* to) {
+    const int k = i & 3;
+    if (i < 4) widen_pair<0>(k, codes[0], codes[1], scales, lo, hi);
+    else widen_pair<1>(k, codes[2], codes[3], scales, lo, hi);
+    if (k == 3) {
+      *reinterpret_cast<u32x4*>(to + i / 4 * 1024) = lo;
+      *reinterpret_cast<u32x4*>(to + i / 4 * 1024 + 512) = hi;
+    }
+  }
+};
+
+// Runs the prefill item t.cur and, for as long as the workgroup's next item is a prefill item as well, carries straight on into it: the stream of
+// page copies does not stop between items, only the per-row state is swapped.  Returns with t.cur at the first item it did not process.
+//
+// A wavefront's work on a step of two stages, behind the step's synchronisation point (scores of its first stage are there):
+//   scores of the second stage  | second half of the first's softmax, reads of its value fragments, the copies of the page two steps further on
+//   values of the first stage   | first half of the second's softmax, half of the next step's widening, key operands of the next step's first stage
+//   scores of the next step's first stage, values of the second stage likewise.
 template <int D>
 __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
                              char* smem, char* o_stage) {
@@ -511,97 +544,102 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   constexpr int kG = Mx<D>::kGroups;
   const unsigned c_keys = D == 128 || lane < 32 ? (unsigned)(((lane & 15) * kG + ((lane >> 4) & (kG - 1))) * 16) : (unsigned)lane * 16;
   const unsigned c_values = (unsigned)lane * 16, c_scales = (unsigned)(lane & (D / 4 - 1)) * 4;
-  const unsigned lds_raw = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * L::kRawPage;
+  const unsigned lds_raw = (unsigned)uniform((int)((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * L::kRawPage));
   // widening: this lane's value codes in the raw page, their scales, and where its dimensions go
   const int half = lane >> 5;
-  const int w_codes = Mx<D>::kValues + lane * (D / 8);
-  const int w_scales = Mx<D>::kValueScales + (D == 128 ? (lane >> 4) * 16 : half * 16);
+  const int w_codes = wave * L::kRawPage + Mx<D>::kValues + lane * (D / 8);
+  const int w_scales = wave * L::kRawPage + Mx<D>::kValueScales + (D == 128 ? (lane >> 4) * 16 : half * 16);
   const int w_i = D == 128 ? lane & 15 : (lane >> 1) & 15;
-  const int w_to = (D == 128 ? ((lane >> 4) & 1) * 2048 : (lane & 1) * 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
+  const int w_to = wave * L::kValuePage + (D == 128 ? ((lane >> 4) & 1) * 2048 : (lane & 1) * 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
 
   HfxItem it = items[t.cur];
-  HfxItem item1 = items[t.nxt < n_items ? t.nxt : t.cur];
+  const HfxItem item1 = items[t.nxt < n_items ? t.nxt : t.cur];
   bool next_ok = t.nxt < n_items && item1.type == HFX_ITEM_PREFILL;
-  auto source = [&](const HfxItem& item) {
+  const unsigned inv_g = 0xffffffffu / (unsigned)G + 1u;      // h / G by a multiplication (0 for G = 1)
+  auto q_rows = [&](const HfxItem& item, const WaveRows& r) { return a.q + ((long)item.rq.q_start * Hq + r.head) * D; };
+  auto next_item = [&](const HfxItem& item) {
+    const WaveRows r = wave_rows(item, wave);
     NextItem4 x;
     x.left = item_steps(item);
     x.bt = item.rq.bt_start + (int)((unsigned)item.kb / HFX_PAGE) + wave;
     x.last = item.rq.bt_start + item.rq.n_pages - 1;
-    x.head = item.h0 / G;
+    x.head = G == 1 ? item.h0 : (int)__umulhi((unsigned)item.h0, inv_g);
+    x.q_row0 = r.row0;
+    x.q_last = item.rq.q_len - 1;
+    x.q = q_rows(item, r);
     return x;
   };
-  // The stream of page copies: the steps of the current item and then those of the next.  Page ids, one a lane, for up to 64 steps at a time;
-  // the next lot is asked for as soon as one is begun.
-  NextItem4 from = source(it), nx = source(item1);
+  // The stream of page copies: the steps of the current item and then those of the next.  Blocks (page, kv-head), one a lane, for up to 64 steps at a time; the
+  // next lot is asked for as soon as one is begun.
+  NextItem4 nx = next_item(item1);
+  int left_to_ask, ask_bt, ask_last, ask_head;
+  auto ask_start = [&](const NextItem4& x) {
+    left_to_ask = x.left;
+    ask_bt = x.bt;
+    ask_last = x.last;
+    ask_head = x.head;
+  };
   bool in_next = false;
-  int ids = 0, at = 0, have = 0, ids_head = 0;
+  int ids = 0, at = 0, have = 0;
   int ids2 = 0, have2 = 0, head2 = 0;
   int fed = 0, widened = 0;            // steps whose copies have been issued, whose values have been widened, over all items of the run
   int g_st = 0;                        // step at work, likewise
   auto ask = [&]() {
-    if (from.left <= 0 && !in_next && next_ok) {
+    if (left_to_ask <= 0 && !in_next && next_ok) {
       in_next = true;
-      from = nx;
+      ask_start(nx);
     }
-    if (have2 == 0 && from.left > 0) {
-      ids2 = bt[min(from.bt + 4 * lane, from.last)];
-      have2 = min(from.left, 64);
-      head2 = from.head;
-      from.left -= have2;
-      from.bt += 4 * 64;
+    if (have2 == 0 && left_to_ask > 0) {
+      ids2 = bt[min(ask_bt + 4 * lane, ask_last)];
+      have2 = min(left_to_ask, 64);
+      head2 = ask_head;
+      left_to_ask -= have2;
+      ask_bt += 4 * 64;
     }
+  };
+  int raw_g = 0, raw_fed = 0;          // ring offsets of the step at work and of the next one to be copied
+  auto after = [&](int raw) { return raw == (L::kRawSteps - 1) * L::kRawStep ? 0 : raw + L::kRawStep; };
+  auto value_slot = [&](int step) { return values + (step & 1) * L::kValueStep; };
+  // copies the next step, which is in the lot at hand
+  auto copy_one = [&]() {
+    const unsigned block = (unsigned)__builtin_amdgcn_readlane(ids, at);
+    raw_copy<D>(pool + (unsigned long)block * Mx<D>::kBlock, c_keys, c_values, c_scales, lds_raw + (unsigned)raw_fed);
+    raw_fed = after(raw_fed);
+    ++at;
+    ++fed;
   };
   // copies steps up to `limit` as far as they are known
   auto feed = [&](int limit) {
     while (fed < limit) {
       if (at == have) {
         if (have2 == 0) break;
-        ids = ids2;
+        ids = ids2 * Hkv + head2;
         have = have2;
-        ids_head = head2;
         at = have2 = 0;
         ask();
       }
-      const int page = __builtin_amdgcn_readlane(ids, at);
-      ++at;
-      raw_copy<D>(pool + ((long)page * Hkv + ids_head) * Mx<D>::kBlock, c_keys, c_values, c_scales, (unsigned)uniform((int)(lds_raw + (unsigned)(fed % L::kRawSteps) * L::kRawStep)));
-      ++fed;
+      copy_one();
     }
   };
-  auto raw_slot = [&](int step) { return smem + (unsigned)(step % L::kRawSteps) * L::kRawStep; };
-  auto value_slot = [&](int step) { return values + (step & 1) * L::kValueStep; };
   // this wavefront's page of a step's values goes to its slot in bf16
-  auto widen = [&](int step) {
-    const char* raw = raw_slot(step) + wave * L::kRawPage;
-    char* to = value_slot(step) + wave * L::kValuePage + w_to;
-    u32x4 scales = *reinterpret_cast<const u32x4*>(raw + w_scales);
-    u32x4 lo, hi;
-    if constexpr (D == 128) {
-      const u32x4 codes = *reinterpret_cast<const u32x4*>(raw + w_codes);
-      widen_values<0>(codes[0], codes[1], scales, lo, hi);
-      *reinterpret_cast<u32x4*>(to) = lo;
-      *reinterpret_cast<u32x4*>(to + 512) = hi;
-      widen_values<1>(codes[2], codes[3], scales, lo, hi);
-      *reinterpret_cast<u32x4*>(to + 1024) = lo;
-      *reinterpret_cast<u32x4*>(to + 1536) = hi;
-    } else {
-      const uint2 codes = *reinterpret_cast<const uint2*>(raw + w_codes);
-      const int w = lane & 1;          // which 32 dimensions
+  auto widen = [&](int step, int raw) {
+    Widening<D> wd;
+    wd.read(smem + raw, w_codes, w_scales, lane);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) scales[k] >>= 8 * w;
-      widen_values<0>(codes.x, codes.y, scales, lo, hi);
-      *reinterpret_cast<u32x4*>(to) = lo;
-      *reinterpret_cast<u32x4*>(to + 512) = hi;
-    }
+    for (int i = 0; i < D / 16; ++i) wd.piece(i, value_slot(step) + w_to);
     widened = step + 1;
   };
-  ask();
 
   PrefillWave4<D> w;
   WaveRows wr = wave_rows(it, wave);
-  bf16x8 qx[D / 64][4];
-  auto q_rows = [&](const HfxItem& item, const WaveRows& r) { return a.q + ((long)item.rq.q_start * Hq + r.head) * D; };
-  query_load4<D>(qx, q_rows(it, wr), wr.row0, it.rq.q_len - 1, Hq, n, j);
+  {
+    bf16x8 qx[D / 64][4];
+    const NextItem4 first = next_item(it);
+    ask_start(first);
+    ask();
+    query_load4<D>(qx, first.q, first.q_row0, first.q_last, Hq, n, j);
+    query_rows4<D>(w, qx);
+  }
 
   for (;;) {
     // Start of an item: its first step's keys have landed for everybody and its values are widened, or that is done now.
@@ -610,85 +648,150 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       feed(g_st + L::kRawSteps);
       HFX_WAIT_VMCNT(0);
       ring_barrier();
-      widen(g_st);
+      widen(g_st, raw_g);
     }
-    query_rows4<D>(w, qx);
     w.l = 0.f;
     const int wave_end = wr.wave_kend, unmasked_upto = wr.wave_pmin, ctx_len = it.rq.ctx_len;
-    const int steps = item_steps(it);
+    int left = item_steps(it);
     int kt = it.kb;
     auto mask_stage = [&](f32x16& s, int key0) {     // keys past this lane's row's horizon (rows past the chunk: its last row's)
       if (key0 + SK - 1 > unmasked_upto) mask_scores(s, min(wr.wave_pmin + n, ctx_len - 1), key0 + j * 8);
     };
-    bf16x8 frag[S];
-    f32x16 s0, s1;
+    f32x16 s0;
     Weighing wt;
-    Keys4<D> keys = read_keys4<D>(raw_slot(g_st), k_lane, s_lane, j);
-    s0 = first_scores4<D>(w, keys);
-    keys = read_keys4<D>(raw_slot(g_st) + 2 * L::kRawPage, k_lane, s_lane, j);
+    Keys4<D> keys = read_keys4<D>(smem + raw_g, k_lane, s_lane);
+    s0 = first_scores4<D>(w, keys, j);
+    keys = read_keys4<D>(smem + raw_g + 2 * L::kRawPage, k_lane, s_lane);
     mask_stage(s0, kt);
     w.m = fmaxf(HFX_M_NONE, row_max(s0, sl2));
     wt.portion(0, 0, 4, s0, sl2, w.m);
     wt.portion(0, 4, 8, s0, sl2, w.m);
     wt.portion(4, Share<D>::values[S - 1], Share<D>::values[S - 1], s0, sl2, w.m);
-    auto mask_values = [&](int key0) {               // unused slots may hold anything
+    auto mask_values = [&](bf16x8* frag, int key0) {               // unused slots may hold anything
       if (key0 + SK > ctx_len) {
 #pragma unroll
         for (int i = 0; i < S; ++i) frag[i] = keep_first(frag[i], ctx_len - (key0 + i / (D / 32) * 16 + j * 8));
       }
     };
-    for (int left = steps; left > 0; --left) {
-      // Synchronisation point: the values of this step are widened, the next one's raw pages have landed, and nobody reads the slots any more that are
-      // filled next.  In the item's last step the next ticket is asked for and published.
-      if (left == 1) {
-        int reply = 0;
-        tickets_reserve(t, reply, ctrl);
-        HFX_WAIT_VMCNT(0);
-        tickets_publish(t, reply, s_tk, ctrl, H);
-      } else if (fed == g_st + L::kRawSteps) {
-        HFX_WAIT_VMCNT(L::kCopies);
-      } else {
-        HFX_WAIT_VMCNT(0);
+    auto settle = [&](const f32x16& s, bf16x8* pb) {
+      pb[0] = wt.fragment(0);
+      pb[1] = wt.fragment(1);
+      settle_weights<D>(w, s, pb, wt.sum(), sl2);
+    };
+    while (left > 1) {
+      // Steps that every row of the wavefront sees whole, with all copies in time: the common case, without any other condition.
+      int plain = 0;
+      if (wave_end > 0 && fed == g_st + L::kRawSteps && kt + 3 * SK - 1 <= unmasked_upto)
+        plain = uniform(min(min(left - 1, have - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1));
+      if (plain > 0) {
+        left -= plain;
+        kt += plain * kStepKeys;
+#pragma unroll 1
+        do {
+          HFX_WAIT_VMCNT(L::kCopies);
+          ring_barrier();
+          raw_g = after(raw_g);
+          const char* raw = smem + raw_g;
+          Widening<D> wd;
+          bf16x8 frag[S], pb[2];
+          char* const to = value_slot(g_st + 1) + w_to;
+          __builtin_amdgcn_sched_barrier(0);
+          const f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, value_slot(g_st), v_lane, [&](int i) {
+            if (i == 0) copy_one();
+            if (i == 1) wd.read(raw, w_codes, w_scales, lane);
+          });
+          settle(s0, pb);
+          __builtin_amdgcn_sched_barrier(0);
+          values_phase4<D>(w, frag, pb, s1, wt, sl2, [&](int i) {
+            if (i == 0) keys = read_keys4<D>(raw, k_lane, s_lane);
+            if (i % 2 == 1) wd.piece(i / 2, to);
+          });
+          s0 = scores_phase4<D>(w, keys, j, frag, s1, wt, sl2, value_slot(g_st) + 2 * L::kValuePage, v_lane, Nothing());
+          settle(s1, pb);
+          __builtin_amdgcn_sched_barrier(0);
+          values_phase4<D>(w, frag, pb, s0, wt, sl2, [&](int i) {
+            if (i == 0) keys = read_keys4<D>(raw + 2 * L::kRawPage, k_lane, s_lane);
+            if (i % 2 == 1) wd.piece(S / 2 + i / 2, to);
+          });
+          ++g_st;
+        } while (--plain > 0);
+        widened = g_st + 1;
+        ask();
+        continue;
       }
+      // Synchronisation point: the values of this step are widened, the next one's raw pages have landed, and nobody reads the slots any more that are
+      // filled next.
+      if (fed == g_st + L::kRawSteps) HFX_WAIT_VMCNT(L::kCopies);
+      else HFX_WAIT_VMCNT(0);
       ring_barrier();
       const bool landed = fed > g_st + 1;       // the next step's pages; copies issued now have not
       feed(g_st + 1 + L::kRawSteps);
       ask();
-      if (landed) widen(g_st + 1);
-      bf16x8 pb[2];
+      if (landed) widen(g_st + 1, after(raw_g));
       if (kt < wave_end) {
-        s1 = scores_phase4<D>(w, keys, frag, s0, wt, sl2, value_slot(g_st), v_lane);
-        pb[0] = wt.fragment(0);
-        pb[1] = wt.fragment(1);
-        settle_weights<D>(w, s0, pb, wt.sum(), sl2);
+        bf16x8 frag[S], pb[2];
+        f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, value_slot(g_st), v_lane, Nothing());
+        settle(s0, pb);
         mask_stage(s1, kt + SK);
-        mask_values(kt);
-        if (left > 1) keys = read_keys4<D>(raw_slot(g_st + 1), k_lane, s_lane, j);
+        mask_values(frag, kt);
+        keys = read_keys4<D>(smem + after(raw_g), k_lane, s_lane);
         __builtin_amdgcn_sched_barrier(0);
-        values_phase4<D>(w, frag, pb, s1, wt, sl2);
-      }
-      if (kt + SK < wave_end) {
-        if (left > 1) {
-          s0 = scores_phase4<D>(w, keys, frag, s1, wt, sl2, value_slot(g_st) + 2 * L::kValuePage, v_lane);
-        } else {
-#pragma unroll
-          for (int i = 0; i < S; ++i) frag[i] = value_fragment4<D>(value_slot(g_st) + 2 * L::kValuePage, i, v_lane);
-          wt.portion(Share<D>::values[S - 1], 8, 12, s1, sl2, w.m);
-          wt.portion(8, 12, 16, s1, sl2, w.m);
-          wt.portion(12, 16, 16, s1, sl2, w.m);
+        values_phase4<D>(w, frag, pb, s1, wt, sl2, Nothing());
+        if (kt + SK < wave_end) {
+          s0 = scores_phase4<D>(w, keys, j, frag, s1, wt, sl2, value_slot(g_st) + 2 * L::kValuePage, v_lane, Nothing());
+          settle(s1, pb);
+          mask_stage(s0, kt + 2 * SK);
+          mask_values(frag, kt + SK);
+          keys = read_keys4<D>(smem + after(raw_g) + 2 * L::kRawPage, k_lane, s_lane);
+          __builtin_amdgcn_sched_barrier(0);
+          values_phase4<D>(w, frag, pb, s0, wt, sl2, Nothing());
         }
-        pb[0] = wt.fragment(0);
-        pb[1] = wt.fragment(1);
-        settle_weights<D>(w, s1, pb, wt.sum(), sl2);
-        if (left > 1) mask_stage(s0, kt + 2 * SK);
-        mask_values(kt + SK);
-        if (left > 1) keys = read_keys4<D>(raw_slot(g_st + 1) + 2 * L::kRawPage, k_lane, s_lane, j);
-        __builtin_amdgcn_sched_barrier(0);
-        values_phase4<D>(w, frag, pb, s0, wt, sl2);
       }
       kt += kStepKeys;
       ++g_st;
+      raw_g = after(raw_g);
+      --left;
     }
+    // The item's last step.  The next ticket is asked for and published.
+    {
+      int reply = 0;
+      tickets_reserve(t, reply, ctrl);
+      HFX_WAIT_VMCNT(0);
+      tickets_publish(t, reply, s_tk, ctrl, H);
+      ring_barrier();
+      const bool landed = fed > g_st + 1;
+      feed(g_st + 1 + L::kRawSteps);
+      ask();
+      if (landed) widen(g_st + 1, after(raw_g));
+    }
+    bf16x8 qx[D / 64][4];
+    auto next_query = [&]() {          // the queries are not needed any more, and the next item's are asked for (where there is none: this one's again)
+      query_load4<D>(qx, nx.q, nx.q_row0, nx.q_last, Hq, n, j);
+    };
+    if (kt < wave_end) {
+      bf16x8 frag[S], pb[2];
+      f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, value_slot(g_st), v_lane, Nothing());
+      settle(s0, pb);
+      mask_stage(s1, kt + SK);
+      mask_values(frag, kt);
+      __builtin_amdgcn_sched_barrier(0);
+      values_phase4<D>(w, frag, pb, s1, wt, sl2, Nothing());
+      next_query();
+      if (kt + SK < wave_end) {
+#pragma unroll
+        for (int i = 0; i < S; ++i) frag[i] = value_fragment4<D>(value_slot(g_st) + 2 * L::kValuePage, i, v_lane);
+        wt.portion(Share<D>::values[S - 1], 8, 12, s1, sl2, w.m);
+        wt.portion(8, 12, 16, s1, sl2, w.m);
+        wt.portion(12, 16, 16, s1, sl2, w.m);
+        settle(s1, pb);
+        mask_values(frag, kt + SK);
+        last_values4<D>(w, frag, pb);
+      }
+    } else {
+      next_query();
+    }
+    ++g_st;
+    raw_g = after(raw_g);
     // hand-over
     tickets_take(t, s_tk, n_items);
     if (!next_ok) {
@@ -697,15 +800,14 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     }
     const HfxItem item_c = items[t.cur];
     const HfxItem item_n = items[t.nxt < n_items ? t.nxt : t.cur];
-    const WaveRows wr_c = wave_rows(item_c, wave);
-    query_load4<D>(qx, q_rows(item_c, wr_c), wr_c.row0, item_c.rq.q_len - 1, Hq, n, j);
-    if (!in_next) from = nx;
+    if (!in_next) ask_start(nx);
     in_next = false;
-    nx = source(item_n);
+    nx = next_item(item_n);
     next_ok = t.nxt < n_items && item_n.type == HFX_ITEM_PREFILL;
+    query_rows4<D>(w, qx);
     prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
     it = item_c;
-    wr = wr_c;
+    wr = wave_rows(it, wave);
   }
   __syncthreads();     // every wavefront is done with the ring before the LDS is used for anything else
 }
