@@ -372,27 +372,6 @@ __device__ __forceinline__ void score_product(const PrefillWave4<D>& w, const Ke
   asm volatile("" : "+v"(s));
 }
 
-// Scores of an item's first stage; the accumulators are cleared between the instructions.
-template <int D>
-__device__ __forceinline__ f32x16 first_scores4(PrefillWave4<D>& w, Keys4<D>& k, int j) {
-  keys_ready<D>(k, j);
-  f32x16 s;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) s[v] = 0.f;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    score_product<D>(w, k, i, s);
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      float zero = 0.f;
-      asm volatile("" : "+v"(zero));
-      w.o[i][v] = zero;
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  return s;
-}
-
 template <int D>
 __device__ __forceinline__ bf16x8 value_fragment4(const char* values, int i, int v_lane) {
   constexpr int B = D / 32;
@@ -442,14 +421,6 @@ __device__ __forceinline__ void values_phase4(PrefillWave4<D>& w, const bf16x8* 
   }
 }
 
-// Weighted values of an item's last stage.
-template <int D>
-__device__ __forceinline__ void last_values4(PrefillWave4<D>& w, const bf16x8* frag, const bf16x8* pb) {
-  constexpr int B = D / 32;
-#pragma unroll
-  for (int i = 0; i < 2 * B; ++i) w.o[i % B] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i], pb[i / B], w.o[i % B], 0, 0, 0);
-}
-
 // Query operands of this lane's row (rows past the chunk read the last row and are never stored): of each 64 dimensions lane group j has 32j .. 32j + 31.
 template <int D>
 __device__ __forceinline__ void query_load4(bf16x8 (*x)[4], const __bf16* q, int row0, int last, int Hq, int n, int j) {
@@ -487,12 +458,12 @@ struct Widening {
   u32x4 codes, scales;
   u32x4 lo, hi;
 
-  __device__ __forceinline__ void read(const char* raw, int w_codes, int w_scales, int lane) {
-    scales = *reinterpret_cast<const u32x4*>(raw + w_scales);
+  __device__ __forceinline__ void read(const char* from, const char* from_scales, int lane) {
+    scales = *reinterpret_cast<const u32x4*>(from_scales);
     if constexpr (D == 128) {
-      codes = *reinterpret_cast<const u32x4*>(raw + w_codes);
+      codes = *reinterpret_cast<const u32x4*>(from);
     } else {
-      const uint2 c = *reinterpret_cast<const uint2*>(raw + w_codes);
+      const uint2 c = *reinterpret_cast<const uint2*>(from);
       codes[0] = c.x;
       codes[1] = c.y;
 #pragma unroll
@@ -531,7 +502,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const int G = Hq / Hkv;
   const int n = lane & 31, j = lane >> 5;
   char* stage = o_stage + wave * 2048;
-  const float sl2 = H->softmax_scale * 1.4426950408889634f;
+  const float sl2 = __builtin_bit_cast(float, uniform(__builtin_bit_cast(int, H->softmax_scale * 1.4426950408889634f)));
   const int* __restrict__ bt = reinterpret_cast<const int*>(a.desc + H->off_bt);
   const char* pool = reinterpret_cast<const char*>(a.pool);
   // row of this lane's key inside a stage's 32 keys (as over the bf16 pool)
@@ -545,9 +516,9 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const unsigned c_keys = D == 128 || lane < 32 ? (unsigned)(((lane & 15) * kG + ((lane >> 4) & (kG - 1))) * 16) : (unsigned)lane * 16;
   const unsigned c_values = (unsigned)lane * 16, c_scales = (unsigned)(lane & (D / 4 - 1)) * 4;
   const unsigned lds_raw = (unsigned)uniform((int)((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * L::kRawPage));
-  // widening: this lane's value codes in the raw page, their scales, and where its dimensions go
+  // widening: this lane's value codes in the raw page (D = 128: at c_values too), their scales, and where its dimensions go
   const int half = lane >> 5;
-  const int w_codes = wave * L::kRawPage + Mx<D>::kValues + lane * (D / 8);
+  const int w_codes = wave * L::kRawPage + Mx<D>::kValues, w_lane = lane * (D / 8);
   const int w_scales = wave * L::kRawPage + Mx<D>::kValueScales + (D == 128 ? (lane >> 4) * 16 : half * 16);
   const int w_i = D == 128 ? lane & 15 : (lane >> 1) & 15;
   const int w_to = wave * L::kValuePage + (D == 128 ? ((lane >> 4) & 1) * 2048 : (lane & 1) * 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
@@ -624,7 +595,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   // this wavefront's page of a step's values goes to its slot in bf16
   auto widen = [&](int step, int raw) {
     Widening<D> wd;
-    wd.read(smem + raw, w_codes, w_scales, lane);
+    wd.read(smem + raw + w_codes + w_lane, smem + raw + w_scales, lane);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) wd.piece(i, value_slot(step) + w_to);
     widened = step + 1;
@@ -660,7 +631,15 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     f32x16 s0;
     Weighing wt;
     Keys4<D> keys = read_keys4<D>(smem + raw_g, k_lane, s_lane);
-    s0 = first_scores4<D>(w, keys, j);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) w.o[b][v] = 0.f;
+    keys_ready<D>(keys, j);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s0[v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) score_product<D>(w, keys, i, s0);
     keys = read_keys4<D>(smem + raw_g + 2 * L::kRawPage, k_lane, s_lane);
     mask_stage(s0, kt);
     w.m = fmaxf(HFX_M_NONE, row_max(s0, sl2));
@@ -678,120 +657,57 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       pb[1] = wt.fragment(1);
       settle_weights<D>(w, s, pb, wt.sum(), sl2);
     };
-    while (left > 1) {
-      // Steps that every row of the wavefront sees whole, with all copies in time: the common case, without any other condition.
-      int plain = 0;
-      if (wave_end > 0 && fed == g_st + L::kRawSteps && kt + 3 * SK - 1 <= unmasked_upto)
-        plain = uniform(min(min(left - 1, have - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1));
-      if (plain > 0) {
-        left -= plain;
-        kt += plain * kStepKeys;
-#pragma unroll 1
-        do {
-          HFX_WAIT_VMCNT(L::kCopies);
-          ring_barrier();
-          raw_g = after(raw_g);
-          const char* raw = smem + raw_g;
-          Widening<D> wd;
-          bf16x8 frag[S], pb[2];
-          char* const to = value_slot(g_st + 1) + w_to;
-          __builtin_amdgcn_sched_barrier(0);
-          const f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, value_slot(g_st), v_lane, [&](int i) {
-            if (i == 0) copy_one();
-            if (i == 1) wd.read(raw, w_codes, w_scales, lane);
-          });
-          settle(s0, pb);
-          __builtin_amdgcn_sched_barrier(0);
-          values_phase4<D>(w, frag, pb, s1, wt, sl2, [&](int i) {
-            if (i == 0) keys = read_keys4<D>(raw, k_lane, s_lane);
-            if (i % 2 == 1) wd.piece(i / 2, to);
-          });
-          s0 = scores_phase4<D>(w, keys, j, frag, s1, wt, sl2, value_slot(g_st) + 2 * L::kValuePage, v_lane, Nothing());
-          settle(s1, pb);
-          __builtin_amdgcn_sched_barrier(0);
-          values_phase4<D>(w, frag, pb, s0, wt, sl2, [&](int i) {
-            if (i == 0) keys = read_keys4<D>(raw + 2 * L::kRawPage, k_lane, s_lane);
-            if (i % 2 == 1) wd.piece(S / 2 + i / 2, to);
-          });
-          ++g_st;
-        } while (--plain > 0);
-        widened = g_st + 1;
-        ask();
-        continue;
-      }
+    while (left > 0) {
       // Synchronisation point: the values of this step are widened, the next one's raw pages have landed, and nobody reads the slots any more that are
-      // filled next.
-      if (fed == g_st + L::kRawSteps) HFX_WAIT_VMCNT(L::kCopies);
+      // filled next.  In the item's last step the next ticket is asked for and published (and what comes after the item is multiplied for nothing).
+      if (left == 1) {
+        int reply = 0;
+        tickets_reserve(t, reply, ctrl);
+        HFX_WAIT_VMCNT(0);
+        tickets_publish(t, reply, s_tk, ctrl, H);
+      } else if (fed == g_st + L::kRawSteps) HFX_WAIT_VMCNT(L::kCopies);
       else HFX_WAIT_VMCNT(0);
       ring_barrier();
       const bool landed = fed > g_st + 1;       // the next step's pages; copies issued now have not
       feed(g_st + 1 + L::kRawSteps);
       ask();
-      if (landed) widen(g_st + 1, after(raw_g));
+      const char* raw = smem + after(raw_g);
+      const char* slot = value_slot(g_st);
+      char* const to = value_slot(g_st + 1) + w_to;
+      Widening<D> wd;
       if (kt < wave_end) {
         bf16x8 frag[S], pb[2];
-        f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, value_slot(g_st), v_lane, Nothing());
+        f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, slot, v_lane, [&](int i) {
+          if (i == 1) wd.read(raw + w_codes + w_lane, raw + w_scales, lane);
+        });
         settle(s0, pb);
         mask_stage(s1, kt + SK);
         mask_values(frag, kt);
-        keys = read_keys4<D>(smem + after(raw_g), k_lane, s_lane);
         __builtin_amdgcn_sched_barrier(0);
-        values_phase4<D>(w, frag, pb, s1, wt, sl2, Nothing());
-        if (kt + SK < wave_end) {
-          s0 = scores_phase4<D>(w, keys, j, frag, s1, wt, sl2, value_slot(g_st) + 2 * L::kValuePage, v_lane, Nothing());
-          settle(s1, pb);
-          mask_stage(s0, kt + 2 * SK);
-          mask_values(frag, kt + SK);
-          keys = read_keys4<D>(smem + after(raw_g) + 2 * L::kRawPage, k_lane, s_lane);
-          __builtin_amdgcn_sched_barrier(0);
-          values_phase4<D>(w, frag, pb, s0, wt, sl2, Nothing());
-        }
+        values_phase4<D>(w, frag, pb, s1, wt, sl2, [&](int i) {
+          if (i == 0) keys = read_keys4<D>(raw, k_lane, s_lane);
+          if (i % 2 == 1) wd.piece(i / 2, to);
+        });
+        s0 = scores_phase4<D>(w, keys, j, frag, s1, wt, sl2, slot + 2 * L::kValuePage, v_lane, Nothing());
+        settle(s1, pb);
+        mask_stage(s0, kt + 2 * SK);
+        mask_values(frag, kt + SK);
+        __builtin_amdgcn_sched_barrier(0);
+        values_phase4<D>(w, frag, pb, s0, wt, sl2, [&](int i) {
+          if (i == 0) keys = read_keys4<D>(raw + 2 * L::kRawPage, k_lane, s_lane);
+          if (i % 2 == 1) wd.piece(S / 2 + i / 2, to);
+        });
+      } else {
+        wd.read(raw + w_codes + w_lane, raw + w_scales, lane);
+#pragma unroll
+        for (int i = 0; i < S; ++i) wd.piece(i, to);
       }
+      if (landed) widened = g_st + 2;           // (otherwise what has been widened was nothing yet, and it is done again)
       kt += kStepKeys;
       ++g_st;
       raw_g = after(raw_g);
       --left;
     }
-    // The item's last step.  The next ticket is asked for and published.
-    {
-      int reply = 0;
-      tickets_reserve(t, reply, ctrl);
-      HFX_WAIT_VMCNT(0);
-      tickets_publish(t, reply, s_tk, ctrl, H);
-      ring_barrier();
-      const bool landed = fed > g_st + 1;
-      feed(g_st + 1 + L::kRawSteps);
-      ask();
-      if (landed) widen(g_st + 1, after(raw_g));
-    }
-    bf16x8 qx[D / 64][4];
-    auto next_query = [&]() {          // the queries are not needed any more, and the next item's are asked for (where there is none: this one's again)
-      query_load4<D>(qx, nx.q, nx.q_row0, nx.q_last, Hq, n, j);
-    };
-    if (kt < wave_end) {
-      bf16x8 frag[S], pb[2];
-      f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, value_slot(g_st), v_lane, Nothing());
-      settle(s0, pb);
-      mask_stage(s1, kt + SK);
-      mask_values(frag, kt);
-      __builtin_amdgcn_sched_barrier(0);
-      values_phase4<D>(w, frag, pb, s1, wt, sl2, Nothing());
-      next_query();
-      if (kt + SK < wave_end) {
-#pragma unroll
-        for (int i = 0; i < S; ++i) frag[i] = value_fragment4<D>(value_slot(g_st) + 2 * L::kValuePage, i, v_lane);
-        wt.portion(Share<D>::values[S - 1], 8, 12, s1, sl2, w.m);
-        wt.portion(8, 12, 16, s1, sl2, w.m);
-        wt.portion(12, 16, 16, s1, sl2, w.m);
-        settle(s1, pb);
-        mask_values(frag, kt + SK);
-        last_values4<D>(w, frag, pb);
-      }
-    } else {
-      next_query();
-    }
-    ++g_st;
-    raw_g = after(raw_g);
     // hand-over
     tickets_take(t, s_tk, n_items);
     if (!next_ok) {
@@ -800,12 +716,14 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     }
     const HfxItem item_c = items[t.cur];
     const HfxItem item_n = items[t.nxt < n_items ? t.nxt : t.cur];
+    bf16x8 qx[D / 64][4];
+    query_load4<D>(qx, nx.q, nx.q_row0, nx.q_last, Hq, n, j);
     if (!in_next) ask_start(nx);
     in_next = false;
     nx = next_item(item_n);
     next_ok = t.nxt < n_items && item_n.type == HFX_ITEM_PREFILL;
-    query_rows4<D>(w, qx);
     prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
+    query_rows4<D>(w, qx);
     it = item_c;
     wr = wave_rows(it, wave);
   }
