@@ -329,6 +329,10 @@ __device__ __forceinline__ void raw_copy(const char* base, unsigned keys, unsign
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dword %1, %2 offset:1024"
                  :: "v"(keys), "v"(scales), "s"(base), "s"(lds) : "memory", "m0");
 }
+// 64 page ids, one a lane, out of a table (scalar base) at the lane's byte offset.
+__device__ __forceinline__ void ids_copy(const int* table, unsigned offset, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(offset), "s"(table), "s"(lds) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 template <int D>
@@ -382,6 +386,19 @@ struct Nothing {
   __device__ __forceinline__ void operator()(int) const {}
 };
 
+// Which weights are formed where (see Share): of a stage's 16 the value phase takes 10, the score phase, half as long here, 6, and its last
+// instruction none, so that the sum of the weights is known when it ends.  Two portions go behind each instruction of the score phase.
+template <int D>
+struct Share4;
+template <>
+struct Share4<128> {
+  static constexpr int values[9] = {0, 0, 1, 3, 4, 6, 7, 9, 10}, scores[9] = {10, 11, 12, 13, 14, 15, 16, 16, 16};
+};
+template <>
+struct Share4<64> {
+  static constexpr int values[5] = {0, 2, 5, 7, 10}, scores[5] = {10, 13, 16, 16, 16};
+};
+
 // First phase of a stage: scores of the next one, the second half of the weights of the present one (scores cur) between them, and the present
 // stage's value fragments.  between(i) goes behind instruction i.
 template <int D, class Between>
@@ -399,11 +416,11 @@ __device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, Keys4<
 #pragma unroll
     for (int h = 2 * i; h < 2 * i + 2; ++h) {
       frag[h] = value_fragment4<D>(values, h, v_lane);
-      wt.portion(h == 0 ? Share<D>::values[S - 1] : Share<D>::scores[h - 1], Share<D>::scores[h], Share<D>::scores[h + 1], cur, sl2, w.m);
+      wt.portion(h == 0 ? Share4<D>::values[S - 1] : Share4<D>::scores[h - 1], Share4<D>::scores[h], Share4<D>::scores[h + 1], cur, sl2, w.m);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  wt.portion(Share<D>::scores[S - 1], 16, 16, cur, sl2, w.m);
+  wt.portion(Share4<D>::scores[S - 1], 16, 16, cur, sl2, w.m);
   return acc;
 }
 
@@ -416,7 +433,7 @@ __device__ __forceinline__ void values_phase4(PrefillWave4<D>& w, const bf16x8* 
   for (int i = 0; i < S; ++i) {
     w.o[i % B] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i], pb[i / B], w.o[i % B], 0, 0, 0);
     between(i);
-    wt.portion(i == 0 ? 0 : Share<D>::values[i - 1], Share<D>::values[i], Share<D>::values[i + 1], next, sl2, w.m);
+    wt.portion(i == 0 ? 0 : Share4<D>::values[i - 1], Share4<D>::values[i], Share4<D>::values[i + 1], next, sl2, w.m);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -491,7 +508,7 @@ struct Widening {
 //   scores of the next step's first stage, values of the second stage likewise.
 template <int D>
 __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
-                             char* smem, char* o_stage) {
+                             char* smem, char* o_stage, int* s_ids) {
   typedef Smem4<D> L;
   constexpr int SK = HFX_STAGE_KEYS, S = D / 16;
   const int tid = threadIdx.x;
@@ -523,8 +540,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const int w_i = D == 128 ? lane & 15 : (lane >> 1) & 15;
   const int w_to = wave * L::kValuePage + (D == 128 ? ((lane >> 4) & 1) * 2048 : (lane & 1) * 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
 
-  HfxItem it = items[t.cur];
-  const HfxItem item1 = items[t.nxt < n_items ? t.nxt : t.cur];
+  const HfxItem item0 = items[t.cur], item1 = items[t.nxt < n_items ? t.nxt : t.cur];
   bool next_ok = t.nxt < n_items && item1.type == HFX_ITEM_PREFILL;
   const unsigned inv_g = 0xffffffffu / (unsigned)G + 1u;      // h / G by a multiplication (0 for G = 1)
   auto q_rows = [&](const HfxItem& item, const WaveRows& r) { return a.q + ((long)item.rq.q_start * Hq + r.head) * D; };
@@ -540,8 +556,9 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     x.q = q_rows(item, r);
     return x;
   };
-  // The stream of page copies: the steps of the current item and then those of the next.  Blocks (page, kv-head), one a lane, for up to 64 steps at a time; the
-  // next lot is asked for as soon as one is begun.
+  // The stream of page copies: the steps of the current item and then those of the next.  Page ids come in lots of up to 64 steps, into LDS by the same
+  // kind of load as the pages (with a lot in a register the compiler waited for it, and with it for every copy in flight, wherever the paths of
+  // the step loop meet: a 4096-row chunk behind 61440 tokens took 862 us); the next lot is asked for as soon as one is begun.
   NextItem4 nx = next_item(item1);
   int left_to_ask, ask_bt, ask_last, ask_head;
   auto ask_start = [&](const NextItem4& x) {
@@ -551,82 +568,93 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     ask_head = x.head;
   };
   bool in_next = false;
-  int ids = 0, at = 0, have = 0;
-  int ids2 = 0, have2 = 0, head2 = 0;
-  int fed = 0, widened = 0;            // steps whose copies have been issued, whose values have been widened, over all items of the run
-  int g_st = 0;                        // step at work, likewise
+  const int* const lots = s_ids + wave * 128;
+  const unsigned lds_lots = (unsigned)uniform((int)((unsigned)(uintptr_t)(__attribute__((address_space(3))) int*)s_ids + wave * 512));
+  int lot = 1, at = 0, have = 0, head = 0;             // the lot at hand: which half of the lots, next entry, entries, kv-head
+  int have2 = 0, head2 = 0;                            // the one behind it
+  bool asked = false;                                  // since the last wait for everything
+  int ahead = 0;                       // steps whose copies have been issued, counted from the one at work
+  int wide = 0;                        // steps whose values have been widened, likewise
+  int raw_g = 0, value_g = 0;          // ring offsets of the step at work
   auto ask = [&]() {
     if (left_to_ask <= 0 && !in_next && next_ok) {
       in_next = true;
       ask_start(nx);
     }
     if (have2 == 0 && left_to_ask > 0) {
-      ids2 = bt[min(ask_bt + 4 * lane, ask_last)];
+      ids_copy(bt, (unsigned)min(ask_bt + 4 * lane, ask_last) * 4u, lds_lots + (unsigned)(lot ^ 1) * 256u);
       have2 = min(left_to_ask, 64);
       head2 = ask_head;
       left_to_ask -= have2;
       ask_bt += 4 * 64;
+      asked = true;
     }
   };
-  int raw_g = 0, raw_fed = 0;          // ring offsets of the step at work and of the next one to be copied
-  auto after = [&](int raw) { return raw == (L::kRawSteps - 1) * L::kRawStep ? 0 : raw + L::kRawStep; };
-  auto value_slot = [&](int step) { return values + (step & 1) * L::kValueStep; };
-  // copies the next step, which is in the lot at hand
-  auto copy_one = [&]() {
-    const unsigned block = (unsigned)__builtin_amdgcn_readlane(ids, at);
-    raw_copy<D>(pool + (unsigned long)block * Mx<D>::kBlock, c_keys, c_values, c_scales, lds_raw + (unsigned)raw_fed);
-    raw_fed = after(raw_fed);
-    ++at;
-    ++fed;
+  auto raw_slot = [&](int steps) {     // of the step so many behind the one at work
+    const int to = raw_g + steps * L::kRawStep;
+    return to < L::kRing ? to : to - L::kRing;
   };
-  // copies steps up to `limit` as far as they are known
+  // copies the next step, whose entry of the lot at hand is `page`, to ring offset `to`
+  auto copy_one = [&](int page, int to) {
+    raw_copy<D>(pool + ((long)page * Hkv + head) * Mx<D>::kBlock, c_keys, c_values, c_scales, lds_raw + (unsigned)to);
+    ++at;
+  };
+  // copies steps until `limit` are on their way, as far as they are known; lots that have been asked for have landed, unless `asked`
   auto feed = [&](int limit) {
-    while (fed < limit) {
+    while (ahead < limit) {
       if (at == have) {
-        if (have2 == 0) break;
-        ids = ids2 * Hkv + head2;
+        if (have2 == 0 || asked) break;
+        lot ^= 1;
         have = have2;
+        head = head2;
         at = have2 = 0;
         ask();
       }
-      copy_one();
+      copy_one(uniform(lots[lot * 64 + at]), raw_slot(ahead));
+      ++ahead;
     }
   };
-  // this wavefront's page of a step's values goes to its slot in bf16
-  auto widen = [&](int step, int raw) {
-    Widening<D> wd;
-    wd.read(smem + raw + w_codes + w_lane, smem + raw + w_scales, lane);
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) wd.piece(i, value_slot(step) + w_to);
-    widened = step + 1;
-  };
-
   PrefillWave4<D> w;
-  WaveRows wr = wave_rows(it, wave);
+  // Of the item at work the loop keeps these; the rest is read from its record again at its end.
+  int kt, left, ctx_len;
+  WaveRows wr;
+  auto item_start = [&](const HfxItem& item) {
+    kt = item.kb;
+    left = item_steps(item);
+    ctx_len = item.rq.ctx_len;
+    wr = wave_rows(item, wave);
+  };
+  item_start(item0);
   {
     bf16x8 qx[D / 64][4];
-    const NextItem4 first = next_item(it);
+    const NextItem4 first = next_item(item0);
     ask_start(first);
-    ask();
     query_load4<D>(qx, first.q, first.q_row0, first.q_last, Hq, n, j);
+    ask();
     query_rows4<D>(w, qx);
   }
 
   for (;;) {
     // Start of an item: its first step's keys have landed for everybody and its values are widened, or that is done now.
     ask();
-    if (widened <= g_st) {
-      feed(g_st + L::kRawSteps);
+    if (wide < 1) {
       HFX_WAIT_VMCNT(0);
+      asm volatile("" ::: "memory");
+      asked = false;
+      feed(L::kRawSteps);
+      HFX_WAIT_VMCNT(0);
+      asked = false;
       ring_barrier();
-      widen(g_st, raw_g);
+      Widening<D> wd;
+      wd.read(smem + raw_g + w_codes + w_lane, smem + raw_g + w_scales, lane);
+#pragma unroll
+      for (int i = 0; i < S; ++i) wd.piece(i, values + value_g + w_to);
+      wide = 1;
     }
     w.l = 0.f;
-    const int wave_end = wr.wave_kend, unmasked_upto = wr.wave_pmin, ctx_len = it.rq.ctx_len;
-    int left = item_steps(it);
-    int kt = it.kb;
+    const int wave_end = wr.wave_kend, unmasked_upto = wr.wave_pmin;
     auto mask_stage = [&](f32x16& s, int key0) {     // keys past this lane's row's horizon (rows past the chunk: its last row's)
-      if (key0 + SK - 1 > unmasked_upto) mask_scores(s, min(wr.wave_pmin + n, ctx_len - 1), key0 + j * 8);
+      if (key0 + SK - 1 > unmasked_upto) mask_scores(s, min(unmasked_upto + n, ctx_len - 1), key0 + j * 8);
     };
     f32x16 s0;
     Weighing wt;
@@ -644,8 +672,8 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     mask_stage(s0, kt);
     w.m = fmaxf(HFX_M_NONE, row_max(s0, sl2));
     wt.portion(0, 0, 4, s0, sl2, w.m);
-    wt.portion(0, 4, 8, s0, sl2, w.m);
-    wt.portion(4, Share<D>::values[S - 1], Share<D>::values[S - 1], s0, sl2, w.m);
+    wt.portion(0, 4, Share4<D>::values[S], s0, sl2, w.m);
+    wt.portion(4, Share4<D>::values[S - 1], Share4<D>::values[S - 1], s0, sl2, w.m);
     auto mask_values = [&](bf16x8* frag, int key0) {               // unused slots may hold anything
       if (key0 + SK > ctx_len) {
 #pragma unroll
@@ -657,23 +685,45 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       pb[1] = wt.fragment(1);
       settle_weights<D>(w, s, pb, wt.sum(), sl2);
     };
-    while (left > 0) {
+    int plain = 0;        // steps ahead that every row of the wavefront sees whole and whose copies are in the lot at hand and in time
+    for (; left > 0; --left) {
+      if (plain == 0 && ahead == L::kRawSteps && !asked && wave_end > 0 && kt + 3 * SK - 1 <= unmasked_upto)
+        plain = min(min(left - 1, have - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1);
+      const bool whole = plain > 0;
+      const int page = lots[lot * 64 + (at & 63)];         // (read ahead of the waits; at == have: of no use)
+      const char* const slot = values + value_g;
+      value_g ^= L::kValueStep;
+      char* const to = values + value_g + w_to;
+      const int raw_next = raw_slot(1);
+      const char* const raw = smem + raw_next;
       // Synchronisation point: the values of this step are widened, the next one's raw pages have landed, and nobody reads the slots any more that are
       // filled next.  In the item's last step the next ticket is asked for and published (and what comes after the item is multiplied for nothing).
-      if (left == 1) {
-        int reply = 0;
-        tickets_reserve(t, reply, ctrl);
-        HFX_WAIT_VMCNT(0);
-        tickets_publish(t, reply, s_tk, ctrl, H);
-      } else if (fed == g_st + L::kRawSteps) HFX_WAIT_VMCNT(L::kCopies);
-      else HFX_WAIT_VMCNT(0);
-      ring_barrier();
-      const bool landed = fed > g_st + 1;       // the next step's pages; copies issued now have not
-      feed(g_st + 1 + L::kRawSteps);
-      ask();
-      const char* raw = smem + after(raw_g);
-      const char* slot = value_slot(g_st);
-      char* const to = value_slot(g_st + 1) + w_to;
+      if (whole) {
+        --plain;
+        HFX_WAIT_VMCNT(L::kCopies);
+        ring_barrier();
+        copy_one(uniform(page), raw_g);
+      } else {
+        if (left == 1) {
+          int reply = 0;
+          tickets_reserve(t, reply, ctrl);
+          HFX_WAIT_VMCNT(0);
+          asked = false;
+          tickets_publish(t, reply, s_tk, ctrl, H);
+        } else if (ahead == L::kRawSteps && !asked) {
+          HFX_WAIT_VMCNT(L::kCopies);
+        } else {
+          HFX_WAIT_VMCNT(0);
+          asked = false;
+        }
+        ring_barrier();
+        wide = ahead > 1 ? 2 : 1;            // the next step's pages have landed (copies issued now have not); if not, what is widened below is nothing yet
+        feed(1 + L::kRawSteps);
+        ask();
+        --ahead;
+        --wide;
+      }
+      raw_g = raw_next;
       Widening<D> wd;
       if (kt < wave_end) {
         bf16x8 frag[S], pb[2];
@@ -681,8 +731,10 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
           if (i == 1) wd.read(raw + w_codes + w_lane, raw + w_scales, lane);
         });
         settle(s0, pb);
-        mask_stage(s1, kt + SK);
-        mask_values(frag, kt);
+        if (!whole) {
+          mask_stage(s1, kt + SK);
+          mask_values(frag, kt);
+        }
         __builtin_amdgcn_sched_barrier(0);
         values_phase4<D>(w, frag, pb, s1, wt, sl2, [&](int i) {
           if (i == 0) keys = read_keys4<D>(raw, k_lane, s_lane);
@@ -690,25 +742,24 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
         });
         s0 = scores_phase4<D>(w, keys, j, frag, s1, wt, sl2, slot + 2 * L::kValuePage, v_lane, Nothing());
         settle(s1, pb);
-        mask_stage(s0, kt + 2 * SK);
-        mask_values(frag, kt + SK);
+        if (!whole) {
+          mask_stage(s0, kt + 2 * SK);
+          mask_values(frag, kt + SK);
+        }
         __builtin_amdgcn_sched_barrier(0);
         values_phase4<D>(w, frag, pb, s0, wt, sl2, [&](int i) {
           if (i == 0) keys = read_keys4<D>(raw + 2 * L::kRawPage, k_lane, s_lane);
-          if (i % 2 == 1) wd.piece(S / 2 + i / 2, to);
+          if (i < S / 2) wd.piece(S / 2 + i, to);          // (early, so that the synchronisation point does not wait for the writes)
         });
       } else {
         wd.read(raw + w_codes + w_lane, raw + w_scales, lane);
 #pragma unroll
         for (int i = 0; i < S; ++i) wd.piece(i, to);
       }
-      if (landed) widened = g_st + 2;           // (otherwise what has been widened was nothing yet, and it is done again)
       kt += kStepKeys;
-      ++g_st;
-      raw_g = after(raw_g);
-      --left;
     }
     // hand-over
+    const HfxItem it = items[t.cur];
     tickets_take(t, s_tk, n_items);
     if (!next_ok) {
       prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
@@ -724,8 +775,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     next_ok = t.nxt < n_items && item_n.type == HFX_ITEM_PREFILL;
     prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
     query_rows4<D>(w, qx);
-    it = item_c;
-    wr = wave_rows(it, wave);
+    item_start(item_c);
   }
   __syncthreads();     // every wavefront is done with the ring before the LDS is used for anything else
 }
@@ -743,13 +793,14 @@ __global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(c
   __shared__ __attribute__((aligned(1024))) char smem[Smem4<D>::kBytes];
   __shared__ int s_tk[2];
   __shared__ __attribute__((aligned(128))) char s_ostage[4 * 2048];      // result rows on their way out (prefill_store)
+  __shared__ __attribute__((aligned(16))) int s_ids[4 * 128];            // page ids of steps to come (prefill_run4)
   const HfxHeader* H = &hdr;
   const HfxItem* items = reinterpret_cast<const HfxItem*>(a.desc + H->off_items);
   const int n_items = H->n_items;
   Tickets t = tickets_start(H, a.desc);
   while (t.cur < n_items) {
     if (items[t.cur].type == HFX_ITEM_DECODE) decode_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem);
-    else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ostage);
+    else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ostage, s_ids);
   }
   queue_done(H, ctrl);
 }
