@@ -570,8 +570,8 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   bool in_next = false;
   const int* const lots = s_ids + wave * 128;
   const unsigned lds_lots = (unsigned)uniform((int)((unsigned)(uintptr_t)(__attribute__((address_space(3))) int*)s_ids + wave * 512));
-  int lot = 1, at = 0, have = 0, head = 0;             // the lot at hand: which half of the lots, next entry, entries, kv-head
-  int have2 = 0, head2 = 0;                            // the one behind it
+  int lot = 1, at = 0, end = 0, head = 0;              // the lot at hand: which half of the lots, next entry, end, kv-head
+  int have2 = 0, head2 = 0;                            // entries and kv-head of the one behind it
   bool asked = false;                                  // since the last wait for everything
   int ahead = 0;                       // steps whose copies have been issued, counted from the one at work
   int wide = 0;                        // steps whose values have been widened, likewise
@@ -596,29 +596,32 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   };
   // copies the next step, whose entry of the lot at hand is `page`, to ring offset `to`
   auto copy_one = [&](int page, int to) {
-    raw_copy<D>(pool + ((long)page * Hkv + head) * Mx<D>::kBlock, c_keys, c_values, c_scales, lds_raw + (unsigned)to);
+    const unsigned block = (unsigned)page * (unsigned)Hkv + (unsigned)head;
+    raw_copy<D>(pool + (unsigned long)block * Mx<D>::kBlock, c_keys, c_values, c_scales, lds_raw + (unsigned)to);
     ++at;
   };
   // copies steps until `limit` are on their way, as far as they are known; lots that have been asked for have landed, unless `asked`
   auto feed = [&](int limit) {
     while (ahead < limit) {
-      if (at == have) {
+      if (at == end) {
         if (have2 == 0 || asked) break;
         lot ^= 1;
-        have = have2;
+        at = lot * 64;
+        end = at + have2;
         head = head2;
-        at = have2 = 0;
+        have2 = 0;
         ask();
       }
-      copy_one(uniform(lots[lot * 64 + at]), raw_slot(ahead));
+      copy_one(uniform(lots[at]), raw_slot(ahead));
       ++ahead;
     }
   };
   PrefillWave4<D> w;
-  // Of the item at work the loop keeps these; the rest is read from its record again at its end.
+  HfxItem it;
   int kt, left, ctx_len;
   WaveRows wr;
   auto item_start = [&](const HfxItem& item) {
+    it = item;
     kt = item.kb;
     left = item_steps(item);
     ctx_len = item.rq.ctx_len;
@@ -688,9 +691,8 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     int plain = 0;        // steps ahead that every row of the wavefront sees whole and whose copies are in the lot at hand and in time
     for (; left > 0; --left) {
       if (plain == 0 && ahead == L::kRawSteps && !asked && wave_end > 0 && kt + 3 * SK - 1 <= unmasked_upto)
-        plain = min(min(left - 1, have - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1);
+        plain = uniform(min(min(left - 1, end - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1));
       const bool whole = plain > 0;
-      const int page = lots[lot * 64 + (at & 63)];         // (read ahead of the waits; at == have: of no use)
       const char* const slot = values + value_g;
       value_g ^= L::kValueStep;
       char* const to = values + value_g + w_to;
@@ -700,6 +702,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       // filled next.  In the item's last step the next ticket is asked for and published (and what comes after the item is multiplied for nothing).
       if (whole) {
         --plain;
+        const int page = lots[at];           // (read ahead of the waits)
         HFX_WAIT_VMCNT(L::kCopies);
         ring_barrier();
         copy_one(uniform(page), raw_g);
@@ -725,7 +728,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       }
       raw_g = raw_next;
       Widening<D> wd;
-      if (kt < wave_end) {
+      if (whole || kt < wave_end) {
         bf16x8 frag[S], pb[2];
         f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, slot, v_lane, [&](int i) {
           if (i == 1) wd.read(raw + w_codes + w_lane, raw + w_scales, lane);
@@ -759,7 +762,6 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       kt += kStepKeys;
     }
     // hand-over
-    const HfxItem it = items[t.cur];
     tickets_take(t, s_tk, n_items);
     if (!next_ok) {
       prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
