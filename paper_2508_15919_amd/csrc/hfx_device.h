@@ -253,19 +253,19 @@ __device__ __forceinline__ DecodeWave decode_wave(const int* __restrict__ bt, co
 
 // Combines a decode item's wavefronts and stores the result: wavefront partials (o[b][v] is dimension 16b + 4j + v of q-head n of the
 // wavefront's kv-head, m and l its reference exponent and running sum) go through LDS, and the token partitions of each head are joined into
-// normalised bf16 rows or, where the item is one split of a group, into (m, l, acc) partial rows.
-constexpr int decode_part_bytes(int D) { return 4 * 16 * (D + 4) * 4; }     // LDS: [4 wavefronts][16 heads][D + 4] floats
+// normalised bf16 rows or, where the item is one split of a group, into (m, l, acc) partial rows.  A wavefront's 16 rows of D + 4 floats lie `stride` bytes
+// behind those of the one before it.
+constexpr int decode_part_bytes(int D) { return 4 * 16 * (D + 4) * 4; }     // LDS that they take without gaps
 template <int D>
 __device__ __forceinline__ void decode_store(const KArgs& a, const HfxHeader* H, const HfxItem& it, const f32x4* o, float m, float l, int Hq, int G,
-                                             int tid, int wave, int n, int j, char* smem) {
+                                             int tid, int wave, int n, int j, char* smem, int stride = decode_part_bytes(D) / 4) {
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
 
-  // part[wave][head n][D + 4]
   constexpr int PS = D + 4;
-  float* part = reinterpret_cast<float*>(smem);
+  auto part = [&](int w, int head) { return reinterpret_cast<float*>(smem + w * stride) + head * PS; };
   if (n < G) {
-    float* dst = part + ((wave * 16 + n) * PS);
+    float* dst = part(wave, n);
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(dst + b * 16 + 4 * j) = o[b];
     if (j == 0) {
@@ -285,11 +285,11 @@ __device__ __forceinline__ void decode_store(const KArgs& a, const HfxHeader* H,
     const int row = idx / C4, d4 = (idx % C4) * 4;
     const int hwi = row / G, hh = row % G;
     float mm = NEG_INF;
-    for (int tt = 0; tt < TW; ++tt) mm = fmaxf(mm, part[((tt * HW + hwi) * 16 + hh) * PS + D]);
+    for (int tt = 0; tt < TW; ++tt) mm = fmaxf(mm, part(tt * HW + hwi, hh)[D]);
     float ll = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int tt = 0; tt < TW; ++tt) {
-      const float* src = part + ((tt * HW + hwi) * 16 + hh) * PS;
+      const float* src = part(tt * HW + hwi, hh);
       const float wgt = fast_exp2(src[D] - mm);
       ll += src[D + 1] * wgt;
       acc += *reinterpret_cast<const f32x4*>(src + d4) * wgt;

@@ -84,40 +84,71 @@ __device__ __forceinline__ void widen_values(unsigned a, unsigned b, const u32x4
   for (int k = 0; k < 4; ++k) widen_pair<At>(k, a, b, scales, lo, hi);
 }
 
+// A page's block in LDS: key codes [group][16 keys][16 bytes], value codes, then the scales as in the block; the copy of the scales writes 256
+// bytes, and 64 more put the keys of two pages in a row on different banks.
+template <int D>
+struct RawPage {
+  static constexpr int kBytes = 16 * D + 256 + 64;
+  static constexpr int kCopies = D == 128 ? 3 : 2;     // instructions that copy it
+};
+// Offsets, inside a block, of the lane's parts of the copy: keys change their order from [key][group] to [group][key].
+template <int D>
+struct CopyLane {
+  unsigned keys, values, scales;
+};
+template <int D>
+__device__ __forceinline__ CopyLane<D> copy_lane(int lane) {
+  constexpr int kG = Mx<D>::kGroups;
+  CopyLane<D> c;
+  c.keys = D == 128 || lane < 32 ? (unsigned)(((lane & 15) * kG + ((lane >> 4) & (kG - 1))) * 16) : (unsigned)lane * 16;
+  c.values = (unsigned)lane * 16;
+  c.scales = (unsigned)(lane & (D / 4 - 1)) * 4;
+  return c;
+}
+// Reads of the block table between copies that the compiler does not know of are scalar loads all the same: constant memory does not change.
+typedef const __attribute__((address_space(4))) int* ConstantInts;
+__device__ __forceinline__ ConstantInts constant(const int* p) { return (ConstantInts)(uintptr_t)p; }
+
+__device__ __forceinline__ unsigned lds_offset(const void* p) {
+  return (unsigned)uniform((int)(unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)p);
+}
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// Direct-to-LDS copy of a page's block: base (scalar), the lane's offsets, LDS destination.  The compiler does not know of these loads: its own
+// waits for vector memory become stricter by them, and those for what is copied are explicit (HFX_WAIT_VMCNT).
+template <int D>
+__device__ __forceinline__ void raw_copy(const char* base, const CopyLane<D>& c, unsigned lds) {
+  if constexpr (D == 128)
+    asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %3\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024\n\t"
+                 "global_load_lds_dword %2, %3 offset:2048"
+                 :: "v"(c.keys), "v"(c.values), "v"(c.scales), "s"(base), "s"(lds) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dword %1, %2 offset:1024"
+                 :: "v"(c.keys), "v"(c.scales), "s"(base), "s"(lds) : "memory", "m0");
+}
+// 64 page ids, one a lane, out of a table (scalar base) at the lane's byte offset.
+__device__ __forceinline__ void ids_copy(const int* table, unsigned offset, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(offset), "s"(table), "s"(lds) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // ----------------------------------------------------------------------------------------------
 // Decode item: as over the bf16 pool one wavefront per kv-head (hn of them), the others interleave over page pairs.  Per pair (32 tokens) and kv-head a
-// wavefront takes 4352 bytes (D = 128).
+// wavefront takes 4352 bytes (D = 128), by direct-to-LDS copies into a ring of its own, three pairs ahead of their use: 104 KB in flight on a CU
+// without a register.
 //   S^T[token][head]: 16x16x128, a lane has 32 dimensions of one key (a group) with their scale; D = 64: lanes of the upper half have the
 //                     same keys again, and the queries' remainders there, so that one instruction does both products.
 //   O^T[d][head]    : 16x16x32 bf16, a lane has eight tokens of dimension n of each tile.
+// The softmax is that of the prefill items: weights against the maximum of the item's first pair, which is raised only when a lane's eight weights sum to
+// more than 2^8, so that the common pair needs no maximum, no exchange between lanes and no rescaling.
 // ----------------------------------------------------------------------------------------------
-template <int D>
-struct PairRegs4 {
-  u32x4 ka, kb;                          // key codes of the two score tiles
-  unsigned sa, sb;                       // and scale bytes
-  u32x4 v[D / 64], vs[D / 64];           // value codes and scales of 64 dimensions
-};
+constexpr int kRingPairs = 4;
 
-// Lane's parts of the addresses inside a block.
+// Lane's parts of the LDS addresses inside a pair.
 struct DecodeLane4 {
   int key, key_scale, value, value_scale;
-  bool key_second, value_second;         // page of the pair
 };
-
-template <int D>
-__device__ __forceinline__ void decode_load4(PairRegs4<D>& r, const char* pool, int pg0, int pg1, int Hkv, int g, const DecodeLane4& a) {
-  const char* kp = pool + ((long)(a.key_second ? pg1 : pg0) * Hkv + g) * Mx<D>::kBlock;
-  const char* vp = pool + ((long)(a.value_second ? pg1 : pg0) * Hkv + g) * Mx<D>::kBlock;
-  r.ka = *reinterpret_cast<const u32x4*>(kp + a.key);
-  r.kb = *reinterpret_cast<const u32x4*>(kp + a.key + 4 * (D / 2));
-  r.sa = *reinterpret_cast<const uint8_t*>(kp + a.key_scale);
-  r.sb = *reinterpret_cast<const uint8_t*>(kp + a.key_scale + 4 * Mx<D>::kGroups);
-#pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    r.v[i] = *reinterpret_cast<const u32x4*>(vp + a.value + i * 256);
-    r.vs[i] = *reinterpret_cast<const u32x4*>(vp + a.value_scale + i * 16);
-  }
-}
 
 template <int D>
 struct DecodeQuery4 {
@@ -134,48 +165,80 @@ __device__ __forceinline__ f32x4 decode_scores4(const u32x4& k, unsigned ks, con
   return s;
 }
 
+// State of a decode item: reference exponent and running sum of this lane's column, O^T accumulators.
 template <int D>
-__device__ __forceinline__ void decode_compute4(PairRegs4<D>& r, const DecodeQuery4<D>& q, f32x4* o, float& m, float& l, float sl2, int nv) {
-  const f32x4 sa = decode_scores4<D>(r.ka, r.sa, q), sb = decode_scores4<D>(r.kb, r.sb, q);
+struct DecodeState4 {
+  float m, l;
+  f32x4 o[D / 16];
+};
+
+// Maximum over a column: lanes n, n + 16, n + 32, n + 48.
+__device__ __forceinline__ float column_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return max_xor32(x);
+}
+
+__device__ __forceinline__ float decode_weights(const float* s, float sl2, float m, bf16x8& pb) {
+  float p[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    p[e] = fast_exp2(__builtin_fmaf(s[e], sl2, -m));
+    pb[e] = (__bf16)p[e];
+  }
+  return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+}
+
+template <int D>
+__device__ __forceinline__ void decode_pair4(const char* ring, const DecodeLane4& a, const DecodeQuery4<D>& q, DecodeState4<D>& w, float sl2, bool first, bool tail,
+                                             int nv) {
+  const u32x4 ka = *reinterpret_cast<const u32x4*>(ring + a.key), kb = *reinterpret_cast<const u32x4*>(ring + a.key + 64);
+  const unsigned ea = *reinterpret_cast<const uint8_t*>(ring + a.key_scale);
+  const unsigned eb = *reinterpret_cast<const uint8_t*>(ring + a.key_scale + 4 * Mx<D>::kGroups);
+  u32x4 v[D / 64], vs[D / 64];
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    v[i] = *reinterpret_cast<const u32x4*>(ring + a.value + i * 256);
+    vs[i] = *reinterpret_cast<const u32x4*>(ring + a.value_scale + i * 16);
+  }
+  const f32x4 sa = decode_scores4<D>(ka, ea, q), sb = decode_scores4<D>(kb, eb, q);
   float s[8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    s[e] = sa[e] * sl2;
-    s[4 + e] = sb[e] * sl2;
+    s[e] = sa[e];
+    s[4 + e] = sb[e];
   }
-  if (nv < 8) {
+  if (tail) {              // tokens past the context
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] = keep_or_neg_inf(s[e], e < nv);
   }
-  float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-  const float mn = fmaxf(m, mx);
-  const float alpha = fast_exp2(m - mn);
-  float ps = 0.f;
+  auto top = [&]() {
+    return column_max(fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])))) * sl2;
+  };
+  if (first) w.m = top();
   bf16x8 pb;
+  float sum = decode_weights(s, sl2, w.m, pb);
+  if (__builtin_expect(__any(sum > 256.0f), 0)) {
+    const float m = fmaxf(w.m, top());
+    const float alpha = fast_exp2(w.m - m);
+    w.l *= alpha;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float p = fast_exp2(s[e] - mn);
-    ps += p;
-    pb[e] = (__bf16)p;
+    for (int b = 0; b < D / 16; ++b) w.o[b] *= alpha;
+    w.m = m;
+    sum = decode_weights(s, sl2, m, pb);
   }
-  l = l * alpha + ps;
-  m = mn;
+  w.l += sum;
 #pragma unroll
   for (int t = 0; t < D / 32; ++t) {
     u32x4 lo, hi;
-    if (t % 2 == 0) widen_values<0>(r.v[t / 2][0], r.v[t / 2][1], r.vs[t / 2], lo, hi);
-    else widen_values<1>(r.v[t / 2][2], r.v[t / 2][3], r.vs[t / 2], lo, hi);
+    if (t % 2 == 0) widen_values<0>(v[t / 2][0], v[t / 2][1], vs[t / 2], lo, hi);
+    else widen_values<1>(v[t / 2][2], v[t / 2][3], vs[t / 2], lo, hi);
     bf16x8 v0 = __builtin_bit_cast(bf16x8, lo), v1 = __builtin_bit_cast(bf16x8, hi);
-    if (nv < 8) {          // unused slots hold anything
+    if (tail) {            // unused slots hold anything
       v0 = keep_first(v0, nv);
       v1 = keep_first(v1, nv);
     }
-    o[2 * t] *= alpha;
-    o[2 * t + 1] *= alpha;
-    o[2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pb, o[2 * t], 0, 0, 0);
-    o[2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pb, o[2 * t + 1], 0, 0, 0);
+    w.o[2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pb, w.o[2 * t], 0, 0, 0);
+    w.o[2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pb, w.o[2 * t + 1], 0, 0, 0);
   }
 }
 
@@ -202,10 +265,11 @@ __device__ __forceinline__ DecodeQuery4<D> decode_query4(const __bf16* q, const 
   return r;
 }
 
-// Runs the decode item t.cur and carries on for as long as the workgroup's next item is a decode item too, as over the bf16 pool.
+// Runs the decode item t.cur and carries on for as long as the workgroup's next item is a decode item too.
 template <int D>
 __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
                             char* smem) {
+  constexpr int kPage = RawPage<D>::kBytes, kRing = 2 * kRingPairs * kPage, kCopies = 2 * RawPage<D>::kCopies;
   const int tid = threadIdx.x;
   int lane = tid & 63;
   asm volatile("" : "+v"(lane));     // what follows from it is formed per run, not kept in registers through prefill runs
@@ -213,7 +277,7 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
   const int Hq = H->num_q_heads, Hkv = H->num_kv_heads;
   const int G = Hq / Hkv;
   const int n = lane & 15, j = lane >> 4;
-  const float sl2 = H->softmax_scale * 1.4426950408889634f;
+  const float sl2 = __builtin_bit_cast(float, uniform(__builtin_bit_cast(int, H->softmax_scale * 1.4426950408889634f)));
   const int* bt = reinterpret_cast<const int*>(a.desc + H->off_bt);
   const char* pool = reinterpret_cast<const char*>(a.pool);
   // Row rho of score tile A is token ((rho>>2)&1)*8 + (rho&3) of page rho>>3, of tile B the token 4 further on; so a lane holds the scores of 8
@@ -221,72 +285,70 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
   constexpr int kG = Mx<D>::kGroups;
   const int token = ((n >> 2) & 1) * 8 + (n & 3), group = j & (kG - 1);
   DecodeLane4 la;
-  la.key_second = (n >> 3) != 0;
-  la.key = (token * kG + group) * 16;
-  la.key_scale = Mx<D>::kKeyScales + token * kG + group;
-  la.value_second = (j >> 1) != 0;
-  la.value = Mx<D>::kValues + (j & 1) * Mx<D>::kHalf + n * 16;
-  la.value_scale = Mx<D>::kValueScales + (j & 1) * Mx<D>::kHalfScales;
+  la.key = (n >> 3) * kPage + group * 256 + token * 16;
+  la.key_scale = (n >> 3) * kPage + Mx<D>::kKeyScales + token * kG + group;
+  la.value = (j >> 1) * kPage + Mx<D>::kValues + (j & 1) * Mx<D>::kHalf + n * 16;
+  la.value_scale = (j >> 1) * kPage + Mx<D>::kValueScales + (j & 1) * Mx<D>::kHalfScales;
   const int tok_lane = (j >> 1) * 16 + (j & 1) * 8;   // first of this lane's 8 tokens inside the pair
+  const CopyLane<D> cl = copy_lane<D>(lane);
+  char* const ring = smem + wave * kRing;
+  const unsigned lds_ring = lds_offset(ring);
 
   HfxItem it = items[t.cur];
   DecodeWave d = decode_wave(bt, it, wave);
-  PairRegs4<D> r0, r1;
-  if (d.pp < d.pe) decode_load4<D>(r0, pool, d.a0, d.a1, Hkv, d.g, la);
-  DecodeQuery4<D> qf = decode_query4<D>(a.q, it, d.g, Hq, G, n, j);
-
   for (;;) {
+    // The ring holds the pairs from the one at work on; page ids are fetched one pair ahead of the copies that need them.
+    int next = d.pp;                   // pair to be copied next
+    int n0 = d.a0, n1 = d.a1;          // its pages
+    int to = 0;                        // and its place in the ring
+    auto copy_pair = [&]() {
+      const unsigned long b0 = (unsigned)n0 * (unsigned)Hkv + (unsigned)d.g, b1 = (unsigned)n1 * (unsigned)Hkv + (unsigned)d.g;
+      raw_copy<D>(pool + b0 * Mx<D>::kBlock, cl, lds_ring + (unsigned)to);
+      raw_copy<D>(pool + b1 * Mx<D>::kBlock, cl, lds_ring + (unsigned)(to + kPage));
+      next += d.step;
+      to = to == kRing - 2 * kPage ? 0 : to + 2 * kPage;
+      n0 = constant(bt)[d.bt0 + min(next, d.last_page)];
+      n1 = constant(bt)[d.bt0 + min(next + 1, d.last_page)];
+    };
+#pragma unroll 1
+    for (int i = 0; i < kRingPairs - 1 && next < d.pe; ++i) copy_pair();
+    const DecodeQuery4<D> qf = decode_query4<D>(a.q, it, d.g, Hq, G, n, j);
     // the record of the next item and, if it is a decode item, this wavefront's share of it
     const HfxItem nx = items[t.nxt < n_items ? t.nxt : t.cur];
     const bool carry_on = t.nxt < n_items && nx.type == HFX_ITEM_DECODE;
     const DecodeWave dn = decode_wave(bt, nx, wave);
 
-    f32x4 o[D / 16];
+    DecodeState4<D> w;
 #pragma unroll
-    for (int b = 0; b < D / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = NEG_INF, l = 0.f;
-    const int step = d.step, pe = d.pe, tend = d.tend, g = d.g;
-    int pp = d.pp;
-    int a0 = d.a0, a1 = d.a1, b0 = d.b0, b1 = d.b1;
-    bool reserved = false;
-    int pending = 0;
-    // page ids are fetched one pair ahead of the loads that need them
-    while (pp < pe) {
-      if (!reserved && pp + 4 * step >= pe) {   // a few pairs before the end (thread 0 sits in the first wavefront, which always has pairs)
+    for (int b = 0; b < D / 16; ++b) w.o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    w.m = NEG_INF;
+    w.l = 0.f;
+    bool reserved = false, first = true;
+    int pending = 0, at = 0;
+    for (int pp = d.pp; pp < d.pe; pp += d.step) {
+      if (!reserved && pp + 4 * d.step >= d.pe) {   // a few pairs before the end (thread 0 sits in the first wavefront, which always has pairs)
         tickets_reserve(t, pending, ctrl);
         reserved = true;
       }
-      if (pp + step < pe) decode_load4<D>(r1, pool, b0, b1, Hkv, g, la);
-      if (pp + 2 * step < pe) {
-        a0 = decode_page(bt, d, pp + 2 * step);
-        a1 = decode_page(bt, d, pp + 2 * step + 1);
+      // this pair's copies have landed: those of the pairs behind it may be on their way
+      if (next < d.pe) {
+        __builtin_amdgcn_s_waitcnt(0xc07f);     // lgkmcnt(0): the pair before this one, whose place is copied into, has been read
+        copy_pair();
+        HFX_WAIT_VMCNT((kRingPairs - 1) * kCopies);
+      } else {
+        const int behind = (next - pp) - d.step;
+        if (behind == 2 * d.step) HFX_WAIT_VMCNT(2 * kCopies);
+        else if (behind == d.step) HFX_WAIT_VMCNT(kCopies);
+        else HFX_WAIT_VMCNT(0);
       }
-      {
-        const int nv = tend - (pp * HFX_PAGE + tok_lane);
-        if ((pp + 2) * HFX_PAGE <= tend) decode_compute4<D>(r0, qf, o, m, l, sl2, 8);
-        else decode_compute4<D>(r0, qf, o, m, l, sl2, nv);
-      }
-      pp += step;
-      if (pp >= pe) break;
-      if (pp + step < pe) decode_load4<D>(r0, pool, a0, a1, Hkv, g, la);
-      if (pp + 2 * step < pe) {
-        b0 = decode_page(bt, d, pp + 2 * step);
-        b1 = decode_page(bt, d, pp + 2 * step + 1);
-      }
-      {
-        const int nv = tend - (pp * HFX_PAGE + tok_lane);
-        if ((pp + 2) * HFX_PAGE <= tend) decode_compute4<D>(r1, qf, o, m, l, sl2, 8);
-        else decode_compute4<D>(r1, qf, o, m, l, sl2, nv);
-      }
-      pp += step;
+      asm volatile("" ::: "memory");
+      decode_pair4<D>(ring + at, la, qf, w, sl2, first, (pp + 2) * HFX_PAGE > d.tend, d.tend - (pp * HFX_PAGE + tok_lane));
+      asm volatile("" ::: "memory");
+      first = false;
+      at = at == kRing - 2 * kPage ? 0 : at + 2 * kPage;
     }
     tickets_publish(t, pending, s_tk, ctrl, H);
-    // both register sets and the query operand are free now: start on the next item
-    if (carry_on) {
-      if (dn.pp < dn.pe) decode_load4<D>(r0, pool, dn.a0, dn.a1, Hkv, dn.g, la);
-      qf = decode_query4<D>(a.q, nx, dn.g, Hq, G, n, j);
-    }
-    decode_store<D>(a, H, it, o, m, l, Hq, G, tid, wave, n, j, smem);
+    decode_store<D>(a, H, it, w.o, w.m, w.l, Hq, G, tid, wave, n, j, smem, kRing);
     __syncthreads();                  // frees the LDS partials; the ticket was published before the barrier in decode_store
     tickets_take(t, s_tk, n_items);
     if (!carry_on) break;
@@ -305,35 +367,17 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
 // ----------------------------------------------------------------------------------------------
 template <int D>
 struct Smem4 {
-  static constexpr int kRawPage = 16 * D + 256;        // key codes [group][16 keys][16 bytes], value codes, then the scales as in the block (the copy of them writes 256 bytes)
+  static constexpr int kRawPage = RawPage<D>::kBytes;
   static constexpr int kRawStep = 4 * kRawPage;
   static constexpr int kRawSteps = 3;
   static constexpr int kValuePage = 32 * D;            // [D / 32][32 dimensions][2 halves of 8 tokens] bf16, halves of rows 8-15 and 24-31 swapped
   static constexpr int kValueStep = 4 * kValuePage;
   static constexpr int kRing = kRawSteps * kRawStep;
-  static constexpr int kBytes = kRing + 2 * kValueStep > decode_part_bytes(D) ? kRing + 2 * kValueStep : decode_part_bytes(D);
-  static constexpr int kCopies = D == 128 ? 3 : 2;     // instructions that copy a page
+  static constexpr int kOut = kRing + 2 * kValueStep;  // result rows on their way out (prefill_store), 2 KB a wavefront
+  static constexpr int kPrefill = kOut + 4 * 2048, kDecode = 4 * 2 * kRingPairs * kRawPage;
+  static constexpr int kBytes = kPrefill > kDecode ? kPrefill : kDecode;
 };
 constexpr int kStepKeys = 64;
-
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// The block of one page: base (scalar), offsets of the lane's 16 bytes of keys, of values and 4 bytes of scales, LDS destination.
-template <int D>
-__device__ __forceinline__ void raw_copy(const char* base, unsigned keys, unsigned values, unsigned scales, unsigned lds) {
-  if constexpr (D == 128)
-    asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %3\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024\n\t"
-                 "global_load_lds_dword %2, %3 offset:2048"
-                 :: "v"(keys), "v"(values), "v"(scales), "s"(base), "s"(lds) : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dword %1, %2 offset:1024"
-                 :: "v"(keys), "v"(scales), "s"(base), "s"(lds) : "memory", "m0");
-}
-// 64 page ids, one a lane, out of a table (scalar base) at the lane's byte offset.
-__device__ __forceinline__ void ids_copy(const int* table, unsigned offset, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(offset), "s"(table), "s"(lds) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 
 template <int D>
 struct PrefillWave4 {
@@ -508,7 +552,7 @@ struct Widening {
 //   scores of the next step's first stage, values of the second stage likewise.
 template <int D>
 __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
-                             char* smem, char* o_stage, int* s_ids) {
+                             char* smem, int* s_ids) {
   typedef Smem4<D> L;
   constexpr int SK = HFX_STAGE_KEYS, S = D / 16;
   const int tid = threadIdx.x;
@@ -518,7 +562,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const int Hq = H->num_q_heads, Hkv = H->num_kv_heads;
   const int G = Hq / Hkv;
   const int n = lane & 31, j = lane >> 5;
-  char* stage = o_stage + wave * 2048;
+  char* stage = smem + Smem4<D>::kOut + wave * 2048;
   const float sl2 = __builtin_bit_cast(float, uniform(__builtin_bit_cast(int, H->softmax_scale * 1.4426950408889634f)));
   const int* __restrict__ bt = reinterpret_cast<const int*>(a.desc + H->off_bt);
   const char* pool = reinterpret_cast<const char*>(a.pool);
@@ -528,12 +572,9 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const int s_lane = (krow >> 4) * L::kRawPage + Mx<D>::kKeyScales + (krow & 15) * Mx<D>::kGroups;
   const int v_lane = (n * 2 + (j ^ ((n >> 3) & 1))) * 16;   // V^T rows 32b + n, keys 8j.. of a page
   char* const values = smem + L::kRing;
-  // copies: a page's keys change their order from [key][group] to [group][key]
-  constexpr int kG = Mx<D>::kGroups;
-  const unsigned c_keys = D == 128 || lane < 32 ? (unsigned)(((lane & 15) * kG + ((lane >> 4) & (kG - 1))) * 16) : (unsigned)lane * 16;
-  const unsigned c_values = (unsigned)lane * 16, c_scales = (unsigned)(lane & (D / 4 - 1)) * 4;
-  const unsigned lds_raw = (unsigned)uniform((int)((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * L::kRawPage));
-  // widening: this lane's value codes in the raw page (D = 128: at c_values too), their scales, and where its dimensions go
+  const CopyLane<D> cl = copy_lane<D>(lane);
+  const unsigned lds_raw = lds_offset(smem + wave * L::kRawPage);
+  // widening: this lane's value codes in the raw page (D = 128: at cl.values too), their scales, and where its dimensions go
   const int half = lane >> 5;
   const int w_codes = wave * L::kRawPage + Mx<D>::kValues, w_lane = lane * (D / 8);
   const int w_scales = wave * L::kRawPage + Mx<D>::kValueScales + (D == 128 ? (lane >> 4) * 16 : half * 16);
@@ -569,7 +610,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   };
   bool in_next = false;
   const int* const lots = s_ids + wave * 128;
-  const unsigned lds_lots = (unsigned)uniform((int)((unsigned)(uintptr_t)(__attribute__((address_space(3))) int*)s_ids + wave * 512));
+  const unsigned lds_lots = lds_offset(lots);
   int lot = 1, at = 0, end = 0, head = 0;              // the lot at hand: which half of the lots, next entry, end, kv-head
   int have2 = 0, head2 = 0;                            // entries and kv-head of the one behind it
   bool asked = false;                                  // since the last wait for everything
@@ -597,7 +638,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   // copies the next step, whose entry of the lot at hand is `page`, to ring offset `to`
   auto copy_one = [&](int page, int to) {
     const unsigned block = (unsigned)page * (unsigned)Hkv + (unsigned)head;
-    raw_copy<D>(pool + (unsigned long)block * Mx<D>::kBlock, c_keys, c_values, c_scales, lds_raw + (unsigned)to);
+    raw_copy<D>(pool + (unsigned long)block * Mx<D>::kBlock, cl, lds_raw + (unsigned)to);
     ++at;
   };
   // copies steps until `limit` are on their way, as far as they are known; lots that have been asked for have landed, unless `asked`
@@ -703,7 +744,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       if (whole) {
         --plain;
         const int page = lots[at];           // (read ahead of the waits)
-        HFX_WAIT_VMCNT(L::kCopies);
+        HFX_WAIT_VMCNT(RawPage<D>::kCopies);
         ring_barrier();
         copy_one(uniform(page), raw_g);
       } else {
@@ -714,7 +755,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
           asked = false;
           tickets_publish(t, reply, s_tk, ctrl, H);
         } else if (ahead == L::kRawSteps && !asked) {
-          HFX_WAIT_VMCNT(L::kCopies);
+          HFX_WAIT_VMCNT(RawPage<D>::kCopies);
         } else {
           HFX_WAIT_VMCNT(0);
           asked = false;
@@ -794,7 +835,6 @@ __global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(c
   a.out = out;
   __shared__ __attribute__((aligned(1024))) char smem[Smem4<D>::kBytes];
   __shared__ int s_tk[2];
-  __shared__ __attribute__((aligned(128))) char s_ostage[4 * 2048];      // result rows on their way out (prefill_store)
   __shared__ __attribute__((aligned(16))) int s_ids[4 * 128];            // page ids of steps to come (prefill_run4)
   const HfxHeader* H = &hdr;
   const HfxItem* items = reinterpret_cast<const HfxItem*>(a.desc + H->off_items);
@@ -802,7 +842,7 @@ __global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(c
   Tickets t = tickets_start(H, a.desc);
   while (t.cur < n_items) {
     if (items[t.cur].type == HFX_ITEM_DECODE) decode_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem);
-    else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ostage, s_ids);
+    else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ids);
   }
   queue_done(H, ctrl);
 }
