@@ -657,6 +657,12 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       ++ahead;
     }
   };
+  // Workgroups b and b + 256 share a CU, and where both have something to issue the older one goes first: left to that, the older half of a long step's
+  // workgroups ended at 710 us and the younger at 895.  So the younger one has the higher priority in two of three of its steps (in one of two, three of
+  // four and all: 816, 819 and 835 us; none: 838; two of three: 803).  Where prefill items do not fill two rounds, the older workgroups have the
+  // largest ones and rightly go first (64-wide heads, 488 prefill items: 41.5 us, 46.5 with turns).
+  const bool turns = gridDim.x == HFX_PLAN_WGS && blockIdx.x >= HFX_PLAN_WGS / 2 && H->n_prefill_items >= 2 * HFX_PLAN_WGS;
+  int turn = 0;
   PrefillWave4<D> w;
   HfxItem it;
   int kt, left, ctx_len;
@@ -734,6 +740,11 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       if (plain == 0 && ahead == L::kRawSteps && !asked && wave_end > 0 && kt + 3 * SK - 1 <= unmasked_upto)
         plain = uniform(min(min(left - 1, end - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1));
       const bool whole = plain > 0;
+      if (turns) {
+        if (turn == 0) __builtin_amdgcn_s_setprio(0);
+        if (turn == 1) __builtin_amdgcn_s_setprio(1);
+        turn = turn == 2 ? 0 : turn + 1;
+      }
       const char* const slot = values + value_g;
       value_g ^= L::kValueStep;
       char* const to = values + value_g + w_to;
@@ -820,6 +831,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     query_rows4<D>(w, qx);
     item_start(item_c);
   }
+  __builtin_amdgcn_s_setprio(0);
   __syncthreads();     // every wavefront is done with the ring before the LDS is used for anything else
 }
 
