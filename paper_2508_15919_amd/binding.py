@@ -38,8 +38,9 @@ class hfx_rope(ctypes.Structure):
     """Keeps the table it was made with alive (see make_rope)."""
     _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
-    def data_ptr(self):
-        return ctypes.addressof(self)
+    def __init__(self, *args):
+        super().__init__(*args)
+        self.address = ctypes.addressof(self)      # (asked for by every call)
 
 
 class hfx_latency_model(ctypes.Structure):
@@ -282,7 +283,7 @@ def hfx_copy_pages(shape: hfx_shape, src_pool, dst_pool, dst_num_pages: int, src
 
 def hfx_rope_append_kv(shape: hfx_shape, rope, q, q_stride: int, k_new, k_stride: int, v_new, v_stride: int, q_out, kv_pool, host_desc, device_desc,
                        stream=None) -> None:
-    rc = (_calls or _serving()).rope_append(shape, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, kv_pool, host_desc, device_desc, stream)
+    rc = (_calls or _serving()).rope_append(shape, rope.address if rope else None, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, kv_pool, host_desc, device_desc, stream)
     if rc != HFX_OK:
         raise HfxError(rc, "hfx_rope_append_kv")
 
@@ -297,7 +298,7 @@ def hfx_mx_pool_bytes(shape: hfx_shape) -> int:
 
 def hfx_rope_append_kv_mx(shape: hfx_shape, rope, q, q_stride: int, k_new, k_stride: int, v_new, v_stride: int, q_out, mx_pool, host_desc, device_desc,
                         stream=None) -> None:
-    rc = (_calls or _serving()).rope_append4(shape, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, mx_pool, host_desc, device_desc, stream)
+    rc = (_calls or _serving()).rope_append4(shape, rope.address if rope else None, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, mx_pool, host_desc, device_desc, stream)
     if rc != HFX_OK:
         raise HfxError(rc, "hfx_rope_append_kv_mx")
 

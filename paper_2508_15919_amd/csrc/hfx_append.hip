@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "hfx_desc.h"
 #include "hfx_device.h"
@@ -112,103 +113,140 @@ __device__ __forceinline__ unsigned block_top(const float* x) {
   return max(top, (unsigned)__builtin_amdgcn_mov_dpp((int)top, 0x4e, 0xf, 0xf, true));     // lane ^ 2
 }
 
-// One workgroup of 2 D threads per (run, kv-head), a run being the new tokens of one request in one page (at most 16).  A thread has one
+// Value codes, key scales and value scales of tokens [lo, hi) of a block, which lie in LDS as they lie there: four bytes at a time where the run has all
+// of their tokens, else those of its tokens.
+template <int D, int T>
+__device__ __forceinline__ void store_values_and_scales(char* blk, const uint8_t* s4, int tid, int lo, int hi) {
+  constexpr int kG = D / 32;
+  for (int i = tid; i < 9 * D / 4; i += T) {
+    const int b = 4 * i;
+    int first, per;              // token of the first byte; bytes that a token has in a row
+    if (b < 8 * D) {
+      first = b / Mx<D>::kHalf * 8 + (b & 7);
+      per = 1;
+    } else if (b < 8 * D + D / 2) {
+      first = (b - 8 * D) / kG;
+      per = kG;
+    } else {
+      const int r = b - 8 * D - D / 2;
+      first = r / Mx<D>::kHalfScales * 8 + (r & 15) / 2;
+      per = 2;
+    }
+    const int shift = per >> 1;  // 1, 2 or 4, and its logarithm
+    if (first >= lo && first + (3 >> shift) < hi) {
+      *reinterpret_cast<unsigned*>(blk + Mx<D>::kValues + b) = *reinterpret_cast<const unsigned*>(s4 + b);
+    } else if (first + (3 >> shift) >= lo && first < hi) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int token = first + (e >> shift);
+        if (token >= lo && token < hi) blk[Mx<D>::kValues + b + e] = (char)s4[b + e];
+      }
+    }
+  }
+}
+
+// Q-heads of a kv-head whose loads are in flight together.
+constexpr int kQueries = 4;
+
+// Which (run, kv-head) a workgroup takes.  Workgroups go to the dies by their index modulo 8; of 32 in a row a die takes four that follow each other, so
+// that the heads of a run, which share its angles and rows, meet in the same L2.
+__device__ __forceinline__ bool run_and_head(int n_runs, int heads, int& index, int& g) {
+  constexpr unsigned kDies = HFX_QUEUE_CLASSES, kRow = 4;
+  const unsigned all = (unsigned)heads * (unsigned)n_runs;
+  unsigned block = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+  if (block >= all) return false;
+  if (block < all / (kDies * kRow) * (kDies * kRow)) block = block / (kDies * kRow) * (kDies * kRow) + block % kDies * kRow + block / kDies % kRow;
+  index = (int)(block / (unsigned)heads);
+  g = (int)(block - (unsigned)index * (unsigned)heads);
+  return true;
+}
+
+// One workgroup of T threads per (run, kv-head), a run being the new tokens of one request in one page (at most 16).  A thread has one
 // 16-byte piece of one token: of its key row, of its value row, and of the rows of the q-heads that share the kv-head, all of which take the
-// same angles.
-template <int D, bool Four, bool Interleaved>
-__global__ __launch_bounds__(2 * D) void rope_append_kernel(const RopeAppend a) {
+// same angles and are asked for together.  T = 2 D: all 16 tokens at once; 64: a wavefront goes round, for steps whose runs are of a few tokens.
+template <int D, bool Four, bool Interleaved, int T>
+__global__ __launch_bounds__(T) void rope_append_kernel(const RopeAppend a) {
   constexpr int LD = D + 8;                       // LDS row stride in elements
+  constexpr int kTokens = T / (D / 8);            // at a time
   __shared__ __attribute__((aligned(16))) uint16_t sv[Four ? 1 : HFX_PAGE * LD];
   __shared__ __attribute__((aligned(16))) uint8_t s4[Four ? 9 * D : 16];      // value codes, key scales, value scales as in the block
-  const int Hkv = a.num_kv_heads, G = a.num_q_heads / Hkv;
-  const unsigned block = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
-  const int index = (int)(block / (unsigned)Hkv), g = (int)(block - (unsigned)index * Hkv), tid = threadIdx.x;
-  if (index >= a.n_runs) return;
+  const int Hkv = a.num_kv_heads, G = a.num_q_heads / Hkv, tid = threadIdx.x;
+  int index, g;
+  if (!run_and_head(a.n_runs, Hkv, index, g)) return;
   const HfxRun run = a.runs[index];
-  const int tok = tid / (D / 8), piece = tid % (D / 8), lane = tid & 63;
-  const bool live = tok < run.n;
+  const int position = a.rot > 0 ? a.run_pos[index] : 0;
+  const int piece = tid % (D / 8), lane = tid & 63;
   const bool any = a.rot > 0;
-  Turn t;
-  if (any) t = turn_of<Interleaved>(a.cos_sin + (long)(a.run_pos[index] + min(tok, run.n - 1)) * a.rot, a.rot, piece, lane);
-  const long row = (long)run.row0 + tok;
-  u32x4 kv = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
-  if (live) {
-    kv = *reinterpret_cast<const u32x4*>(a.k + row * a.k_stride + g * D + piece * 8);
-    vv = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + g * D + piece * 8);
-  }
-  if (a.q) {
-    for (int h = g * G; h < (g + 1) * G; ++h) {
-      u32x4 qv = {0, 0, 0, 0};
-      if (live) qv = *reinterpret_cast<const u32x4*>(a.q + row * a.q_stride + h * D + piece * 8);
-      float y[8];
-      turn<Interleaved>(t, any, qv, y);
-      if (live) *reinterpret_cast<u32x4*>(a.q_out + (row * a.num_q_heads + h) * D + piece * 8) = narrow(y);
-    }
-  }
-  float y[8];
-  turn<Interleaved>(t, any, kv, y);
-  const int slot = run.slot0 + tok;
-  if constexpr (!Four) {
-    uint16_t* kblk = reinterpret_cast<uint16_t*>(a.pool) + (((long)run.page * Hkv + g) * 2) * (16L * D);
-    if (live) {
-      *reinterpret_cast<u32x4*>(kblk + ((piece >> 1) * HFX_PAGE + slot) * 16 + (piece & 1) * 8) = any ? narrow(y) : kv;
-      *reinterpret_cast<u32x4*>(sv + slot * LD + piece * 8) = vv;
-    }
-    __syncthreads();
-    store_value_columns<D>(kblk + 16L * D, sv, LD, tid, run.slot0, run.n);
-  } else {
-    constexpr int kG = D / 32;
-    char* blk = reinterpret_cast<char*>(a.pool) + ((long)run.page * Hkv + g) * Mx<D>::kBlock;
-    const int group = piece >> 2, part = piece & 3;
-    const unsigned ke = scale_byte(block_top(y));
-    const unsigned kc = to_fp4(y, ke);
-    float x[8];
-    widen(vv, x);
-    const unsigned ve = scale_byte(block_top(x));
-    const unsigned vc = to_fp4(x, ve);
-    // a byte of value codes holds dimensions i and i + 16: lanes part and part ^ 2 join theirs, each for four of the eight
-    const unsigned other = (unsigned)__builtin_amdgcn_mov_dpp((int)vc, 0x4e, 0xf, 0xf, true);
-    const unsigned low = part < 2 ? vc : other >> 16, high = part < 2 ? other : vc >> 16;
-    if (live) {
-      *reinterpret_cast<unsigned*>(blk + (slot * kG + group) * 16 + part * 4) = kc;
-      const int half = slot >> 3, at = slot & 7, tp = group >> 1, w = group & 1;
-      const int i0 = 8 * (part & 1) + (part < 2 ? 0 : 4);
+  uint16_t* const kblk = reinterpret_cast<uint16_t*>(a.pool) + (((long)run.page * Hkv + g) * 2) * (16L * D);
+  char* const blk = reinterpret_cast<char*>(a.pool) + ((long)run.page * Hkv + g) * Mx<D>::kBlock;
+  for (int tok = tid / (D / 8); tok < HFX_PAGE; tok += kTokens) {
+    if (kTokens < HFX_PAGE && uniform(tok - tid / (D / 8)) >= run.n) break;
+    const bool live = tok < run.n;
+    // pieces without a token read the run's last one and are not stored
+    const int own = min(tok, run.n - 1);
+    const long row = (long)run.row0 + own;
+    Turn t;
+    if (any) t = turn_of<Interleaved>(a.cos_sin + (long)(position + own) * a.rot, a.rot, piece, lane);
+    const u32x4 kv = *reinterpret_cast<const u32x4*>(a.k + row * a.k_stride + g * D + piece * 8);
+    const u32x4 vv = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + g * D + piece * 8);
+    u32x4 qv[kQueries];
+    auto query_loads = [&](int h0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        s4[half * Mx<D>::kHalf + ((tp * 16 + i0 + i) * 2 + w) * 8 + at] = (uint8_t)((low >> (4 * i) & 15u) | (high >> (4 * i) & 15u) << 4);
-      if (part == 0) {
-        s4[8 * D + slot * kG + group] = (uint8_t)ke;
-        s4[8 * D + D / 2 + half * Mx<D>::kHalfScales + (tp * 8 + at) * 2 + w] = (uint8_t)ve;
+      for (int i = 0; i < kQueries; ++i)
+        qv[i] = *reinterpret_cast<const u32x4*>(a.q + row * a.q_stride + (g * G + min(h0 + i, G - 1)) * D + piece * 8);
+    };
+    if (a.q) query_loads(0);
+    float y[8];
+    turn<Interleaved>(t, any, kv, y);
+    const int slot = run.slot0 + tok;
+    if constexpr (!Four) {
+      if (live) {
+        *reinterpret_cast<u32x4*>(kblk + ((piece >> 1) * HFX_PAGE + slot) * 16 + (piece & 1) * 8) = any ? narrow(y) : kv;
+        *reinterpret_cast<u32x4*>(sv + slot * LD + piece * 8) = vv;
       }
-    }
-    __syncthreads();
-    // four bytes at a time where the run has all of their tokens, else those of its tokens
-    for (int i = tid; i < 9 * D / 4; i += 2 * D) {
-      const int b = 4 * i;
-      int first, step;          // token of byte b, and 4 / how many bytes a token has in a row
-      if (b < 8 * D) {
-        first = b / Mx<D>::kHalf * 8 + (b & 7);
-        step = 1;
-      } else if (b < 8 * D + D / 2) {
-        first = (b - 8 * D) / kG;
-        step = -kG;
-      } else {
-        const int r = b - 8 * D - D / 2;
-        first = r / Mx<D>::kHalfScales * 8 + (r & 15) / 2;
-        step = -2;
-      }
-      const int last = step > 0 ? first + 3 : first + 3 / -step;
-      const int lo = run.slot0, hi = run.slot0 + run.n;
-      if (first >= lo && last < hi) {
-        *reinterpret_cast<unsigned*>(blk + Mx<D>::kValues + b) = *reinterpret_cast<const unsigned*>(s4 + b);
-      } else if (last >= lo && first < hi) {
+    } else {
+      constexpr int kG = D / 32;
+      const int group = piece >> 2, part = piece & 3;
+      const unsigned ke = scale_byte(block_top(y));
+      const unsigned kc = to_fp4(y, ke);
+      float x[8];
+      widen(vv, x);
+      const unsigned ve = scale_byte(block_top(x));
+      const unsigned vc = to_fp4(x, ve);
+      // a byte of value codes holds dimensions i and i + 16: lanes part and part ^ 2 join theirs, each for four of the eight
+      const unsigned other = (unsigned)__builtin_amdgcn_mov_dpp((int)vc, 0x4e, 0xf, 0xf, true);
+      const unsigned low = part < 2 ? vc : other >> 16, high = part < 2 ? other : vc >> 16;
+      if (live) {
+        *reinterpret_cast<unsigned*>(blk + (slot * kG + group) * 16 + part * 4) = kc;
+        const int half = slot >> 3, at = slot & 7, tp = group >> 1, w = group & 1;
+        const int i0 = 8 * (part & 1) + (part < 2 ? 0 : 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int token = step > 0 ? first + e : first + e / -step;
-          if (token >= lo && token < hi) blk[Mx<D>::kValues + b + e] = (char)s4[b + e];
+        for (int i = 0; i < 4; ++i)
+          s4[half * Mx<D>::kHalf + ((tp * 16 + i0 + i) * 2 + w) * 8 + at] = (uint8_t)((low >> (4 * i) & 15u) | (high >> (4 * i) & 15u) << 4);
+        if (part == 0) {
+          s4[8 * D + slot * kG + group] = (uint8_t)ke;
+          s4[8 * D + D / 2 + half * Mx<D>::kHalfScales + (tp * 8 + at) * 2 + w] = (uint8_t)ve;
         }
       }
     }
+    if (a.q) {
+      for (int h0 = 0;;) {
+#pragma unroll
+        for (int i = 0; i < kQueries; ++i) {
+          turn<Interleaved>(t, any, qv[i], y);
+          if (live && h0 + i < G) *reinterpret_cast<u32x4*>(a.q_out + (row * a.num_q_heads + g * G + h0 + i) * D + piece * 8) = any ? narrow(y) : qv[i];
+        }
+        h0 += kQueries;
+        if (h0 >= G) break;
+        query_loads(h0);
+      }
+    }
+  }
+  __syncthreads();
+  if constexpr (!Four) {
+    for (int i = tid; i < 2 * D; i += T) store_value_columns<D>(kblk + 16L * D, sv, LD, i, run.slot0, run.n);
+  } else {
+    store_values_and_scales<D, T>(blk, s4, tid, run.slot0, run.slot0 + run.n);
   }
 }
 
@@ -218,17 +256,17 @@ __global__ __launch_bounds__(2 * D) void read_new_kv_mx_kernel(const HfxRun* __r
                                                              uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out) {
   __shared__ __attribute__((aligned(16))) uint8_t s4[9 * D];
   constexpr int kG = D / 32;
-  const unsigned block = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
-  const int index = (int)(block / (unsigned)Hkv), g = (int)(block - (unsigned)index * Hkv), tid = threadIdx.x;
-  if (index >= n_runs) return;
+  int index, g;
+  if (!run_and_head(n_runs, Hkv, index, g)) return;
+  const int tid = threadIdx.x;
   const HfxRun run = runs[index];
   const char* blk = pool + ((long)run.page * Hkv + g) * Mx<D>::kBlock;
-  for (int i = tid; i < 9 * D / 4; i += 2 * D) *reinterpret_cast<unsigned*>(s4 + 4 * i) = *reinterpret_cast<const unsigned*>(blk + Mx<D>::kValues + 4 * i);
-  __syncthreads();
   const int tok = tid / (D / 8), piece = tid % (D / 8);
-  if (tok >= run.n) return;
-  const int slot = run.slot0 + tok, group = piece >> 2, part = piece & 3;
+  const int slot = run.slot0 + min(tok, run.n - 1), group = piece >> 2, part = piece & 3;
   const unsigned kc = *reinterpret_cast<const unsigned*>(blk + (slot * kG + group) * 16 + part * 4);
+  for (int i = tid; i < 9 * D / 16; i += 2 * D) *reinterpret_cast<u32x4*>(s4 + 16 * i) = *reinterpret_cast<const u32x4*>(blk + Mx<D>::kValues + 16 * i);
+  __syncthreads();
+  if (tok >= run.n) return;
   const int half = slot >> 3, at = slot & 7, tp = group >> 1, w = group & 1;
   unsigned vc = 0;
 #pragma unroll
@@ -256,11 +294,17 @@ hipError_t launch_rope_append(const HfxHeader& h, const void* desc, RopeAppend a
   a.n_runs = h.n_runs;
   a.num_q_heads = h.num_q_heads;
   a.num_kv_heads = h.num_kv_heads;
-  const unsigned threads = 2u * (unsigned)h.head_dim;
-  void (*const kernels[])(RopeAppend) = {rope_append_kernel<64, false, false>,  rope_append_kernel<64, false, true>,  rope_append_kernel<64, true, false>,
-                                         rope_append_kernel<64, true, true>,    rope_append_kernel<128, false, false>, rope_append_kernel<128, false, true>,
-                                         rope_append_kernel<128, true, false>,  rope_append_kernel<128, true, true>};
-  return launch(kernels[(h.head_dim == 128 ? 4 : 0) + (four ? 2 : 0) + (a.interleaved ? 1 : 0)], run_grid(h), threads, stream, a);
+  // Runs of at most 4 tokens on average (decodes, chunks of a few rows) go to single wavefronts.
+  const bool few = (long)h.total_q <= 4l * h.n_runs;
+  auto pick = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    void (*const kernels[])(RopeAppend) = {rope_append_kernel<D, false, false, 2 * D>, rope_append_kernel<D, false, true, 2 * D>,
+                                           rope_append_kernel<D, true, false, 2 * D>,  rope_append_kernel<D, true, true, 2 * D>,
+                                           rope_append_kernel<D, false, false, 64>,    rope_append_kernel<D, false, true, 64>,
+                                           rope_append_kernel<D, true, false, 64>,     rope_append_kernel<D, true, true, 64>};
+    return launch(kernels[(few ? 4 : 0) + (four ? 2 : 0) + (a.interleaved ? 1 : 0)], run_grid(h), few ? 64u : 2u * D, stream, a);
+  };
+  return h.head_dim == 128 ? pick(std::integral_constant<int, 128>()) : pick(std::integral_constant<int, 64>());
 }
 
 hipError_t launch_read_new_kv_mx(const HfxHeader& h, const void* desc, const void* pool, void* k_out, void* v_out, hipStream_t stream) {
