@@ -736,30 +736,35 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       settle_weights<D>(w, s, pb, wt.sum(), sl2);
     };
     int plain = 0;        // steps ahead that every row of the wavefront sees whole and whose copies are in the lot at hand and in time
+    bool whole = false;   // the present step is one
     for (; left > 0; --left) {
-      if (plain == 0 && ahead == L::kRawSteps && !asked && wave_end > 0 && kt + 3 * SK - 1 <= unmasked_upto)
-        plain = uniform(min(min(left - 1, end - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1));
-      const bool whole = plain > 0;
-      if (turns) {
-        if (turn == 0) __builtin_amdgcn_s_setprio(0);
-        if (turn == 1) __builtin_amdgcn_s_setprio(1);
-        turn = turn == 2 ? 0 : turn + 1;
-      }
       const char* const slot = values + value_g;
       value_g ^= L::kValueStep;
       char* const to = values + value_g + w_to;
       const int raw_next = raw_slot(1);
       const char* const raw = smem + raw_next;
       // Synchronisation point: the values of this step are widened, the next one's raw pages have landed, and nobody reads the slots any more that are
-      // filled next.  In the item's last step the next ticket is asked for and published (and what comes after the item is multiplied for nothing).
-      if (whole) {
+      // filled next.
+      if (plain == 0) {
+        whole = false;
+        if (ahead == L::kRawSteps && !asked && wave_end > 0 && kt + 3 * SK - 1 <= unmasked_upto) {
+          plain = uniform(min(min(left - 1, end - at), (int)((unsigned)(unmasked_upto - kt - 3 * SK + 1) / kStepKeys) + 1));
+          whole = plain > 0;
+        }
+      }
+      if (__builtin_expect(whole, 1)) {
         --plain;
         const int page = lots[at];           // (read ahead of the waits)
         HFX_WAIT_VMCNT(RawPage<D>::kCopies);
         ring_barrier();
         copy_one(uniform(page), raw_g);
+        if (turns) {
+          if (turn == 0) __builtin_amdgcn_s_setprio(0);
+          if (turn == 1) __builtin_amdgcn_s_setprio(1);
+          turn = turn == 2 ? 0 : turn + 1;
+        }
       } else {
-        if (left == 1) {
+        if (left == 1) {                     // the next ticket is asked for and published (and what comes after the item is multiplied for nothing)
           int reply = 0;
           tickets_reserve(t, reply, ctrl);
           HFX_WAIT_VMCNT(0);
@@ -772,11 +777,10 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
           asked = false;
         }
         ring_barrier();
-        wide = ahead > 1 ? 2 : 1;            // the next step's pages have landed (copies issued now have not); if not, what is widened below is nothing yet
+        wide = ahead > 1 ? 1 : 0;            // whether the next step's pages have landed (copies issued now have not); if not, what is widened below is nothing yet
         feed(1 + L::kRawSteps);
         ask();
         --ahead;
-        --wide;
       }
       raw_g = raw_next;
       Widening<D> wd;
