@@ -355,8 +355,10 @@ hfx_status hfx_read_new_kv_mx(const hfx_shape* shape, const void* mx_pool, const
                             void* k_out, void* v_out, void* stream);
 
 /*
- * hfx_mixed_paged_attention over a 4-bit pool: the same result as over a bf16 pool that holds the values that this one stands for, to rounding (scores
- * against the bf16 queries and the weighted sum accumulate in fp32, softmax weights are rounded to bf16).  Same descriptor, workspace, arguments and errors.
+ * hfx_mixed_paged_attention over a 4-bit pool: the same result as over a bf16 pool that holds the values that this one stands for, to rounding.  Scores and
+ * the weighted sum accumulate in fp32, and softmax weights are rounded to bf16.  A query value enters as the sum of two 6-bit numbers with scales per 32
+ * dimensions: exactly, where it is at least 1/4 of the largest of the 32, and to 2^-10 of that one otherwise (half of what bf16 rounds it by itself).
+ * Same descriptor, workspace, arguments and errors.
  */
 hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, const void* mx_pool, const void* host_desc,
                                          void* device_desc, void* workspace, size_t workspace_bytes, void* out,

@@ -23,21 +23,22 @@ typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef __bf16 bf16x32 __attribute__((ext_vector_type(32)));
 
 // Operand formats of the scaled matrix instructions.
-constexpr int kFp6 = 2, kFp4 = 4;
+constexpr int kE2M3 = 2, kE3M2 = 3, kE2M1 = 4;
 
 // The 4-bit operand takes four registers of the eight that the builtins ask for, the 6-bit one six.
 __device__ __forceinline__ i32x8 fp4_operand(const u32x4& c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
 __device__ __forceinline__ i32x8 fp6_operand(const u32x6& c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], (int)c[4], (int)c[5], 0, 0}; }
 
-// 32 query values as the sum of two sets of 6-bit numbers with scales 2^(e - 127) and 2^(e - 4 - 127).  e brings the largest magnitude into [3.875, 7.75),
-// where the nearest number of E2M3 (4 significant bits, up to 7.5, steps of 1/8 below 2) is at most 1/4 away; a remainder is at most 4 of its own
-// scale's units.  A bf16 value has 8 significant bits: from 1/8 of the largest magnitude's power of two up the two numbers hold all of them; smaller values
-// are off by at most 2^-8 units, 2^-10 of the largest, half of what bf16 itself rounds that one by.
+// 32 query values as the sum of two sets of 6-bit numbers with scales 2^(e - 127) and 2^(e - 6 - 127).  e brings the largest magnitude into [3.875, 7.75),
+// where the nearest number of E2M3 (4 significant bits, up to 7.5, steps of 1/8 below 2) is at most 1/4 away.  A bf16 value has 8 significant bits: from 1
+// up the remainder is at most eight of its last places, which the 3 significant bits of E3M2 hold, so the two numbers are the value; a smaller value's
+// remainder is at most 1/16 and rounds by at most 2^-8, 2^-10 of the largest, half of what bf16 itself rounds that one by.  (Remainders as E2M3, whose
+// steps do not get finer with the remainder, put results 2.5e-3 off in all at 65536 keys, these 2.4e-3; the weights and the result in bf16 alone are 2.35e-3.)
 struct Query6 {
   u32x6 first, rest;
   unsigned scale;          // bytes: of first, of rest
 };
-constexpr unsigned kRestScale = 4;
+constexpr unsigned kRestScale = 6;
 __device__ __forceinline__ Query6 split_query(const bf16x8* q) {
   unsigned top = 0;
 #pragma unroll
@@ -46,7 +47,7 @@ __device__ __forceinline__ Query6 split_query(const bf16x8* q) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = max(top, max(u[w] & 0x7fff0000u, u[w] << 16 & 0x7fff0000u));
   }
-  const unsigned e = (unsigned)max((int)((top + 0x80000u) >> 23) - 2, 5);
+  const unsigned e = (unsigned)max((int)((top + 0x80000u) >> 23) - 2, (int)kRestScale + 1);
   const float scale = __builtin_bit_cast(float, e << 23), rest_scale = __builtin_bit_cast(float, (e - kRestScale) << 23);
   bf16x32 x, r;
 #pragma unroll
@@ -56,7 +57,7 @@ __device__ __forceinline__ Query6 split_query(const bf16x8* q) {
   const f32x32 f = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(t.first, scale);
 #pragma unroll
   for (int i = 0; i < 32; ++i) r[i] = (__bf16)((float)x[i] - f[i]);          // (exact)
-  t.rest = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(r, rest_scale);
+  t.rest = __builtin_amdgcn_cvt_scalef32_pk32_bf6_bf16(r, rest_scale);
   t.scale = e | (e - kRestScale) << 8;
   return t;
 }
@@ -138,7 +139,7 @@ __device__ __forceinline__ void ids_copy(const int* table, unsigned offset, unsi
 // wavefront takes 4352 bytes (D = 128), by direct-to-LDS copies into a ring of its own, three pairs ahead of their use: 104 KB in flight on a CU
 // without a register.
 //   S^T[token][head]: 16x16x128, a lane has 32 dimensions of one key (a group) with their scale; D = 64: lanes of the upper half have the
-//                     same keys again, and the queries' remainders there, so that one instruction does both products.
+//                     same keys again, against zeros.
 //   O^T[d][head]    : 16x16x32 bf16, a lane has eight tokens of dimension n of each tile.
 // The softmax is that of the prefill items: weights against the maximum of the item's first pair, which is raised only when a lane's eight weights sum to
 // more than 2^8, so that the common pair needs no maximum, no exchange between lanes and no rescaling.
@@ -152,16 +153,15 @@ struct DecodeLane4 {
 
 template <int D>
 struct DecodeQuery4 {
-  u32x6 q[D / 64];        // D = 128: first numbers, remainders; D = 64: both in one
-  unsigned scale;         // bytes: of q[0], of q[1]
+  u32x6 q[2];             // first numbers, remainders
+  unsigned scale;         // bytes: of either
 };
 
 template <int D>
 __device__ __forceinline__ f32x4 decode_scores4(const u32x4& k, unsigned ks, const DecodeQuery4<D>& q) {
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[0]), s, kFp4, kFp6, 0, (int)ks, 0, (int)q.scale);
-  if constexpr (D == 128)
-    s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[1]), s, kFp4, kFp6, 0, (int)ks, 1, (int)q.scale);
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[0]), s, kE2M1, kE2M3, 0, (int)ks, 0, (int)q.scale);
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[1]), s, kE2M1, kE3M2, 0, (int)ks, 1, (int)q.scale);
   return s;
 }
 
@@ -242,26 +242,19 @@ __device__ __forceinline__ void decode_pair4(const char* ring, const DecodeLane4
   }
 }
 
-// Query operand of a kv-head's q-heads (column n), zero past the group: lane group j has 32 dimensions, group j (D = 128), or group j & 1 (D = 64), whose
-// first numbers go to the lower half of the lanes and whose remainders to the upper.
+// Query operands of a kv-head's q-heads (column n), zero past the group: lane group j has 32 dimensions, 32j .. 32j + 31, or zeros past the head's.
 template <int D>
 __device__ __forceinline__ DecodeQuery4<D> decode_query4(const __bf16* q, const HfxItem& item, int g, int Hq, int G, int n, int j) {
   const int hh = n < G ? n : G - 1;
-  const __bf16* row = q + ((long)item.rq.q_start * Hq + g * G + hh) * D + (j & (D / 32 - 1)) * 32;
+  const __bf16* row = q + ((long)item.rq.q_start * Hq + g * G + hh) * D + (j & (Mx<D>::kGroups - 1)) * 32;
   bf16x8 x[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = keep_first(ld16(row + i * 8), n < G ? 8 : 0);
+  for (int i = 0; i < 4; ++i) x[i] = keep_first(ld16(row + i * 8), n < G && j < Mx<D>::kGroups ? 8 : 0);
   const Query6 t = split_query(x);
   DecodeQuery4<D> r;
-  if constexpr (D == 128) {
-    r.q[0] = t.first;
-    r.q[1] = t.rest;
-    r.scale = t.scale;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 6; ++i) r.q[0][i] = j < 2 ? t.first[i] : t.rest[i];
-    r.scale = j < 2 ? t.scale : t.scale >> 8;
-  }
+  r.q[0] = t.first;
+  r.q[1] = t.rest;
+  r.scale = t.scale;
   return r;
 }
 
@@ -413,10 +406,10 @@ template <int D>
 __device__ __forceinline__ void score_product(const PrefillWave4<D>& w, const Keys4<D>& k, int i, f32x16& s) {
   const i32x8 a = fp4_operand(k.k[i / 2]), b = fp6_operand(w.q[i / 2][i % 2]);
   const int ks = (int)k.scale, qs = (int)w.qs;
-  if (i == 0) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 0, ks, 0, qs);
-  if (i == 1) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 0, ks, 1, qs);
-  if (i == 2) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 2, ks, 2, qs);
-  if (i == 3) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kFp4, kFp6, 2, ks, 3, qs);
+  if (i == 0) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE2M3, 0, ks, 0, qs);
+  if (i == 1) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE3M2, 0, ks, 1, qs);
+  if (i == 2) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE2M3, 2, ks, 2, qs);
+  if (i == 3) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE3M2, 2, ks, 3, qs);
   asm volatile("" : "+v"(s));
 }
 
