@@ -148,10 +148,10 @@ __device__ __forceinline__ void store_values_and_scales(char* blk, const uint8_t
 // Q-heads of a kv-head whose loads are in flight together.
 constexpr int kQueries = 4;
 
-// Which (run, kv-head) a workgroup takes.  Workgroups go to the dies by their index modulo 8; of 32 in a row a die takes four that follow each other, so
-// that the heads of a run, which share its angles and rows, meet in the same L2.
+// Which (run, kv-head) a workgroup takes.  Workgroups go to the dies by their index modulo 8; of 128 in a row a die takes 16 that follow each other, so
+// that the heads of a run, which share its angles and rows, meet in the same L2 (8224 rows of 32 q-heads: 32.4 us; 34.2 with four in a row, 39.5 with one).
 __device__ __forceinline__ bool run_and_head(int n_runs, int heads, int& index, int& g) {
-  constexpr unsigned kDies = HFX_QUEUE_CLASSES, kRow = 4;
+  constexpr unsigned kDies = HFX_QUEUE_CLASSES, kRow = 16;
   const unsigned all = (unsigned)heads * (unsigned)n_runs;
   unsigned block = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
   if (block >= all) return false;
@@ -161,48 +161,84 @@ __device__ __forceinline__ bool run_and_head(int n_runs, int heads, int& index, 
   return true;
 }
 
-// One workgroup of T threads per (run, kv-head), a run being the new tokens of one request in one page (at most 16).  A thread has one
-// 16-byte piece of one token: of its key row, of its value row, and of the rows of the q-heads that share the kv-head, all of which take the
-// same angles and are asked for together.  T = 2 D: all 16 tokens at once; 64: a wavefront goes round, for steps whose runs are of a few tokens.
+// One workgroup per (run, kv-head) and part, a run being the new tokens of one request in one page (at most 16): the key and value rows of the
+// head are one part, the rows of the q-heads that share it the other.  A thread has one 16-byte piece of one token, of both rows or of as many q-heads as
+// its loads may be in flight for.  T = 2 D threads have all 16 tokens at once, and pass the values through LDS, where a page has the tokens of a dimension
+// side by side.  T = 64, for steps whose runs are of a few tokens: a wavefront goes round, values go to their bytes straight from the registers, and the
+// two parts are the two wavefronts of one workgroup.
+// Bound by memory where there is much to do (32 q-heads, 8 kv-heads, 128 wide, 8224 rows in long chunks: 206 MB in 32.4 us, 6.4 TB/s; 4-bit pages:
+// 177 MB in 29.6 us), and by the chain of its loads (record of the run, then rows and angles) where there is little (four decodes: 3.6 us, of which an empty kernel
+// takes 1.5; 256 decodes into 4-bit pages 5.6).  With keys, values and queries in turn in one wavefront those were 6.0 and 7.5 us.
 template <int D, bool Four, bool Interleaved, int T>
-__global__ __launch_bounds__(T) void rope_append_kernel(const RopeAppend a) {
+__global__ __launch_bounds__(T == 64 ? 128 : T) void rope_append_kernel(const RopeAppend a) {
+  constexpr bool kFew = T == 64;
   constexpr int LD = D + 8;                       // LDS row stride in elements
   constexpr int kTokens = T / (D / 8);            // at a time
-  __shared__ __attribute__((aligned(16))) uint16_t sv[Four ? 1 : HFX_PAGE * LD];
-  __shared__ __attribute__((aligned(16))) uint8_t s4[Four ? 9 * D : 16];      // value codes, key scales, value scales as in the block
-  const int Hkv = a.num_kv_heads, G = a.num_q_heads / Hkv, tid = threadIdx.x;
-  int index, g;
-  if (!run_and_head(a.n_runs, Hkv, index, g)) return;
+  __shared__ __attribute__((aligned(16))) uint16_t sv[Four || kFew ? 1 : HFX_PAGE * LD];
+  __shared__ __attribute__((aligned(16))) uint8_t s4[Four && !kFew ? 9 * D : 16];      // value codes, key scales, value scales as in the block
+  const int Hkv = a.num_kv_heads, G = a.num_q_heads / Hkv, tid = threadIdx.x % T;
+  const int parts = a.q ? 2 : 1;
+  int index, g, part_of_head;
+  if constexpr (kFew) {
+    if (!run_and_head(a.n_runs, Hkv, index, g)) return;
+    part_of_head = uniform((int)threadIdx.x / T);
+  } else {
+    if (!run_and_head(a.n_runs, parts * Hkv, index, g)) return;
+    part_of_head = g & (parts - 1);
+    g = parts == 2 ? g >> 1 : g;
+  }
   const HfxRun run = a.runs[index];
-  const int position = a.rot > 0 ? a.run_pos[index] : 0;
-  const int piece = tid % (D / 8), lane = tid & 63;
   const bool any = a.rot > 0;
+  const int position = any ? a.run_pos[index] : 0;
+  const int piece = tid % (D / 8), lane = tid & 63;
+  if (part_of_head == 1) {
+    for (int tok = tid / (D / 8); tok < HFX_PAGE; tok += kTokens) {
+      if (kTokens < HFX_PAGE && uniform(tok - tid / (D / 8)) >= run.n) break;
+      const int own = min(tok, run.n - 1);         // pieces without a token read the run's last one and are not stored
+      const long row = (long)run.row0 + own;
+      Turn t;
+      if (any) t = turn_of<Interleaved>(a.cos_sin + (long)(position + own) * a.rot, a.rot, piece, lane);
+      const uint16_t* const from = a.q + row * a.q_stride + g * G * D + piece * 8;
+      uint16_t* const to = a.q_out + (row * a.num_q_heads + g * G) * D + piece * 8;
+      for (int h0 = 0; h0 < G; h0 += kQueries) {
+        u32x4 qv[kQueries];
+#pragma unroll
+        for (int i = 0; i < kQueries; ++i) qv[i] = *reinterpret_cast<const u32x4*>(from + min(h0 + i, G - 1) * D);
+#pragma unroll
+        for (int i = 0; i < kQueries; ++i) {
+          if (h0 + i >= G) break;
+          float y[8];
+          turn<Interleaved>(t, any, qv[i], y);
+          if (tok < run.n) *reinterpret_cast<u32x4*>(to + (h0 + i) * D) = any ? narrow(y) : qv[i];
+        }
+      }
+    }
+    return;
+  }
   uint16_t* const kblk = reinterpret_cast<uint16_t*>(a.pool) + (((long)run.page * Hkv + g) * 2) * (16L * D);
   char* const blk = reinterpret_cast<char*>(a.pool) + ((long)run.page * Hkv + g) * Mx<D>::kBlock;
   for (int tok = tid / (D / 8); tok < HFX_PAGE; tok += kTokens) {
     if (kTokens < HFX_PAGE && uniform(tok - tid / (D / 8)) >= run.n) break;
     const bool live = tok < run.n;
-    // pieces without a token read the run's last one and are not stored
     const int own = min(tok, run.n - 1);
     const long row = (long)run.row0 + own;
     Turn t;
     if (any) t = turn_of<Interleaved>(a.cos_sin + (long)(position + own) * a.rot, a.rot, piece, lane);
     const u32x4 kv = *reinterpret_cast<const u32x4*>(a.k + row * a.k_stride + g * D + piece * 8);
     const u32x4 vv = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + g * D + piece * 8);
-    u32x4 qv[kQueries];
-    auto query_loads = [&](int h0) {
-#pragma unroll
-      for (int i = 0; i < kQueries; ++i)
-        qv[i] = *reinterpret_cast<const u32x4*>(a.q + row * a.q_stride + (g * G + min(h0 + i, G - 1)) * D + piece * 8);
-    };
-    if (a.q) query_loads(0);
     float y[8];
     turn<Interleaved>(t, any, kv, y);
     const int slot = run.slot0 + tok;
     if constexpr (!Four) {
       if (live) {
         *reinterpret_cast<u32x4*>(kblk + ((piece >> 1) * HFX_PAGE + slot) * 16 + (piece & 1) * 8) = any ? narrow(y) : kv;
-        *reinterpret_cast<u32x4*>(sv + slot * LD + piece * 8) = vv;
+        if constexpr (kFew) {
+          uint16_t* const to = kblk + 16L * D + piece * 8 * HFX_PAGE + slot;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) to[e * HFX_PAGE] = (uint16_t)(vv[e >> 1] >> (16 * (e & 1)));
+        } else {
+          *reinterpret_cast<u32x4*>(sv + slot * LD + piece * 8) = vv;
+        }
       }
     } else {
       constexpr int kG = D / 32;
@@ -220,37 +256,29 @@ __global__ __launch_bounds__(T) void rope_append_kernel(const RopeAppend a) {
         *reinterpret_cast<unsigned*>(blk + (slot * kG + group) * 16 + part * 4) = kc;
         const int half = slot >> 3, at = slot & 7, tp = group >> 1, w = group & 1;
         const int i0 = 8 * (part & 1) + (part < 2 ? 0 : 4);
+        uint8_t* const to = kFew ? reinterpret_cast<uint8_t*>(blk) + Mx<D>::kValues : s4;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          s4[half * Mx<D>::kHalf + ((tp * 16 + i0 + i) * 2 + w) * 8 + at] = (uint8_t)((low >> (4 * i) & 15u) | (high >> (4 * i) & 15u) << 4);
+          to[half * Mx<D>::kHalf + ((tp * 16 + i0 + i) * 2 + w) * 8 + at] = (uint8_t)((low >> (4 * i) & 15u) | (high >> (4 * i) & 15u) << 4);
         if (part == 0) {
-          s4[8 * D + slot * kG + group] = (uint8_t)ke;
-          s4[8 * D + D / 2 + half * Mx<D>::kHalfScales + (tp * 8 + at) * 2 + w] = (uint8_t)ve;
+          to[8 * D + slot * kG + group] = (uint8_t)ke;
+          to[8 * D + D / 2 + half * Mx<D>::kHalfScales + (tp * 8 + at) * 2 + w] = (uint8_t)ve;
         }
-      }
-    }
-    if (a.q) {
-      for (int h0 = 0;;) {
-#pragma unroll
-        for (int i = 0; i < kQueries; ++i) {
-          turn<Interleaved>(t, any, qv[i], y);
-          if (live && h0 + i < G) *reinterpret_cast<u32x4*>(a.q_out + (row * a.num_q_heads + g * G + h0 + i) * D + piece * 8) = any ? narrow(y) : qv[i];
-        }
-        h0 += kQueries;
-        if (h0 >= G) break;
-        query_loads(h0);
       }
     }
   }
-  __syncthreads();
-  if constexpr (!Four) {
-    for (int i = tid; i < 2 * D; i += T) store_value_columns<D>(kblk + 16L * D, sv, LD, i, run.slot0, run.n);
-  } else {
-    store_values_and_scales<D, T>(blk, s4, tid, run.slot0, run.slot0 + run.n);
+  if constexpr (!kFew) {
+    __syncthreads();
+    if constexpr (!Four) {
+      for (int i = tid; i < 2 * D; i += T) store_value_columns<D>(kblk + 16L * D, sv, LD, i, run.slot0, run.n);
+    } else {
+      store_values_and_scales<D, T>(blk, s4, tid, run.slot0, run.slot0 + run.n);
+    }
   }
 }
 
-// The way back: bf16 rows [T][Hkv][D] of the values that the 4-bit pages hold for the step's tokens, one workgroup of 2 D threads per (run, kv-head).
+// The way back: bf16 rows [T][Hkv][D] of the values that the 4-bit pages hold for the step's tokens, one workgroup of 2 D threads per (run, kv-head).  It
+// writes 3.8 times what it reads and is bound by that (8224 rows of 8 heads of 128: 43 MB in 8.5 us; 256 decodes: 2.4 us).
 template <int D>
 __global__ __launch_bounds__(2 * D) void read_new_kv_mx_kernel(const HfxRun* __restrict__ runs, int n_runs, int Hkv, const char* __restrict__ pool,
                                                              uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out) {
@@ -281,10 +309,10 @@ __global__ __launch_bounds__(2 * D) void read_new_kv_mx_kernel(const HfxRun* __r
   *reinterpret_cast<u32x4*>(v_out + to) = u32x4{from_fp4<0>(vc, ve), from_fp4<1>(vc, ve), from_fp4<2>(vc, ve), from_fp4<3>(vc, ve)};
 }
 
-// A workgroup for each (run, kv-head); the runs fill the two slower dimensions, the first of which holds at most 65535.
-static dim3 run_grid(const HfxHeader& h) {
+// `heads` workgroups for each run; the runs fill the two slower dimensions, the first of which holds at most 65535.
+static dim3 run_grid(const HfxHeader& h, unsigned heads) {
   const unsigned per_z = (unsigned)std::min(h.n_runs, 32768);
-  return dim3((unsigned)h.num_kv_heads, per_z, ((unsigned)h.n_runs + per_z - 1) / per_z);
+  return dim3(heads, per_z, ((unsigned)h.n_runs + per_z - 1) / per_z);
 }
 
 hipError_t launch_rope_append(const HfxHeader& h, const void* desc, RopeAppend a, bool four, hipStream_t stream) {
@@ -294,15 +322,17 @@ hipError_t launch_rope_append(const HfxHeader& h, const void* desc, RopeAppend a
   a.n_runs = h.n_runs;
   a.num_q_heads = h.num_q_heads;
   a.num_kv_heads = h.num_kv_heads;
-  // Runs of at most 4 tokens on average (decodes, chunks of a few rows) go to single wavefronts.
-  const bool few = (long)h.total_q <= 4l * h.n_runs;
+  // Runs of at most 8 tokens on average go to single wavefronts (128 chunks of n tokens, bf16 pages, then 4-bit ones, against 2 D threads: n = 2
+  // 5.0 us : 7.8, 4.5 : 7.6; n = 4 5.2 : 7.8, 4.8 : 7.7; n = 8 7.4 : 8.5, 7.2 : 8.0; n = 12 10.6 : 8.4; n = 16 12.4 : 8.9; 256 decodes 5.7 : 11.8).
+  const bool few = (long)h.total_q <= 8l * h.n_runs;
   auto pick = [&](auto d) {
     constexpr int D = decltype(d)::value;
     void (*const kernels[])(RopeAppend) = {rope_append_kernel<D, false, false, 2 * D>, rope_append_kernel<D, false, true, 2 * D>,
                                            rope_append_kernel<D, true, false, 2 * D>,  rope_append_kernel<D, true, true, 2 * D>,
                                            rope_append_kernel<D, false, false, 64>,    rope_append_kernel<D, false, true, 64>,
                                            rope_append_kernel<D, true, false, 64>,     rope_append_kernel<D, true, true, 64>};
-    return launch(kernels[(few ? 4 : 0) + (four ? 2 : 0) + (a.interleaved ? 1 : 0)], run_grid(h), few ? 64u : 2u * D, stream, a);
+    return launch(kernels[(few ? 4 : 0) + (four ? 2 : 0) + (a.interleaved ? 1 : 0)],
+                  run_grid(h, (few || !a.q ? 1u : 2u) * (unsigned)h.num_kv_heads), few ? (a.q ? 128u : 64u) : 2u * D, stream, a);
   };
   return h.head_dim == 128 ? pick(std::integral_constant<int, 128>()) : pick(std::integral_constant<int, 64>());
 }
@@ -310,7 +340,7 @@ hipError_t launch_rope_append(const HfxHeader& h, const void* desc, RopeAppend a
 hipError_t launch_read_new_kv_mx(const HfxHeader& h, const void* desc, const void* pool, void* k_out, void* v_out, hipStream_t stream) {
   if (h.n_runs <= 0) return hipSuccess;
   const HfxRun* runs = reinterpret_cast<const HfxRun*>(static_cast<const char*>(desc) + h.off_runs);
-  return launch(h.head_dim == 128 ? read_new_kv_mx_kernel<128> : read_new_kv_mx_kernel<64>, run_grid(h), 2u * (unsigned)h.head_dim, stream, runs, h.n_runs,
+  return launch(h.head_dim == 128 ? read_new_kv_mx_kernel<128> : read_new_kv_mx_kernel<64>, run_grid(h, (unsigned)h.num_kv_heads), 2u * (unsigned)h.head_dim, stream, runs, h.n_runs,
                 h.num_kv_heads, static_cast<const char*>(pool), static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out));
 }
 
