@@ -339,7 +339,8 @@ hfx_status hfx_mx_pool_bytes(const hfx_shape* shape, size_t* bytes);
 /*
  * hfx_rope_append_kv into a 4-bit pool.  The rotated keys, in fp32, and the values are quantised: e is the smallest power of two's under which the
  * block's largest magnitude is nearest to one of at most 6 (it is less than 7), kept within [2, 252]; codes are nearest, ties to the
- * even one.  A block with a value that is not finite gets e = 255 and stands for NaN.  Tokens of the page that are not in the step keep their bytes.
+ * even one.  A block with a value that is not finite gets e = 255 and stands for NaN; what attention over a context with such a block gives for that
+ * request is not defined (other requests are not touched by it).  Tokens of the page that are not in the step keep their bytes.
  * Arguments and errors as above.
  */
 hfx_status hfx_rope_append_kv_mx(const hfx_shape* shape, const hfx_rope* rope, const void* q, int64_t q_stride,
@@ -357,7 +358,7 @@ hfx_status hfx_read_new_kv_mx(const hfx_shape* shape, const void* mx_pool, const
 /*
  * hfx_mixed_paged_attention over a 4-bit pool: the same result as over a bf16 pool that holds the values that this one stands for, to rounding.  Scores and
  * the weighted sum accumulate in fp32, and softmax weights are rounded to bf16.  A query value enters as the sum of two 6-bit numbers with scales per 32
- * dimensions: exactly, where it is at least 1/4 of the largest of the 32, and to 2^-10 of that one otherwise (half of what bf16 rounds it by itself).
+ * dimensions: exactly, where it is at least 0.26 of the largest of the 32, and otherwise to 0.001 of that one (about half of what bf16 rounds it by itself).
  * Same descriptor, workspace, arguments and errors.
  */
 hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, const void* mx_pool, const void* host_desc,

@@ -264,7 +264,7 @@ def test_attention_over_the_4_bit_cache(hb, case):
 @pytest.mark.gpu
 @pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (8, 8, 64)])
 def test_attention_with_queries_of_many_sizes(hb, hq, hkv, d):
-    """Queries whose dimensions differ by many powers of two, whole heads that are tiny or zero: they are taken as sums of two 8-bit numbers with a scale
+    """Queries whose dimensions differ by many powers of two, whole heads that are tiny or zero: they are taken as sums of two 6-bit numbers with a scale
     for 32 dimensions.  Scores stay of order one by the softmax scale, so the bound is the usual one."""
     step = Step(hb, hq, hkv, d, [1, 40, 1], [333, 200, 90], 7)
     pool = random_pool(step)
