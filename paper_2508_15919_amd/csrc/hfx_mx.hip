@@ -377,7 +377,8 @@ struct PrefillWave4 {
   f32x16 o[D / 32];            // O^T accumulators per 32-dimension block
   u32x6 q[D / 64][2];          // of 64 dimensions: first numbers, remainders
   unsigned qs;                 // their scale bytes, in that order
-  float m, l;                  // reference exponent (base-2 domain) and running sum
+  float m, l;                  // reference exponent (base-2 domain); running sum (when the item is done)
+  f32x4 sum;                   // running sum of this lane's weights, four times
 };
 
 // Operand registers of a stage's 32 keys.
@@ -436,10 +437,67 @@ struct Share4<64> {
   static constexpr int values[5] = {0, 2, 5, 7, 10}, scores[5] = {10, 13, 16, 16, 16};
 };
 
+// The weights of a stage on their way, as over the bf16 pool, but summed by the matrix cores (values_phase4): an instruction of 16 clocks for eight
+// weights of each lane, against 40 of the vector unit, which is what bounds a step.  What has to be known beforehand, whether the reference exponent is still
+// in place, is in the rounded weights' top exponent bit: it is set from 2 up, which kHeadroom = 7 below the maximum is a growth of 2^8.
+constexpr float kHeadroom = 7.0f;
+struct Weighing4 {
+  float p[16];
+  unsigned pw[8];            // rounded pairs
+
+  __device__ __forceinline__ void finish(int i) {
+    const bf16x2 r = {(__bf16)p[2 * i], (__bf16)p[2 * i + 1]};
+    pw[i] = __builtin_bit_cast(unsigned, r);
+    asm volatile("" : "+v"(pw[i]));
+  }
+  // weights of scores [e0, e1), and the pairs that were completed in [before, e0)
+  __device__ __forceinline__ void portion(int before, int e0, int e1, const f32x16& s, float sl2, float m) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (e >= e0 && e < e1) {
+        p[e] = fast_exp2(__builtin_fmaf(s[e], sl2, -m));
+        asm volatile("" : "+v"(p[e]));
+      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (2 * i + 1 >= before && 2 * i + 1 < e0) finish(i);
+  }
+  __device__ __forceinline__ bf16x8 fragment(int sp) const {
+    return __builtin_bit_cast(bf16x8, u32x4{pw[4 * sp], pw[4 * sp + 1], pw[4 * sp + 2], pw[4 * sp + 3]});
+  }
+  __device__ __forceinline__ bool large() const {
+    const unsigned any = (pw[0] | pw[1] | pw[2]) | (pw[3] | pw[4] | pw[5]) | (pw[6] | pw[7]);
+    return (any & 0x40004000u) != 0;
+  }
+};
+
+// The weights of a stage, all known, as operands; taken again where the scores have outgrown the reference exponent.
+template <int D>
+__device__ __forceinline__ void settle_weights4(PrefillWave4<D>& w, const f32x16& s, bf16x8* pb, const Weighing4& wt, float sl2) {
+  pb[0] = wt.fragment(0);
+  pb[1] = wt.fragment(1);
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(wt.large()) != 0, 0)) {
+    const float m = fmaxf(w.m, row_max(s, sl2) + kHeadroom);
+    const float alpha = fast_exp2(w.m - m);
+    w.sum *= alpha;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) w.o[b] *= alpha;
+    w.m = m;
+    weights(s, sl2, m, pb);
+  }
+}
+
+// Operand that sums eight weights of each lane: a 16x16x32 product takes the lane's weights as those of k-group lane >> 4 and column lane & 15, and gives it
+// rows 4 (lane >> 4) .. + 3 of that column; so rows 4 g .. 4 g + 3 have ones in k-group g and zeros elsewhere.
+__device__ __forceinline__ bf16x8 summing_operand(int lane) {
+  const unsigned one = (lane & 15) >> 2 == lane >> 4 ? 0x3f803f80u : 0u;
+  return __builtin_bit_cast(bf16x8, u32x4{one, one, one, one});
+}
+
 // First phase of a stage: scores of the next one, the second half of the weights of the present one (scores cur) between them, and the present
 // stage's value fragments.  between(i) goes behind instruction i.
 template <int D, class Between>
-__device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, Keys4<D>& k, int j, bf16x8* frag, const f32x16& cur, Weighing& wt, float sl2,
+__device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, Keys4<D>& k, int j, bf16x8* frag, const f32x16& cur, Weighing4& wt, float sl2,
                                                 const char* values, int v_lane, Between between) {
   constexpr int S = D / 16;
   keys_ready<D>(k, j);
@@ -463,12 +521,13 @@ __device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, Keys4<
 
 // Second phase: weighted values of the present stage, the first half of the weights of the next one (scores next) between them.
 template <int D, class Between>
-__device__ __forceinline__ void values_phase4(PrefillWave4<D>& w, const bf16x8* frag, const bf16x8* pb, const f32x16& next, Weighing& wt, float sl2,
-                                              Between between) {
+__device__ __forceinline__ void values_phase4(PrefillWave4<D>& w, const bf16x8* frag, const bf16x8* pb, const f32x16& next, Weighing4& wt, float sl2,
+                                              const bf16x8& ones, Between between) {
   constexpr int B = D / 32, S = 2 * B;
 #pragma unroll
   for (int i = 0; i < S; ++i) {
     w.o[i % B] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i], pb[i / B], w.o[i % B], 0, 0, 0);
+    if (i % B == B - 1) w.sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[i / B], w.sum, 0, 0, 0);
     between(i);
     wt.portion(i == 0 ? 0 : Share4<D>::values[i - 1], Share4<D>::values[i], Share4<D>::values[i + 1], next, sl2, w.m);
     __builtin_amdgcn_sched_barrier(0);
@@ -565,6 +624,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const int s_lane = (krow >> 4) * L::kRawPage + Mx<D>::kKeyScales + (krow & 15) * Mx<D>::kGroups;
   const int v_lane = (n * 2 + (j ^ ((n >> 3) & 1))) * 16;   // V^T rows 32b + n, keys 8j.. of a page
   char* const values = smem + L::kRing;
+  const bf16x8 ones = summing_operand(lane);
   const CopyLane<D> cl = copy_lane<D>(lane);
   const unsigned lds_raw = lds_offset(smem + wave * L::kRawPage);
   // widening: this lane's value codes in the raw page (D = 128: at cl.values too), their scales, and where its dimensions go
@@ -694,13 +754,13 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       for (int i = 0; i < S; ++i) wd.piece(i, values + value_g + w_to);
       wide = 1;
     }
-    w.l = 0.f;
+    w.sum = f32x4{0.f, 0.f, 0.f, 0.f};
     const int wave_end = wr.wave_kend, unmasked_upto = wr.wave_pmin;
     auto mask_stage = [&](f32x16& s, int key0) {     // keys past this lane's row's horizon (rows past the chunk: its last row's)
       if (key0 + SK - 1 > unmasked_upto) mask_scores(s, min(unmasked_upto + n, ctx_len - 1), key0 + j * 8);
     };
     f32x16 s0;
-    Weighing wt;
+    Weighing4 wt;
     Keys4<D> keys = read_keys4<D>(smem + raw_g, k_lane, s_lane);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
@@ -713,7 +773,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     for (int i = 0; i < D / 32; ++i) score_product<D>(w, keys, i, s0);
     keys = read_keys4<D>(smem + raw_g + 2 * L::kRawPage, k_lane, s_lane);
     mask_stage(s0, kt);
-    w.m = fmaxf(HFX_M_NONE, row_max(s0, sl2));
+    w.m = fmaxf(HFX_M_NONE, row_max(s0, sl2)) + kHeadroom;
     wt.portion(0, 0, 4, s0, sl2, w.m);
     wt.portion(0, 4, Share4<D>::values[S], s0, sl2, w.m);
     wt.portion(4, Share4<D>::values[S - 1], Share4<D>::values[S - 1], s0, sl2, w.m);
@@ -722,11 +782,6 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
 #pragma unroll
         for (int i = 0; i < S; ++i) frag[i] = keep_first(frag[i], ctx_len - (key0 + i / (D / 32) * 16 + j * 8));
       }
-    };
-    auto settle = [&](const f32x16& s, bf16x8* pb) {
-      pb[0] = wt.fragment(0);
-      pb[1] = wt.fragment(1);
-      settle_weights<D>(w, s, pb, wt.sum(), sl2);
     };
     int plain = 0;        // steps ahead that every row of the wavefront sees whole and whose copies are in the lot at hand and in time
     bool whole = false;   // the present step is one
@@ -782,24 +837,24 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
         f32x16 s1 = scores_phase4<D>(w, keys, j, frag, s0, wt, sl2, slot, v_lane, [&](int i) {
           if (i == 1) wd.read(raw + w_codes + w_lane, raw + w_scales, lane);
         });
-        settle(s0, pb);
+        settle_weights4<D>(w, s0, pb, wt, sl2);
         if (!whole) {
           mask_stage(s1, kt + SK);
           mask_values(frag, kt);
         }
         __builtin_amdgcn_sched_barrier(0);
-        values_phase4<D>(w, frag, pb, s1, wt, sl2, [&](int i) {
+        values_phase4<D>(w, frag, pb, s1, wt, sl2, ones, [&](int i) {
           if (i == 0) keys = read_keys4<D>(raw, k_lane, s_lane);
           if (i % 2 == 1) wd.piece(i / 2, to);
         });
         s0 = scores_phase4<D>(w, keys, j, frag, s1, wt, sl2, slot + 2 * L::kValuePage, v_lane, Nothing());
-        settle(s1, pb);
+        settle_weights4<D>(w, s1, pb, wt, sl2);
         if (!whole) {
           mask_stage(s0, kt + 2 * SK);
           mask_values(frag, kt + SK);
         }
         __builtin_amdgcn_sched_barrier(0);
-        values_phase4<D>(w, frag, pb, s0, wt, sl2, [&](int i) {
+        values_phase4<D>(w, frag, pb, s0, wt, sl2, ones, [&](int i) {
           if (i == 0) keys = read_keys4<D>(raw + 2 * L::kRawPage, k_lane, s_lane);
           if (i < S / 2) wd.piece(S / 2 + i, to);          // (early, so that the synchronisation point does not wait for the writes)
         });
@@ -810,6 +865,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
       }
       kt += kStepKeys;
     }
+    w.l = w.sum[0];
     // hand-over
     tickets_take(t, s_tk, n_items);
     if (!next_ok) {
