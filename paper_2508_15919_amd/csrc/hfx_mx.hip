@@ -888,8 +888,35 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   __syncthreads();     // every wavefront is done with the ring before the LDS is used for anything else
 }
 
+// Steps whose decode work outweighs their prefill work have a queue that keeps the two on different CUs, for the sake of the decodes' stream of a bf16 pool.
+// Here that stream is a quarter as long, and where every item is dealt (two a workgroup) what counts is that the workgroups end together: prefill
+// items go first, the largest at the front, and the decode items behind them.  (us, the queue's own order and this one: 21 decodes and a 300-token prompt 18.8,
+// 16.6; 32 decodes and 777 tokens 38.0, 32.9; 64-wide heads, 48 decodes and three chunks 41.7, 38.1; 32 decodes of 8k to 64k tokens and 1024
+// rows behind 8192 on 8 / 1 heads 127, 72.  Queues that go on behind the dealt items keep their order: 200 decodes and two chunks 296, 327.)
+//
+// Place in the queue of item number `rank` in that order.  The queue gives the prefill items the workgroups of the first `pair` CUs, in both rounds, the
+// decode items the others, and what is left over follows.  Any two ranks have different places, whatever the queue is.
+__device__ __forceinline__ int place_by_kind(int rank, int n_prefill, int n_decode) {
+  constexpr int kHalf = HFX_PLAN_WGS / 2;
+  const int pair = min((n_prefill + 3) / 4, kHalf / 2);
+  const bool prefill = rank < n_prefill;
+  const int own = prefill ? rank : rank - n_prefill, others = prefill ? n_decode : n_prefill, width = prefill ? pair : kHalf - pair;
+  int i = own, at = prefill ? 0 : pair;
+  if (i >= 2 * width) {
+    i -= 2 * width;
+    at += HFX_PLAN_WGS;
+  }
+  if (i >= width) {
+    i -= width;
+    at += kHalf;
+  }
+  // (past the two rounds, or where the others have run out before: behind all of them)
+  return own < 4 * width && at + i - own <= others ? at + i : others + own;
+}
+
 template <int D>
-__global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(const HfxHeader hdr, const char* __restrict__ desc, int* __restrict__ ctrl,
+__global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(const HfxHeader hdr, const int by_kind, const char* __restrict__ desc,
+                                                                                int* __restrict__ ctrl,
                                                                                 const __bf16* __restrict__ q, const __bf16* __restrict__ pool,
                                                                                 float* __restrict__ ws, __bf16* __restrict__ out) {
   KArgs a;
@@ -905,6 +932,10 @@ __global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(c
   const HfxItem* items = reinterpret_cast<const HfxItem*>(a.desc + H->off_items);
   const int n_items = H->n_items;
   Tickets t = tickets_start(H, a.desc);
+  if (by_kind) {
+    if (t.cur < n_items) t.cur = place_by_kind(t.cur, H->n_prefill_items, H->n_decode_items);
+    if (t.nxt < n_items) t.nxt = place_by_kind(t.nxt, H->n_prefill_items, H->n_decode_items);
+  }
   while (t.cur < n_items) {
     if (items[t.cur].type == HFX_ITEM_DECODE) decode_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem);
     else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ids);
@@ -918,14 +949,17 @@ hipError_t max_resident_workgroups_mx(int head_dim, int* per_cu) {
 }
 
 hipError_t launch_mixed_attention_mx(const HfxHeader& h, int grid, void* desc, const void* q, const void* pool, void* ws, void* out, hipStream_t stream) {
-  const HfxHeader hk = launch_header(h, grid);
+  HfxHeader hb = h;
+  const bool by_kind = !h.deal_balanced && h.n_prefill_items > 0 && h.n_items <= kDealtTickets * grid;
+  if (by_kind) hb.deal_balanced = 1;
+  const HfxHeader hk = launch_header(hb, grid);
   const char* d = static_cast<const char*>(desc);
   int* ctrl = reinterpret_cast<int*>(static_cast<char*>(desc) + h.off_ctrl);
   const __bf16* qp = static_cast<const __bf16*>(q);
   const __bf16* pp = static_cast<const __bf16*>(pool);
   float* wp = static_cast<float*>(ws);
   __bf16* op = static_cast<__bf16*>(out);
-  const hipError_t e = launch(h.head_dim == 128 ? mixed_attention_mx_kernel<128> : mixed_attention_mx_kernel<64>, dim3(grid), HFX_WG_THREADS, stream, hk, d,
+  const hipError_t e = launch(h.head_dim == 128 ? mixed_attention_mx_kernel<128> : mixed_attention_mx_kernel<64>, dim3(grid), HFX_WG_THREADS, stream, hk, (int)by_kind, d,
                               ctrl, qp, pp, wp, op);
   return e != hipSuccess ? e : launch_merge(h, desc, ws, out, stream);
 }
