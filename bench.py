@@ -30,7 +30,7 @@ MFMA_BF16_PEAK_TFLOPS = 2500.0  # MI355X dense bf16 MFMA, published
 
 
 TRAFFIC_NOTE = os.path.join(ROOT, "profiles", "bench_hbm_traffic_fetch_write.txt")
-KERNEL_SOURCES = ["hfx_kernels.hip", "hfx_desc.h", "hfx_plan.cpp"]
+KERNEL_SOURCES = ["hfx_kernels.hip", "hfx_device.h", "hfx_desc.h", "hfx_plan.cpp"]
 
 
 def sources_digest() -> str:
