@@ -85,24 +85,26 @@ __device__ __forceinline__ void widen_values(unsigned a, unsigned b, const u32x4
   for (int k = 0; k < 4; ++k) widen_pair<At>(k, a, b, scales, lo, hi);
 }
 
-// A page's block in LDS: key codes [group][16 keys][16 bytes], value codes, then the scales as in the block; the copy of the scales writes 256
-// bytes, and 64 more put the keys of two pages in a row on different banks.
+// A page's block in LDS: key codes [group][16 keys][16 bytes], value codes, then the scales as in the block; the copy of the scales writes 256 bytes.
 template <int D>
 struct RawPage {
-  static constexpr int kBytes = 16 * D + 256 + 64;
+  static constexpr int kBytes = 16 * D + 256;
   static constexpr int kCopies = D == 128 ? 3 : 2;     // instructions that copy it
 };
-// Offsets, inside a block, of the lane's parts of the copy: keys change their order from [key][group] to [group][key].
+// Offsets, inside a block, of the lane's parts of the copy: keys change their order from [key][group] to [group][key].  Value codes, of which a unit of
+// 16 bytes has eight tokens of four dimensions, keep theirs, [8 tokens][64 dimensions][16], or (InTurn) get [64 dimensions][16][8 tokens].
 template <int D>
 struct CopyLane {
   unsigned keys, values, scales;
 };
-template <int D>
+template <int D, bool InTurn>
 __device__ __forceinline__ CopyLane<D> copy_lane(int lane) {
   constexpr int kG = Mx<D>::kGroups;
   CopyLane<D> c;
-  c.keys = D == 128 || lane < 32 ? (unsigned)(((lane & 15) * kG + ((lane >> 4) & (kG - 1))) * 16) : (unsigned)lane * 16;
-  c.values = (unsigned)lane * 16;
+  const int unit = lane & (D / 2 - 1);                 // of the value codes (D = 64: those of the lanes from 32 on)
+  const unsigned values = (unsigned)(InTurn ? (unit & 1) * Mx<D>::kHalf + (unit >> 1) * 16 : unit * 16);
+  c.keys = D == 128 || lane < 32 ? (unsigned)(((lane & 15) * kG + ((lane >> 4) & (kG - 1))) * 16) : Mx<D>::kValues + values;
+  c.values = values;
   c.scales = (unsigned)(lane & (D / 4 - 1)) * 4;
   return c;
 }
@@ -145,6 +147,9 @@ __device__ __forceinline__ void ids_copy(const int* table, unsigned offset, unsi
 // more than 2^8, so that the common pair needs no maximum, no exchange between lanes and no rescaling.
 // ----------------------------------------------------------------------------------------------
 constexpr int kRingPairs = 4;
+// Pages 64 bytes further apart than they are long: lanes of two pages and two groups read keys together.
+template <int D>
+constexpr int kDecodePage = RawPage<D>::kBytes + 64;
 
 // Lane's parts of the LDS addresses inside a pair.
 struct DecodeLane4 {
@@ -262,7 +267,7 @@ __device__ __forceinline__ DecodeQuery4<D> decode_query4(const __bf16* q, const 
 template <int D>
 __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
                             char* smem) {
-  constexpr int kPage = RawPage<D>::kBytes, kRing = 2 * kRingPairs * kPage, kCopies = 2 * RawPage<D>::kCopies;
+  constexpr int kPage = kDecodePage<D>, kRing = 2 * kRingPairs * kPage, kCopies = 2 * RawPage<D>::kCopies;
   const int tid = threadIdx.x;
   int lane = tid & 63;
   asm volatile("" : "+v"(lane));     // what follows from it is formed per run, not kept in registers through prefill runs
@@ -283,7 +288,7 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
   la.value = (j >> 1) * kPage + Mx<D>::kValues + (j & 1) * Mx<D>::kHalf + n * 16;
   la.value_scale = (j >> 1) * kPage + Mx<D>::kValueScales + (j & 1) * Mx<D>::kHalfScales;
   const int tok_lane = (j >> 1) * 16 + (j & 1) * 8;   // first of this lane's 8 tokens inside the pair
-  const CopyLane<D> cl = copy_lane<D>(lane);
+  const CopyLane<D> cl = copy_lane<D, false>(lane);
   char* const ring = smem + wave * kRing;
   const unsigned lds_ring = lds_offset(ring);
 
@@ -367,7 +372,7 @@ struct Smem4 {
   static constexpr int kValueStep = 4 * kValuePage;
   static constexpr int kRing = kRawSteps * kRawStep;
   static constexpr int kOut = kRing + 2 * kValueStep;  // result rows on their way out (prefill_store), 2 KB a wavefront
-  static constexpr int kPrefill = kOut + 4 * 2048, kDecode = 4 * 2 * kRingPairs * kRawPage;
+  static constexpr int kPrefill = kOut + 4 * 2048, kDecode = 4 * 2 * kRingPairs * kDecodePage<D>;
   static constexpr int kBytes = kPrefill > kDecode ? kPrefill : kDecode;
 };
 constexpr int kStepKeys = 64;
@@ -580,7 +585,7 @@ struct Widening {
       codes[0] = c.x;
       codes[1] = c.y;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) scales[k] >>= 8 * (lane & 1);          // which 32 dimensions of 64
+      for (int k = 0; k < 4; ++k) scales[k] >>= 8 * (lane >> 5);         // which 32 dimensions of 64
     }
   }
   // piece i of D / 16; every fourth completes two operands
@@ -625,14 +630,15 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const int v_lane = (n * 2 + (j ^ ((n >> 3) & 1))) * 16;   // V^T rows 32b + n, keys 8j.. of a page
   char* const values = smem + L::kRing;
   const bf16x8 ones = summing_operand(lane);
-  const CopyLane<D> cl = copy_lane<D>(lane);
+  const CopyLane<D> cl = copy_lane<D, true>(lane);
   const unsigned lds_raw = lds_offset(smem + wave * L::kRawPage);
-  // widening: this lane's value codes in the raw page (D = 128: at cl.values too), their scales, and where its dimensions go
-  const int half = lane >> 5;
-  const int w_codes = wave * L::kRawPage + Mx<D>::kValues, w_lane = lane * (D / 8);
-  const int w_scales = wave * L::kRawPage + Mx<D>::kValueScales + (D == 128 ? (lane >> 4) * 16 : half * 16);
-  const int w_i = D == 128 ? lane & 15 : (lane >> 1) & 15;
-  const int w_to = wave * L::kValuePage + (D == 128 ? ((lane >> 4) & 1) * 2048 : (lane & 1) * 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
+  // widening: this lane's value codes in the raw page (tokens half, unit w_i; D = 128: of 64 dimensions w_of, D = 64: of 32), their scales, and where its
+  // dimensions go.  Eight lanes in a row write 128 bytes in a row, which is what a write of 16 bytes a lane takes to do without bank conflicts (with the
+  // dimension in the low bits of the lane it took 16 cycles instead of 8; with the keys' reads, 12 % of a long step's cycles went to conflicts, 1 % now).
+  const int half = lane & 1, w_i = (lane >> 1) & 15, w_of = lane >> 5;
+  const int w_codes = wave * L::kRawPage + Mx<D>::kValues, w_lane = D == 128 ? lane * 16 : (lane & 31) * 16 + w_of * 8;
+  const int w_scales = wave * L::kRawPage + Mx<D>::kValueScales + half * Mx<D>::kHalfScales + (D == 128 ? w_of * 16 : 0);
+  const int w_to = wave * L::kValuePage + w_of * (D == 128 ? 2048 : 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
 
   const HfxItem item0 = items[t.cur], item1 = items[t.nxt < n_items ? t.nxt : t.cur];
   bool next_ok = t.nxt < n_items && item1.type == HFX_ITEM_PREFILL;
