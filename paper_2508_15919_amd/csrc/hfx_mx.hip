@@ -3,7 +3,8 @@
 //
 //   S^T = K . Q^T   on the scaled matrix instructions for 4 to 8 bits: the keys' codes and scale bytes go into them as they lie in the cache.  With their
 //                   other operand in 6 bits they have four times the rate of a bf16 product, and a query is taken as the sum of two 6-bit numbers
-//                   (E2M3, 4 significant bits), each with a scale for 32 dimensions: half the matrix time, and no key is ever converted.
+//                   (split_query), each with a scale for 32 dimensions: half the matrix time, and no key is ever converted.  (Two 8-bit numbers would
+//                   do as well, but with an operand of 8 bits the products take twice the time: 66 clocks a 32x32x64, not 34.)
 //   O^T = V^T . P^T on the bf16 matrix instructions: a scale belongs to a token, which is the contracted index here, so the values are widened to bf16
 //                   (every code times every scale is a bf16 number).
 #include <hip/hip_runtime.h>
@@ -139,7 +140,9 @@ __device__ __forceinline__ void ids_copy(const int* table, unsigned offset, unsi
 // ----------------------------------------------------------------------------------------------
 // Decode item: as over the bf16 pool one wavefront per kv-head (hn of them), the others interleave over page pairs.  Per pair (32 tokens) and kv-head a
 // wavefront takes 4352 bytes (D = 128), by direct-to-LDS copies into a ring of its own, three pairs ahead of their use: 104 KB in flight on a CU
-// without a register.
+// without a register (pairs held in registers, three or four deep, did not fit: 793 us where this takes 475).
+// Bound: HBM.  256 decodes of 2048 to 16384 tokens, 32 / 8 heads of 128: 2.59 GB in 475 us, 5.45 TB/s, merge included; until the first workgroup finds the
+// queue empty 6.0, which is what plain reads reach; without any arithmetic 464 us, with a ring of three pairs 475.
 //   S^T[token][head]: 16x16x128, a lane has 32 dimensions of one key (a group) with their scale; D = 64: lanes of the upper half have the
 //                     same keys again, against zeros.
 //   O^T[d][head]    : 16x16x32 bf16, a lane has eight tokens of dimension n of each tile.
@@ -357,9 +360,12 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
 
 // ----------------------------------------------------------------------------------------------
 // Prefill item: four wavefronts, each with 32 chunk rows of one q-head, all sharing the kv-head.  Keys arrive in steps of 64 (four pages, one a
-// wavefront): the wavefront copies its page's block into a ring of raw slots with direct-to-LDS loads, two to three steps ahead of its use; key codes are
+// wavefront): the wavefront copies its page's block into a ring of raw slots with direct-to-LDS loads, two steps ahead of its use at least; key codes are
 // read from there as operands by all four, and the value codes are widened to bf16 by the wavefront that copied them, a step ahead of
 // their use, into one of two slots in operand order.  So each value is widened once a workgroup, not once a wavefront.
+// Bound: the clock that power leaves, 1.8 to 1.9 GHz on long chunks; of its cycles the matrix cores are busy for 53 %, the vector unit by its
+// instructions for about as many, LDS for 33 %.  Four chunks of 2048 rows behind 0 to 12288 tokens and 32 decodes, 32 / 8 heads of 128: 716 to 731 us by the card, 1317 to 1345 TFLOP/s (over
+// the bf16 pool 800 to 850; a library product of 16384^3 has 1485); on zeros, which take less power, the same cycles run in 595 us.
 //   S^T[key][row]  = K . Q^T     32x32x64 scaled, keys' codes against the two numbers of the queries
 //   O^T[d][row]   += V^T . P^T   32x32x16 bf16, as over the bf16 pool
 // ----------------------------------------------------------------------------------------------
@@ -430,7 +436,7 @@ struct Nothing {
 };
 
 // Which weights are formed where (see Share): of a stage's 16 the value phase takes 10, the score phase, half as long here, 6, and its last
-// instruction none, so that the sum of the weights is known when it ends.  Two portions go behind each instruction of the score phase.
+// instruction none, so that the rounded weights are known when it ends.  Two portions go behind each instruction of the score phase.
 template <int D>
 struct Share4;
 template <>
@@ -442,7 +448,8 @@ struct Share4<64> {
   static constexpr int values[5] = {0, 2, 5, 7, 10}, scores[5] = {10, 13, 16, 16, 16};
 };
 
-// The weights of a stage on their way, as over the bf16 pool, but summed by the matrix cores (values_phase4): an instruction of 16 clocks for eight
+// The weights of a stage on their way, rounded to bf16 like the result that they make (the other operand, values with their scales, fits no other 16-bit type), as
+// over the bf16 pool, but summed, as rounded, by the matrix cores (values_phase4): an instruction of 16 clocks for eight
 // weights of each lane, against 40 of the vector unit, which is what bounds a step.  What has to be known beforehand, whether the reference exponent is still
 // in place, is in the rounded weights' top exponent bit: it is set from 2 up, which kHeadroom = 7 below the maximum is a growth of 2^8.
 constexpr float kHeadroom = 7.0f;
