@@ -388,7 +388,8 @@ class DescHeader(ctypes.Structure):
                 ("n_units", ctypes.c_int32), ("off_units", ctypes.c_uint32), ("n_runs", ctypes.c_int32),
                 ("off_runs", ctypes.c_uint32), ("queue_classes", ctypes.c_uint32),
                 ("deal_balanced", ctypes.c_uint32), ("off_queue", ctypes.c_uint32),
-                ("die_items", ctypes.c_uint32), ("off_run_pos", ctypes.c_uint32)]
+                ("die_items", ctypes.c_uint32), ("off_run_pos", ctypes.c_uint32),
+                ("max_ctx_len", ctypes.c_int32), ("pad1", ctypes.c_int32)]
 
 
 ITEM_DTYPE = np.dtype([(n, np.int32) for n in ("type", "req", "group", "slot_row", "h0", "hn", "row0", "nrows",

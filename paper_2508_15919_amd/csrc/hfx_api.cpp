@@ -94,9 +94,7 @@ hfx_status rope_append(const hfx_shape* shape, const hfx_rope* rope, const void*
     if (rope->rot_dim < 16 || rope->rot_dim > h.head_dim || rope->rot_dim % 16 != 0 || (rope->interleaved != 0 && rope->interleaved != 1))
       return HFX_ERR_SHAPE;
     if (!aligned16(rope->cos_sin)) return HFX_ERR_ALIGN;
-    const HfxReq* reqs = reinterpret_cast<const HfxReq*>(static_cast<const char*>(host_desc) + h.off_req);
-    for (int r = 0; r < h.num_requests; ++r)
-      if (reqs[r].ctx_len > rope->num_positions) return HFX_ERR_LEN;
+    if (h.max_ctx_len > rope->num_positions) return HFX_ERR_LEN;
     a.rot = rope->rot_dim;
     a.interleaved = rope->interleaved;
     a.cos_sin = rope->cos_sin;

@@ -4,7 +4,7 @@
 #include <stdint.h>
 
 #define HFX_DESC_MAGIC 0x31584648u /* "HFX1" */
-#define HFX_DESC_VERSION 18u
+#define HFX_DESC_VERSION 19u
 #define HFX_PAGE 16
 #define HFX_WG_THREADS 256
 #define HFX_PLAN_WGS 512         /* planning width: 256 compute units x 2 resident workgroups */
@@ -48,6 +48,8 @@ struct HfxHeader {
   uint32_t off_queue;           /* 0: queue position p is item p; else n_items item indices, by position */
   uint32_t die_items;           /* of the queue positions, the first die_items belong to dies, p to die p % HFX_QUEUE_CLASSES, and those behind to all */
   uint32_t off_run_pos;         /* logical position of each append run's first token, one int32 a run */
+  int32_t max_ctx_len;          /* longest context of the step */
+  int32_t pad1;
 };
 
 struct HfxReq {

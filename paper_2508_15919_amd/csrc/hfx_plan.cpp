@@ -1042,6 +1042,7 @@ void layout_blob(const hfx_shape* shape, const Plan& P, HfxHeader* h) {
   h->die_items = (uint32_t)P.die_items;
   h->max_group_rows = 0;
   for (const HfxGroup& g : P.groups) h->max_group_rows = std::max(h->max_group_rows, g.rows_per_split);
+  for (const HfxReq& q : P.reqs) h->max_ctx_len = std::max(h->max_ctx_len, q.ctx_len);
   uint64_t off = align_up(sizeof(HfxHeader), 256);
   h->off_ctrl = (uint32_t)off;
   off = align_up(off + 4ull * h->n_ctrl, 64);
