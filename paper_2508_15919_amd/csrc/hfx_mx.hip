@@ -435,13 +435,14 @@ struct Nothing {
   __device__ __forceinline__ void operator()(int) const {}
 };
 
-// Which weights are formed where (see Share): of a stage's 16 the value phase takes 10, the score phase, half as long here, 6, and its last
-// instruction none, so that the rounded weights are known when it ends.  Two portions go behind each instruction of the score phase.
+// Which weights are formed where (see Share): of a stage's 16 the value phase takes 12 (64-wide heads: 10), the score phase, half as long here, the others at
+// its beginning, so that the rounded weights are known well before it ends.  Two portions go behind each instruction of the score phase.  (8, 10, 12, 14 and
+// 16 in the value phase: long chunks 718.6, 719.7, 715.2, 717.1 and 719.0 us.)
 template <int D>
 struct Share4;
 template <>
 struct Share4<128> {
-  static constexpr int values[9] = {0, 0, 1, 3, 4, 6, 7, 9, 10}, scores[9] = {10, 11, 12, 13, 14, 15, 16, 16, 16};
+  static constexpr int values[9] = {0, 0, 2, 4, 6, 8, 10, 11, 12}, scores[9] = {12, 14, 16, 16, 16, 16, 16, 16, 16};
 };
 template <>
 struct Share4<64> {
