@@ -145,6 +145,19 @@ __device__ __forceinline__ void store_values_and_scales(char* blk, const uint8_t
   }
 }
 
+// 16 bytes of a row that is read or written once; Past: past the caches.
+template <bool Past>
+__device__ __forceinline__ u32x4 load_row(const uint16_t* p) {
+  const u32x4* v = reinterpret_cast<const u32x4*>(p);
+  return Past ? __builtin_nontemporal_load(v) : *v;
+}
+template <bool Past>
+__device__ __forceinline__ void store_row(uint16_t* p, const u32x4& x) {
+  u32x4* v = reinterpret_cast<u32x4*>(p);
+  if constexpr (Past) __builtin_nontemporal_store(x, v);
+  else *v = x;
+}
+
 // Q-heads of a kv-head whose loads are in flight together.
 constexpr int kQueries = 4;
 
@@ -166,10 +179,10 @@ __device__ __forceinline__ bool run_and_head(int n_runs, int heads, int& index, 
 // its loads may be in flight for.  T = 2 D threads have all 16 tokens at once, and pass the values through LDS, where a page has the tokens of a dimension
 // side by side.  T = 64, for steps whose runs are of a few tokens: a wavefront goes round, values go to their bytes straight from the registers, and the
 // two parts are the two wavefronts of one workgroup.
-// Bound by memory where there is much to do (32 q-heads, 8 kv-heads, 128 wide, 8224 rows in long chunks: 206 MB in 32.4 us, 6.4 TB/s; 4-bit pages:
-// 177 MB in 29.6 us), and by the chain of its loads (record of the run, then rows and angles) where there is little (four decodes: 3.6 us, of which an empty kernel
+// Bound by memory where there is much to do (32 q-heads, 8 kv-heads, 128 wide, 8224 rows in long chunks: 206 MB in 39.2 us on changing buffers, 5.3 TB/s; a
+// plain copy has 4.9), and by the chain of its loads (record of the run, then rows and angles) where there is little (four decodes: 3.6 us, of which an empty kernel
 // takes 1.5; 256 decodes into 4-bit pages 5.6).  With keys, values and queries in turn in one wavefront those were 6.0 and 7.5 us.
-template <int D, bool Four, bool Interleaved, int T>
+template <int D, bool Four, bool Interleaved, int T, bool Past>
 __global__ __launch_bounds__(T == 64 ? 128 : T) void rope_append_kernel(const RopeAppend a) {
   constexpr bool kFew = T == 64;
   constexpr int LD = D + 8;                       // LDS row stride in elements
@@ -203,13 +216,13 @@ __global__ __launch_bounds__(T == 64 ? 128 : T) void rope_append_kernel(const Ro
       for (int h0 = 0; h0 < G; h0 += kQueries) {
         u32x4 qv[kQueries];
 #pragma unroll
-        for (int i = 0; i < kQueries; ++i) qv[i] = *reinterpret_cast<const u32x4*>(from + min(h0 + i, G - 1) * D);
+        for (int i = 0; i < kQueries; ++i) qv[i] = load_row<Past>(from + min(h0 + i, G - 1) * D);
 #pragma unroll
         for (int i = 0; i < kQueries; ++i) {
           if (h0 + i >= G) break;
           float y[8];
           turn<Interleaved>(t, any, qv[i], y);
-          if (tok < run.n) *reinterpret_cast<u32x4*>(to + (h0 + i) * D) = any ? narrow(y) : qv[i];
+          if (tok < run.n) store_row<Past>(to + (h0 + i) * D, any ? narrow(y) : qv[i]);
         }
       }
     }
@@ -224,8 +237,8 @@ __global__ __launch_bounds__(T == 64 ? 128 : T) void rope_append_kernel(const Ro
     const long row = (long)run.row0 + own;
     Turn t;
     if (any) t = turn_of<Interleaved>(a.cos_sin + (long)(position + own) * a.rot, a.rot, piece, lane);
-    const u32x4 kv = *reinterpret_cast<const u32x4*>(a.k + row * a.k_stride + g * D + piece * 8);
-    const u32x4 vv = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + g * D + piece * 8);
+    const u32x4 kv = load_row<Past>(a.k + row * a.k_stride + g * D + piece * 8);
+    const u32x4 vv = load_row<Past>(a.v + row * a.v_stride + g * D + piece * 8);
     float y[8];
     turn<Interleaved>(t, any, kv, y);
     const int slot = run.slot0 + tok;
@@ -325,13 +338,19 @@ hipError_t launch_rope_append(const HfxHeader& h, const void* desc, RopeAppend a
   // Runs of at most 8 tokens on average go to single wavefronts (128 chunks of n tokens, bf16 pages, then 4-bit ones, against 2 D threads: n = 2
   // 5.0 us : 7.8, 4.5 : 7.6; n = 4 5.2 : 7.8, 4.8 : 7.7; n = 8 7.4 : 8.5, 7.2 : 8.0; n = 12 10.6 : 8.4; n = 16 12.4 : 8.9; 256 decodes 5.7 : 11.8).
   const bool few = (long)h.total_q <= 8l * h.n_runs;
+  // Rows of more than 64 MB in all (queries in and out, keys, values) go past the caches, where they would only be in the way: 8224 rows of 32 / 8 heads, 173 MB,
+  // 43.7 -> 39.2 us on changing buffers (4-bit pages and the way back 50.9 -> 44.9).  With the attention that follows and reads the queries: 8224 rows 263.2 ->
+  // 260.1 us, 4128 rows, 87 MB, 163.4 -> 162.8, but 2064 rows, 43 MB, 80.7 -> 81.6 and 520 25.1 -> 26.0.
+  const int64_t row_bytes = (int64_t)((a.q ? 2 * h.num_q_heads : 0) + 2 * h.num_kv_heads) * h.head_dim * 2;
+  const bool past = !few && row_bytes * h.total_q > (64ll << 20);
   auto pick = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    void (*const kernels[])(RopeAppend) = {rope_append_kernel<D, false, false, 2 * D>, rope_append_kernel<D, false, true, 2 * D>,
-                                           rope_append_kernel<D, true, false, 2 * D>,  rope_append_kernel<D, true, true, 2 * D>,
-                                           rope_append_kernel<D, false, false, 64>,    rope_append_kernel<D, false, true, 64>,
-                                           rope_append_kernel<D, true, false, 64>,     rope_append_kernel<D, true, true, 64>};
-    return launch(kernels[(few ? 4 : 0) + (four ? 2 : 0) + (a.interleaved ? 1 : 0)],
+    void (*const kernels[])(RopeAppend) = {
+        rope_append_kernel<D, false, false, 2 * D, false>, rope_append_kernel<D, false, true, 2 * D, false>, rope_append_kernel<D, true, false, 2 * D, false>,
+        rope_append_kernel<D, true, true, 2 * D, false>,   rope_append_kernel<D, false, false, 2 * D, true>, rope_append_kernel<D, false, true, 2 * D, true>,
+        rope_append_kernel<D, true, false, 2 * D, true>,   rope_append_kernel<D, true, true, 2 * D, true>,   rope_append_kernel<D, false, false, 64, false>,
+        rope_append_kernel<D, false, true, 64, false>,     rope_append_kernel<D, true, false, 64, false>,    rope_append_kernel<D, true, true, 64, false>};
+    return launch(kernels[(few ? 8 : past ? 4 : 0) + (four ? 2 : 0) + (a.interleaved ? 1 : 0)],
                   run_grid(h, (few || !a.q ? 1u : 2u) * (unsigned)h.num_kv_heads), few ? (a.q ? 128u : 64u) : 2u * D, stream, a);
   };
   return h.head_dim == 128 ? pick(std::integral_constant<int, 128>()) : pick(std::integral_constant<int, 64>());

@@ -311,3 +311,37 @@ def test_values_that_are_not_finite_stay_in_their_request(hb):
     got = attend(step, q, torch.from_numpy(bad).cuda())
     others = np.isin(step.request, (0, 3))
     assert np.array_equal(got[others], want[others]) and not np.array_equal(got[~others], want[~others])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,interleaved", [(32, 8, 128, False), (32, 8, 128, True), (64, 16, 64, False), (64, 16, 64, True)])
+def test_a_large_step_is_its_requests_one_by_one(hb, hq, hkv, d, interleaved):
+    """Steps whose rows pass 64 MB take another way through the caches; each of the requests alone does not."""
+    import torch
+    q_len, ctx = [2001, 1, 1997], [2001, 77, 2500]
+    step = Step(hb, hq, hkv, d, q_len, ctx, 71)
+    g = torch.Generator(device="cuda").manual_seed(71)
+    rows = torch.empty((step.tokens, (hq + 2 * hkv) * d), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    assert step.tokens * 2 * (hq + hkv) * d * 2 > 64 << 20 > 2001 * 2 * (hq + hkv) * d * 2
+    rope = hb.make_rope(torch.from_numpy(angles(2500, d)).cuda(), d, interleaved)
+    stream = torch.cuda.current_stream()
+
+    def append(f, sizes, x, q, pool, host, dev):
+        qs, ks, vs = x.split((hq * d, hkv * d, hkv * d), 1)
+        f(sizes, rope, qs, qs.stride(0), ks, ks.stride(0), vs, vs.stride(0), q, pool, host, dev, stream)
+    for f, shape, dtype in ((hb.hfx_rope_append_kv, (step.num_pages, hkv, 2, 16 * d), torch.bfloat16), (hb.hfx_rope_append_kv_mx, (step.num_pages, hkv, 17 * d), torch.uint8)):
+        whole, parts = (torch.zeros(shape, dtype=dtype, device="cuda") for _ in range(2))
+        q, q_parts = (torch.zeros((step.tokens, hq, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        append(f, step.shape, rows, q, whole, step.host, step.dev)
+        kept, at = [], 0
+        for r, n in enumerate(q_len):
+            kind, one, c = step.kind[r:r + 1], step.q_len[r:r + 1], step.ctx_len[r:r + 1]
+            size, _, _ = hb.hfx_batch_desc_sizes(step.shape, kind, one, c)
+            host, dev = torch.empty(size, dtype=torch.uint8, pin_memory=True), torch.empty(size, dtype=torch.uint8, device="cuda")
+            pages = step.pages[step.indptr[r]:step.indptr[r + 1]]
+            hb.hfx_build_batch_desc(step.shape, kind, one, c, np.array([0, len(pages)], np.int32), pages, host, dev, stream)
+            append(f, step.shape, rows[at:at + n], q_parts[at:at + n], parts, host, dev)
+            kept.append((host, dev))
+            at += n
+        torch.cuda.synchronize()
+        assert torch.equal(q.view(torch.int16), q_parts.view(torch.int16)) and torch.equal(whole.view(torch.uint8), parts.view(torch.uint8)) and bool(whole.any())
