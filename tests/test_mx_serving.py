@@ -345,3 +345,30 @@ def test_a_large_step_is_its_requests_one_by_one(hb, hq, hkv, d, interleaved):
             at += n
         torch.cuda.synchronize()
         assert torch.equal(q.view(torch.int16), q_parts.view(torch.int16)) and torch.equal(whole.view(torch.uint8), parts.view(torch.uint8)) and bool(whole.any())
+
+
+def test_which_steps_read_pages_past_the_caches():
+    """Large steps, unless their requests share leading pages that the caches serve; planned on the host."""
+    from paper_2508_15919_amd import binding
+    hq, hkv, d = 32, 8, 128
+    page = 17 * hkv * d
+
+    def flag(requests, pages_each, shared, kind=0):
+        own = pages_each - shared
+        ids = np.concatenate([np.concatenate((np.arange(shared), shared + i * own + np.arange(own))) for i in range(requests)]).astype(np.int32)
+        ctx, q = np.full(requests, 16 * pages_each, np.int32), np.ones(requests, np.int32)
+        shape = binding.make_shape(hq, hkv, d, shared + requests * own)
+        kinds = np.full(requests, kind, np.int32)
+        host = np.zeros(binding.hfx_batch_desc_sizes(shape, kinds, q, ctx)[0], np.uint8)
+        binding.hfx_fill_batch_desc(shape, kinds, q, ctx, (np.arange(requests + 1) * pages_each).astype(np.int32), ids, host)
+        return binding.parse_desc(host)["header"].stream_mx
+    many, behind = (64 << 20) // page + 1, (3 << 20) // page + 1
+    assert flag(8, many // 8 + 1, 0) == 1 and flag(8, many // 8 - 8, 0) == 0 and flag(1, many, 0) == 1
+    assert flag(8, many // 8 + 1, behind) == 0 and flag(8, many // 8 + 1, behind - 1) == 1
+    assert flag(500, behind + 20, behind) == 0 and flag(500, behind + 20, 0) == 1
+
+
+@pytest.mark.gpu
+def test_both_pools_where_pages_go_past_the_caches(hb):
+    test_both_pools_on_larger_steps(hb, 8, 8, 64, [1, 1, 1, 40], [60000, 70001, 50000, 900])
+    test_both_pools_on_larger_steps(hb, 16, 8, 128, [1, 1, 33], [40000, 30001, 700])
