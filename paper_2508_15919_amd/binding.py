@@ -389,7 +389,7 @@ class DescHeader(ctypes.Structure):
                 ("off_runs", ctypes.c_uint32), ("queue_classes", ctypes.c_uint32),
                 ("deal_balanced", ctypes.c_uint32), ("off_queue", ctypes.c_uint32),
                 ("die_items", ctypes.c_uint32), ("off_run_pos", ctypes.c_uint32),
-                ("max_ctx_len", ctypes.c_int32), ("pad1", ctypes.c_int32)]
+                ("max_ctx_len", ctypes.c_int32), ("stream_mx", ctypes.c_uint32)]
 
 
 ITEM_DTYPE = np.dtype([(n, np.int32) for n in ("type", "req", "group", "slot_row", "h0", "hn", "row0", "nrows",

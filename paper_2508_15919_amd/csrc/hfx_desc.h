@@ -49,7 +49,7 @@ struct HfxHeader {
   uint32_t die_items;           /* of the queue positions, the first die_items belong to dies, p to die p % HFX_QUEUE_CLASSES, and those behind to all */
   uint32_t off_run_pos;         /* logical position of each append run's first token, one int32 a run */
   int32_t max_ctx_len;          /* longest context of the step */
-  int32_t pad1;
+  uint32_t stream_mx;           /* over a 4-bit pool, the pages of decode items are read past the caches */
 };
 
 struct HfxReq {

@@ -119,14 +119,21 @@ __device__ __forceinline__ unsigned lds_offset(const void* p) {
 
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-// Direct-to-LDS copy of a page's block: base (scalar), the lane's offsets, LDS destination.  The compiler does not know of these loads: its own
-// waits for vector memory become stricter by them, and those for what is copied are explicit (HFX_WAIT_VMCNT).
-template <int D>
+// Direct-to-LDS copy of a page's block: base (scalar), the lane's offsets, LDS destination; Past: past the caches.  The compiler does not know of these
+// loads: its own waits for vector memory become stricter by them, and those for what is copied are explicit (HFX_WAIT_VMCNT).
+template <int D, bool Past>
 __device__ __forceinline__ void raw_copy(const char* base, const CopyLane<D>& c, unsigned lds) {
-  if constexpr (D == 128)
+  if constexpr (D == 128 && Past)
+    asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %3 nt\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024 nt\n\t"
+                 "global_load_lds_dword %2, %3 offset:2048 nt"
+                 :: "v"(c.keys), "v"(c.values), "v"(c.scales), "s"(base), "s"(lds) : "memory", "m0");
+  else if constexpr (D == 128)
     asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %3\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024\n\t"
                  "global_load_lds_dword %2, %3 offset:2048"
                  :: "v"(c.keys), "v"(c.values), "v"(c.scales), "s"(base), "s"(lds) : "memory", "m0");
+  else if constexpr (Past)
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2 nt\n\tglobal_load_lds_dword %1, %2 offset:1024 nt"
+                 :: "v"(c.keys), "v"(c.scales), "s"(base), "s"(lds) : "memory", "m0");
   else
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dword %1, %2 offset:1024"
                  :: "v"(c.keys), "v"(c.scales), "s"(base), "s"(lds) : "memory", "m0");
@@ -140,9 +147,9 @@ __device__ __forceinline__ void ids_copy(const int* table, unsigned offset, unsi
 // ----------------------------------------------------------------------------------------------
 // Decode item: as over the bf16 pool one wavefront per kv-head (hn of them), the others interleave over page pairs.  Per pair (32 tokens) and kv-head a
 // wavefront takes 4352 bytes (D = 128), by direct-to-LDS copies into a ring of its own, three pairs ahead of their use: 104 KB in flight on a CU
-// without a register (pairs held in registers, three or four deep, did not fit: 793 us where this takes 475).
-// Bound: HBM.  256 decodes of 2048 to 16384 tokens, 32 / 8 heads of 128: 2.59 GB in 475 us, 5.45 TB/s, merge included; until the first workgroup finds the
-// queue empty 6.0, which is what plain reads reach; without any arithmetic 464 us, with a ring of three pairs 475.
+// without a register (pairs held in registers, three or four deep, did not fit: 793 us where this took 475).
+// Bound: HBM.  256 decodes of 2048 to 16384 tokens, 32 / 8 heads of 128: 2.59 GB in 415 to 442 us by the card, 5.9 to 6.2 TB/s, merge included; through the
+// caches 457 to 475, of which all but the arithmetic was 464.
 //   S^T[token][head]: 16x16x128, a lane has 32 dimensions of one key (a group) with their scale; D = 64: lanes of the upper half have the
 //                     same keys again, against zeros.
 //   O^T[d][head]    : 16x16x32 bf16, a lane has eight tokens of dimension n of each tile.
@@ -267,7 +274,7 @@ __device__ __forceinline__ DecodeQuery4<D> decode_query4(const __bf16* q, const 
 }
 
 // Runs the decode item t.cur and carries on for as long as the workgroup's next item is a decode item too.
-template <int D>
+template <int D, bool Past>
 __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
                             char* smem) {
   constexpr int kPage = kDecodePage<D>, kRing = 2 * kRingPairs * kPage, kCopies = 2 * RawPage<D>::kCopies;
@@ -304,8 +311,8 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
     int to = 0;                        // and its place in the ring
     auto copy_pair = [&]() {
       const unsigned long b0 = (unsigned)n0 * (unsigned)Hkv + (unsigned)d.g, b1 = (unsigned)n1 * (unsigned)Hkv + (unsigned)d.g;
-      raw_copy<D>(pool + b0 * Mx<D>::kBlock, cl, lds_ring + (unsigned)to);
-      raw_copy<D>(pool + b1 * Mx<D>::kBlock, cl, lds_ring + (unsigned)(to + kPage));
+      raw_copy<D, Past>(pool + b0 * Mx<D>::kBlock, cl, lds_ring + (unsigned)to);
+      raw_copy<D, Past>(pool + b1 * Mx<D>::kBlock, cl, lds_ring + (unsigned)(to + kPage));
       next += d.step;
       to = to == kRing - 2 * kPage ? 0 : to + 2 * kPage;
       n0 = constant(bt)[d.bt0 + min(next, d.last_page)];
@@ -364,7 +371,7 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
 // read from there as operands by all four, and the value codes are widened to bf16 by the wavefront that copied them, a step ahead of
 // their use, into one of two slots in operand order.  So each value is widened once a workgroup, not once a wavefront.
 // Bound: the clock that power leaves, 1.8 to 1.9 GHz on long chunks; of its cycles the matrix cores are busy for 53 %, the vector unit by its
-// instructions for about as many, LDS for 33 %.  Four chunks of 2048 rows behind 0 to 12288 tokens and 32 decodes, 32 / 8 heads of 128: 716 to 731 us by the card, 1317 to 1345 TFLOP/s (over
+// instructions for about as many, LDS for 33 %.  Four chunks of 2048 rows behind 0 to 12288 tokens and 32 decodes, 32 / 8 heads of 128: 695 to 720 us by the card, 1337 to 1385 TFLOP/s (over
 // the bf16 pool 800 to 850; a library product of 16384^3 has 1485); on zeros, which take less power, the same cycles run in 595 us.
 //   S^T[key][row]  = K . Q^T     32x32x64 scaled, keys' codes against the two numbers of the queries
 //   O^T[d][row]   += V^T . P^T   32x32x16 bf16, as over the bf16 pool
@@ -705,7 +712,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   // copies the next step, whose entry of the lot at hand is `page`, to ring offset `to`
   auto copy_one = [&](int page, int to) {
     const unsigned block = (unsigned)page * (unsigned)Hkv + (unsigned)head;
-    raw_copy<D>(pool + (unsigned long)block * Mx<D>::kBlock, cl, lds_raw + (unsigned)to);
+    raw_copy<D, false>(pool + (unsigned long)block * Mx<D>::kBlock, cl, lds_raw + (unsigned)to);
     ++at;
   };
   // copies steps until `limit` are on their way, as far as they are known; lots that have been asked for have landed, unless `asked`
@@ -928,7 +935,8 @@ __device__ __forceinline__ int place_by_kind(int rank, int n_prefill, int n_deco
   return own < 4 * width && at + i - own <= others ? at + i : others + own;
 }
 
-template <int D>
+// Past: the pages of decode items go past the caches (the planner's stream_mx).
+template <int D, bool Past>
 __global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(const HfxHeader hdr, const int by_kind, const char* __restrict__ desc,
                                                                                 int* __restrict__ ctrl,
                                                                                 const __bf16* __restrict__ q, const __bf16* __restrict__ pool,
@@ -951,15 +959,15 @@ __global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(c
     if (t.nxt < n_items) t.nxt = place_by_kind(t.nxt, H->n_prefill_items, H->n_decode_items);
   }
   while (t.cur < n_items) {
-    if (items[t.cur].type == HFX_ITEM_DECODE) decode_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem);
+    if (items[t.cur].type == HFX_ITEM_DECODE) decode_run4<D, Past>(a, H, items, n_items, t, s_tk, ctrl, smem);
     else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ids);
   }
   queue_done(H, ctrl);
 }
 
 hipError_t max_resident_workgroups_mx(int head_dim, int* per_cu) {
-  if (head_dim == 128) return hipOccupancyMaxActiveBlocksPerMultiprocessor(per_cu, mixed_attention_mx_kernel<128>, HFX_WG_THREADS, 0);
-  return hipOccupancyMaxActiveBlocksPerMultiprocessor(per_cu, mixed_attention_mx_kernel<64>, HFX_WG_THREADS, 0);
+  if (head_dim == 128) return hipOccupancyMaxActiveBlocksPerMultiprocessor(per_cu, mixed_attention_mx_kernel<128, false>, HFX_WG_THREADS, 0);
+  return hipOccupancyMaxActiveBlocksPerMultiprocessor(per_cu, mixed_attention_mx_kernel<64, false>, HFX_WG_THREADS, 0);
 }
 
 hipError_t launch_mixed_attention_mx(const HfxHeader& h, int grid, void* desc, const void* q, const void* pool, void* ws, void* out, hipStream_t stream) {
@@ -973,8 +981,9 @@ hipError_t launch_mixed_attention_mx(const HfxHeader& h, int grid, void* desc, c
   const __bf16* pp = static_cast<const __bf16*>(pool);
   float* wp = static_cast<float*>(ws);
   __bf16* op = static_cast<__bf16*>(out);
-  const hipError_t e = launch(h.head_dim == 128 ? mixed_attention_mx_kernel<128> : mixed_attention_mx_kernel<64>, dim3(grid), HFX_WG_THREADS, stream, hk, (int)by_kind, d,
-                              ctrl, qp, pp, wp, op);
+  void (*const kernels[])(HfxHeader, int, const char*, int*, const __bf16*, const __bf16*, float*, __bf16*) = {
+      mixed_attention_mx_kernel<64, false>, mixed_attention_mx_kernel<64, true>, mixed_attention_mx_kernel<128, false>, mixed_attention_mx_kernel<128, true>};
+  const hipError_t e = launch(kernels[(h.head_dim == 128 ? 2 : 0) + (h.stream_mx ? 1 : 0)], dim3(grid), HFX_WG_THREADS, stream, hk, (int)by_kind, d, ctrl, qp, pp, wp, op);
   return e != hipSuccess ? e : launch_merge(h, desc, ws, out, stream);
 }
 
