@@ -615,6 +615,41 @@ struct Widening {
   }
 };
 
+// What the second half of an item (prefill_run4) hands to the first: a wavefront's accumulators, reference exponents and sums, where its ring was.
+template <int D>
+struct Joined {
+  static constexpr int kWave = (D / 32 * 16 + 2) * 64 * 4;
+  static_assert(4 * kWave <= Smem4<D>::kPrefill, "in the place of the second half's rings");
+};
+template <int D>
+__device__ __forceinline__ void join_halves(PrefillWave4<D>& w, int part, int lane, char* place) {
+  f32x4* const o = reinterpret_cast<f32x4*>(place) + lane;
+  float* const ml = reinterpret_cast<float*>(place + D / 32 * 16 * 256) + lane;
+  ring_barrier();          // the rings are not read any more, and nothing is on its way to them
+  if (part == 1) {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) o[(b * 4 + q4) * 64] = f32x4{w.o[b][q4 * 4], w.o[b][q4 * 4 + 1], w.o[b][q4 * 4 + 2], w.o[b][q4 * 4 + 3]};
+    ml[0] = w.m;
+    ml[64] = w.l;
+  }
+  ring_barrier();
+  if (part == 0) {
+    const float m = fmaxf(w.m, ml[0]), own = fast_exp2(w.m - m), other = fast_exp2(ml[0] - m);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4 x = o[(b * 4 + q4) * 64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w.o[b][q4 * 4 + e] = __builtin_fmaf(x[e], other, w.o[b][q4 * 4 + e] * own);
+      }
+    w.l = __builtin_fmaf(ml[64], other, w.l * own);
+    w.m = m;
+  }
+}
+
 // Runs the prefill item t.cur and, for as long as the workgroup's next item is a prefill item as well, carries straight on into it: the stream of
 // page copies does not stop between items, only the per-row state is swapped.  Returns with t.cur at the first item it did not process.
 //
@@ -622,12 +657,16 @@ struct Widening {
 //   scores of the second stage  | second half of the first's softmax, reads of its value fragments, the copies of the page two steps further on
 //   values of the first stage   | first half of the second's softmax, half of the next step's widening, key operands of the next step's first stage
 //   scores of the next step's first stage, values of the second stage likewise.
-template <int D>
+//
+// Halves: a workgroup of eight wavefronts has one item, the first four the first half of its steps and the others the second, and the first join what both
+// have (prompts_attention_mx_kernel).  Both take the same number of steps, and so cross the same barriers: the second one's last may have no keys left.
+template <int D, bool Halves>
 __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* __restrict__ items, int n_items, Tickets& t, int* s_tk, int* ctrl,
                              char* smem, int* s_ids) {
   typedef Smem4<D> L;
   constexpr int SK = HFX_STAGE_KEYS, S = D / 16;
-  const int tid = threadIdx.x;
+  const int part = Halves ? uniform((int)threadIdx.x / HFX_WG_THREADS) : 0;
+  const int tid = Halves ? (int)threadIdx.x % HFX_WG_THREADS : (int)threadIdx.x;
   int lane = tid & 63;
   asm volatile("" : "+v"(lane));     // what follows from it is formed per run, not kept in registers through decode runs
   const int wave = uniform(tid >> 6);
@@ -655,14 +694,23 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   const int w_scales = wave * L::kRawPage + Mx<D>::kValueScales + half * Mx<D>::kHalfScales + (D == 128 ? w_of * 16 : 0);
   const int w_to = wave * L::kValuePage + w_of * (D == 128 ? 2048 : 1024) + w_i * 32 + (half ^ (w_i >> 3)) * 16;
 
-  const HfxItem item0 = items[t.cur], item1 = items[t.nxt < n_items ? t.nxt : t.cur];
+  HfxItem item0 = items[t.cur];
+  const HfxItem item1 = items[t.nxt < n_items ? t.nxt : t.cur];
+  int half_steps = 0;
+  if constexpr (Halves) {
+    half_steps = (item_steps(item0) + 1) / 2;
+    const int cut = item0.kb + half_steps * kStepKeys;
+    if (part == 0) item0.ke = min(item0.ke, cut);
+    else item0.kb = cut;
+  }
+  auto steps_of = [&](const HfxItem& item) { return Halves ? half_steps : item_steps(item); };
   bool next_ok = t.nxt < n_items && item1.type == HFX_ITEM_PREFILL;
   const unsigned inv_g = 0xffffffffu / (unsigned)G + 1u;      // h / G by a multiplication (0 for G = 1)
   auto q_rows = [&](const HfxItem& item, const WaveRows& r) { return a.q + ((long)item.rq.q_start * Hq + r.head) * D; };
   auto next_item = [&](const HfxItem& item) {
     const WaveRows r = wave_rows(item, wave);
     NextItem4 x;
-    x.left = item_steps(item);
+    x.left = steps_of(item);
     x.bt = item.rq.bt_start + (int)((unsigned)item.kb / HFX_PAGE) + wave;
     x.last = item.rq.bt_start + item.rq.n_pages - 1;
     x.head = G == 1 ? item.h0 : (int)__umulhi((unsigned)item.h0, inv_g);
@@ -744,7 +792,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   auto item_start = [&](const HfxItem& item) {
     it = item;
     kt = item.kb;
-    left = item_steps(item);
+    left = steps_of(item);
     ctx_len = item.rq.ctx_len;
     wr = wave_rows(item, wave);
   };
@@ -889,6 +937,11 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     w.l = w.sum[0];
     // hand-over
     tickets_take(t, s_tk, n_items);
+    if constexpr (Halves) {
+      join_halves<D>(w, part, lane, smem + (part == 0 ? L::kPrefill : 0) + wave * Joined<D>::kWave);
+      if (part == 0) prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
+      break;
+    }
     if (!next_ok) {
       prefill_store<D>(a, H, it, wr, w, Hq, wave, lane, stage);
       break;
@@ -960,9 +1013,34 @@ __global__ __launch_bounds__(HFX_WG_THREADS, 2) void mixed_attention_mx_kernel(c
   }
   while (t.cur < n_items) {
     if (items[t.cur].type == HFX_ITEM_DECODE) decode_run4<D, Past>(a, H, items, n_items, t, s_tk, ctrl, smem);
-    else prefill_run4<D>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ids);
+    else prefill_run4<D, false>(a, H, items, n_items, t, s_tk, ctrl, smem, s_ids);
   }
   queue_done(H, ctrl);
+}
+
+// Steps of prompts alone that have fewer items than the chip has CUs: a workgroup an item, of twice the wavefronts.
+template <int D>
+__global__ __launch_bounds__(2 * HFX_WG_THREADS, 2) void prompts_attention_mx_kernel(const HfxHeader hdr, const char* __restrict__ desc, const __bf16* __restrict__ q,
+                                                                                    const __bf16* __restrict__ pool, float* __restrict__ ws,
+                                                                                    __bf16* __restrict__ out) {
+  KArgs a;
+  a.desc = desc;
+  a.q = q;
+  a.pool = pool;
+  a.ws = ws;
+  a.out = out;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * Smem4<D>::kPrefill];
+  __shared__ __attribute__((aligned(16))) int s_ids[2 * 4 * 128];
+  const HfxHeader* H = &hdr;
+  Tickets t;
+  t.cur = (int)blockIdx.x;
+  t.nxt = 0x7fffffff;
+  t.parity = 0;
+  t.queue = t.own = false;
+  t.order = nullptr;
+  const int part = uniform((int)threadIdx.x / HFX_WG_THREADS);
+  prefill_run4<D, true>(a, H, reinterpret_cast<const HfxItem*>(a.desc + H->off_items), H->n_items, t, nullptr, nullptr, smem + part * Smem4<D>::kPrefill,
+                        s_ids + part * 4 * 128);
 }
 
 hipError_t max_resident_workgroups_mx(int head_dim, int* per_cu) {
@@ -981,6 +1059,14 @@ hipError_t launch_mixed_attention_mx(const HfxHeader& h, int grid, void* desc, c
   const __bf16* pp = static_cast<const __bf16*>(pool);
   float* wp = static_cast<float*>(ws);
   __bf16* op = static_cast<__bf16*>(out);
+  // Prompts alone whose items leave half of the CUs' wavefronts idle: an item goes to eight wavefronts where there are keys enough to share (32 / 8 heads, us: 777
+  // tokens 19.4 -> 17.7, 400 14.1 -> 13.4, 64 behind 500 15.9 -> 15.0, 200 10.8 -> 10.7, but 100 9.0 -> 9.4 and 40 8.4 -> 9.1; 64-wide heads, 700 behind
+  // 300 19.5 -> 15.9).
+  if (h.n_decode_items == 0 && h.n_items <= HFX_PLAN_WGS / 2 && h.max_ctx_len > 4 * kStepKeys) {
+    const hipError_t e = launch(h.head_dim == 128 ? prompts_attention_mx_kernel<128> : prompts_attention_mx_kernel<64>, dim3((unsigned)h.n_items),
+                                2 * HFX_WG_THREADS, stream, hk, d, qp, pp, wp, op);
+    return e != hipSuccess ? e : launch_merge(h, desc, ws, out, stream);
+  }
   void (*const kernels[])(HfxHeader, int, const char*, int*, const __bf16*, const __bf16*, float*, __bf16*) = {
       mixed_attention_mx_kernel<64, false>, mixed_attention_mx_kernel<64, true>, mixed_attention_mx_kernel<128, false>, mixed_attention_mx_kernel<128, true>};
   const hipError_t e = launch(kernels[(h.head_dim == 128 ? 2 : 0) + (h.stream_mx ? 1 : 0)], dim3(grid), HFX_WG_THREADS, stream, hk, (int)by_kind, d, ctrl, qp, pp, wp, op);

@@ -372,3 +372,25 @@ def test_which_steps_read_pages_past_the_caches():
 def test_both_pools_where_pages_go_past_the_caches(hb):
     test_both_pools_on_larger_steps(hb, 8, 8, 64, [1, 1, 1, 40], [60000, 70001, 50000, 900])
     test_both_pools_on_larger_steps(hb, 16, 8, 128, [1, 1, 33], [40000, 30001, 700])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 64), (16, 1, 128)])
+@pytest.mark.parametrize("q_len,ctx", [([1], [1]), ([64], [64]), ([65], [65]), ([33], [191]), ([128], [128]), ([129], [193]), ([300], [300]), ([2], [777]),
+                                       ([1, 31, 64], [64, 700, 65]), ([100], [2000]), ([32, 32], [1025, 63])])
+def test_prompts_alone(hb, hq, hkv, d, q_len, ctx):
+    """Steps without decodes and with few items: keys of one step, of an odd and of an even number of steps, behind earlier tokens, cut into splits or not."""
+    from tests.test_mx_cache import MAX_ABS, MEAN_ABS, dense
+    from paper_2508_15919_amd.synth import bf16_bits_to_f64
+    import torch
+    step = Step(hb, hq, hkv, d, q_len, ctx, 300 + len(q_len) + q_len[0])
+    step.kind[:] = 1
+    size, _, ws = hb.hfx_batch_desc_sizes(step.shape, step.kind, step.q_len, step.ctx_len)
+    step.host, step.dev = torch.empty(size, dtype=torch.uint8, pin_memory=True), torch.empty(size, dtype=torch.uint8, device="cuda")
+    step.ws = torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None
+    hb.hfx_build_batch_desc(step.shape, step.kind, step.q_len, step.ctx_len, step.indptr, step.pages, step.host, step.dev, torch.cuda.current_stream())
+    pool = random_pool(step)
+    q = step.bits(step.tokens, hq, d)
+    got = bf16_bits_to_f64(attend(step, q, torch.from_numpy(pool).cuda()))
+    err = np.abs(got - dense(step, bf16_bits_to_f64(q), pool))
+    assert np.isfinite(got).all() and err.max() <= MAX_ABS and err.mean() <= MEAN_ABS
