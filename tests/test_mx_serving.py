@@ -394,3 +394,32 @@ def test_prompts_alone(hb, hq, hkv, d, q_len, ctx):
     got = bf16_bits_to_f64(attend(step, q, torch.from_numpy(pool).cuda()))
     err = np.abs(got - dense(step, bf16_bits_to_f64(q), pool))
     assert np.isfinite(got).all() and err.max() <= MAX_ABS and err.mean() <= MEAN_ABS
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 64)])
+@pytest.mark.parametrize("kinds,q_len,ctx", [("decodes", [1, 1, 1], [1500, 333, 64]), ("mixed", [1, 70, 1, 33], [700, 500, 90, 33]), ("prompts", [90, 64], [900, 300]),
+                                             ("prompts", [200], [200])])
+def test_maxima_that_keep_growing(hb, hq, hkv, d, kinds, q_len, ctx):
+    """Scores with a spread of a dozen and more, keys that get larger along the context: reference exponents are outgrown again and again, and most weights vanish.
+    The queries are numbers of four significant bits and one size, so that scores are exact but for the order of their sums, and the usual bounds hold."""
+    from tests.test_mx_cache import MAX_ABS, MEAN_ABS, dense, place_tables
+    from paper_2508_15919_amd.synth import bf16_bits_to_f64, f32_to_bf16_bits
+    import torch
+    step = Step(hb, hq, hkv, d, q_len, ctx, 500 + len(q_len) + d, scale=0.6)
+    step.kind[:] = [0 if n == 1 and kinds != "prompts" else 1 for n in q_len]
+    size, _, ws = hb.hfx_batch_desc_sizes(step.shape, step.kind, step.q_len, step.ctx_len)
+    step.host, step.dev = torch.empty(size, dtype=torch.uint8, pin_memory=True), torch.empty(size, dtype=torch.uint8, device="cuda")
+    step.ws = torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None
+    hb.hfx_build_batch_desc(step.shape, step.kind, step.q_len, step.ctx_len, step.indptr, step.pages, step.host, step.dev, torch.cuda.current_stream())
+    pool = random_pool(step)
+    scales = place_tables(d)[4]                                # [16 slots][blocks]: bytes of the key scales
+    for r, c in enumerate(step.ctx_len.tolist()):
+        for t in range(c):
+            page, at = step.pages[step.indptr[r] + t // 16], scales[t % 16]
+            pool[page][:, at] -= np.uint8(5 - 5 * (t + 1) // c)
+    q = f32_to_bf16_bits(step.g.choice(np.array([-3.75, -2.5, -1.5, -1, 1, 1.25, 2, 3.5], np.float32), (step.tokens, hq, d)))
+    got = bf16_bits_to_f64(attend(step, q, torch.from_numpy(pool).cuda()))
+    err = np.abs(got - dense(step, bf16_bits_to_f64(q), pool))
+    print(f"max-abs {err.max():.3e} mean-abs {err.mean():.3e}")
+    assert np.isfinite(got).all() and err.max() <= MAX_ABS and err.mean() <= MEAN_ABS
