@@ -356,9 +356,10 @@ hfx_status hfx_read_new_kv_mx(const hfx_shape* shape, const void* mx_pool, const
                             void* k_out, void* v_out, void* stream);
 
 /*
- * hfx_mixed_paged_attention over a 4-bit pool: the same result as over a bf16 pool that holds the values that this one stands for, to rounding.  Scores and
- * the weighted sum accumulate in fp32, and softmax weights are rounded to bf16.  A query value enters as the sum of two 6-bit numbers with scales per 32
- * dimensions: exactly, where it is at least 0.26 of the largest of the 32, and otherwise to 0.001 of that one (about half of what bf16 rounds it by itself).
+ * hfx_mixed_paged_attention over a 4-bit pool: what that gives over a bf16 pool that holds the values that this one stands for, but for the rounding of softmax weights and
+ * results to bf16 (as there) and that of small query values.  Scores and the weighted sum accumulate in fp32.  A query value enters as the sum of three 6-bit numbers with
+ * scales per 32 dimensions: exactly, where it is at least 1/248 of the largest of the 32, and otherwise off by at most 1.6e-5 of that one (or 2^-126, if that is
+ * more).  A score is off by the sum of these against the keys, times softmax_scale.
  * Same descriptor, workspace, arguments and errors.
  */
 hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, const void* mx_pool, const void* host_desc,

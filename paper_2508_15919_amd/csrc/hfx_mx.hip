@@ -2,9 +2,9 @@
 // the bf16 pool, with kernels of their own for both kinds of items.
 //
 //   S^T = K . Q^T   on the scaled matrix instructions for 4 to 8 bits: the keys' codes and scale bytes go into them as they lie in the cache.  With their
-//                   other operand in 6 bits they have four times the rate of a bf16 product, and a query is taken as the sum of two 6-bit numbers
-//                   (split_query), each with a scale for 32 dimensions: half the matrix time, and no key is ever converted.  (Two 8-bit numbers would
-//                   do as well, but with an operand of 8 bits the products take twice the time: 66 clocks a 32x32x64, not 34.)
+//                   other operand in 6 bits they have four times the rate of a bf16 product, and a query is taken as the sum of three 6-bit numbers
+//                   (split_query), each with a scale for 32 dimensions: three quarters of the matrix time, and no key is ever converted.  (Two 8-bit numbers
+//                   would hold more, but with an operand of 8 bits the products take twice the time: 66 clocks a 32x32x64, not 34.)
 //   O^T = V^T . P^T on the bf16 matrix instructions: a scale belongs to a token, which is the contracted index here, so the values are widened to bf16
 //                   (every code times every scale is a bf16 number).
 #include <hip/hip_runtime.h>
@@ -30,16 +30,17 @@ constexpr int kE2M3 = 2, kE3M2 = 3, kE2M1 = 4;
 __device__ __forceinline__ i32x8 fp4_operand(const u32x4& c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
 __device__ __forceinline__ i32x8 fp6_operand(const u32x6& c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], (int)c[4], (int)c[5], 0, 0}; }
 
-// 32 query values as the sum of two sets of 6-bit numbers with scales 2^(e - 127) and 2^(e - 6 - 127).  e brings the largest magnitude into [3.875, 7.75),
-// where the nearest number of E2M3 (4 significant bits, up to 7.5, steps of 1/8 below 2) is at most 1/4 away.  A bf16 value has 8 significant bits: from 1
-// up the remainder is at most eight of its last places, which the 3 significant bits of E3M2 hold, so the two numbers are the value; a smaller value's
-// remainder is at most 1/16 and rounds by at most 2^-8, 2^-10 of the largest, half of what bf16 itself rounds that one by.  (Remainders as E2M3, whose
-// steps do not get finer with the remainder, put results 2.5e-3 off in all at 65536 keys, these 2.4e-3; the weights and the result in bf16 alone are 2.35e-3.)
+// 32 query values as the sum of three sets of 6-bit numbers with scales 2^(e - 127), 2^(e - 6 - 127) and 2^(e - 10 - 127).  e brings the largest magnitude into
+// [3.875, 7.75), where the nearest number of E2M3 (4 significant bits, up to 7.5, steps of 1/8 below 2) is at most 1/4 away.  A bf16 value has 8 significant bits: from 1
+// up the remainder is at most eight of its last places, which the 3 significant bits of E3M2 hold; a smaller value's remainder is at most 1/16 and rounds by at
+// most 2^-8, which the third number, E2M3 again, takes up in steps of 2^-13 and less.  So the three are the value from 2^-6 up, 1/248 of the largest at most, and below it are at
+// most 2^-14 away, 1.6e-5 of the largest.  (The first two alone, exact from about a quarter of the largest up and 0.001 of it away below, put results 0.004 off where some
+// channels are 8 times the others and 0.037 where they are 100 times those; bf16 weights and result make 0.0024.)
 struct Query6 {
-  u32x6 first, rest;
-  unsigned scale;          // bytes: of first, of rest
+  u32x6 n[3];
+  unsigned scale;          // bytes: of each
 };
-constexpr unsigned kRestScale = 6;
+constexpr unsigned kRestScale = 6, kLastScale = 10;
 __device__ __forceinline__ Query6 split_query(const bf16x8* q) {
   unsigned top = 0;
 #pragma unroll
@@ -48,18 +49,22 @@ __device__ __forceinline__ Query6 split_query(const bf16x8* q) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = max(top, max(u[w] & 0x7fff0000u, u[w] << 16 & 0x7fff0000u));
   }
-  const unsigned e = (unsigned)max((int)((top + 0x80000u) >> 23) - 2, (int)kRestScale + 1);
-  const float scale = __builtin_bit_cast(float, e << 23), rest_scale = __builtin_bit_cast(float, (e - kRestScale) << 23);
-  bf16x32 x, r;
+  const unsigned e = (unsigned)max((int)((top + 0x80000u) >> 23) - 2, (int)kLastScale + 1);
+  auto scale = [&](unsigned lower) { return __builtin_bit_cast(float, (e - lower) << 23); };
+  bf16x32 x;
 #pragma unroll
   for (int i = 0; i < 32; ++i) x[i] = q[i >> 3][i & 7];
-  Query6 t;
-  t.first = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, scale);
-  const f32x32 f = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(t.first, scale);
+  auto rest = [&](const f32x32& taken) {                 // (exact, and a bf16 number)
 #pragma unroll
-  for (int i = 0; i < 32; ++i) r[i] = (__bf16)((float)x[i] - f[i]);          // (exact)
-  t.rest = __builtin_amdgcn_cvt_scalef32_pk32_bf6_bf16(r, rest_scale);
-  t.scale = e | (e - kRestScale) << 8;
+    for (int i = 0; i < 32; ++i) x[i] = (__bf16)((float)x[i] - taken[i]);
+  };
+  Query6 t;
+  t.n[0] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, scale(0));
+  rest(__builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(t.n[0], scale(0)));
+  t.n[1] = __builtin_amdgcn_cvt_scalef32_pk32_bf6_bf16(x, scale(kRestScale));
+  rest(__builtin_amdgcn_cvt_scalef32_pk32_f32_bf6(t.n[1], scale(kRestScale)));
+  t.n[2] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, scale(kLastScale));
+  t.scale = e | (e - kRestScale) << 8 | (e - kLastScale) << 16;
   return t;
 }
 
@@ -166,17 +171,12 @@ struct DecodeLane4 {
   int key, key_scale, value, value_scale;
 };
 
-template <int D>
-struct DecodeQuery4 {
-  u32x6 q[2];             // first numbers, remainders
-  unsigned scale;         // bytes: of either
-};
-
-template <int D>
-__device__ __forceinline__ f32x4 decode_scores4(const u32x4& k, unsigned ks, const DecodeQuery4<D>& q) {
+__device__ __forceinline__ f32x4 decode_scores4(const u32x4& k, unsigned ks, const Query6& q) {
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[0]), s, kE2M1, kE2M3, 0, (int)ks, 0, (int)q.scale);
-  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(k), fp6_operand(q.q[1]), s, kE2M1, kE3M2, 0, (int)ks, 1, (int)q.scale);
+  const i32x8 a = fp4_operand(k);
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, fp6_operand(q.n[0]), s, kE2M1, kE2M3, 0, (int)ks, 0, (int)q.scale);
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, fp6_operand(q.n[1]), s, kE2M1, kE3M2, 0, (int)ks, 1, (int)q.scale);
+  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, fp6_operand(q.n[2]), s, kE2M1, kE2M3, 0, (int)ks, 2, (int)q.scale);
   return s;
 }
 
@@ -204,7 +204,7 @@ __device__ __forceinline__ float decode_weights(const float* s, float sl2, float
 }
 
 template <int D>
-__device__ __forceinline__ void decode_pair4(const char* ring, const DecodeLane4& a, const DecodeQuery4<D>& q, DecodeState4<D>& w, float sl2, bool first, bool tail,
+__device__ __forceinline__ void decode_pair4(const char* ring, const DecodeLane4& a, const Query6& q, DecodeState4<D>& w, float sl2, bool first, bool tail,
                                              int nv) {
   const u32x4 ka = *reinterpret_cast<const u32x4*>(ring + a.key), kb = *reinterpret_cast<const u32x4*>(ring + a.key + 64);
   const unsigned ea = *reinterpret_cast<const uint8_t*>(ring + a.key_scale);
@@ -215,7 +215,7 @@ __device__ __forceinline__ void decode_pair4(const char* ring, const DecodeLane4
     v[i] = *reinterpret_cast<const u32x4*>(ring + a.value + i * 256);
     vs[i] = *reinterpret_cast<const u32x4*>(ring + a.value_scale + i * 16);
   }
-  const f32x4 sa = decode_scores4<D>(ka, ea, q), sb = decode_scores4<D>(kb, eb, q);
+  const f32x4 sa = decode_scores4(ka, ea, q), sb = decode_scores4(kb, eb, q);
   float s[8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -259,18 +259,13 @@ __device__ __forceinline__ void decode_pair4(const char* ring, const DecodeLane4
 
 // Query operands of a kv-head's q-heads (column n), zero past the group: lane group j has 32 dimensions, 32j .. 32j + 31, or zeros past the head's.
 template <int D>
-__device__ __forceinline__ DecodeQuery4<D> decode_query4(const __bf16* q, const HfxItem& item, int g, int Hq, int G, int n, int j) {
+__device__ __forceinline__ Query6 decode_query4(const __bf16* q, const HfxItem& item, int g, int Hq, int G, int n, int j) {
   const int hh = n < G ? n : G - 1;
   const __bf16* row = q + ((long)item.rq.q_start * Hq + g * G + hh) * D + (j & (Mx<D>::kGroups - 1)) * 32;
   bf16x8 x[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = keep_first(ld16(row + i * 8), n < G && j < Mx<D>::kGroups ? 8 : 0);
-  const Query6 t = split_query(x);
-  DecodeQuery4<D> r;
-  r.q[0] = t.first;
-  r.q[1] = t.rest;
-  r.scale = t.scale;
-  return r;
+  return split_query(x);
 }
 
 // Runs the decode item t.cur and carries on for as long as the workgroup's next item is a decode item too.
@@ -320,7 +315,7 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
     };
 #pragma unroll 1
     for (int i = 0; i < kRingPairs - 1 && next < d.pe; ++i) copy_pair();
-    const DecodeQuery4<D> qf = decode_query4<D>(a.q, it, d.g, Hq, G, n, j);
+    const Query6 qf = decode_query4<D>(a.q, it, d.g, Hq, G, n, j);
     // the record of the next item and, if it is a decode item, this wavefront's share of it
     const HfxItem nx = items[t.nxt < n_items ? t.nxt : t.cur];
     const bool carry_on = t.nxt < n_items && nx.type == HFX_ITEM_DECODE;
@@ -373,7 +368,7 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
 // Bound: the clock that power leaves, 1.8 to 1.9 GHz on long chunks; of its cycles the matrix cores are busy for 53 %, the vector unit by its
 // instructions for about as many, LDS for 33 %.  Four chunks of 2048 rows behind 0 to 12288 tokens and 32 decodes, 32 / 8 heads of 128: 695 to 720 us by the card, 1337 to 1385 TFLOP/s (over
 // the bf16 pool 800 to 850; a library product of 16384^3 has 1485); on zeros, which take less power, the same cycles run in 595 us.
-//   S^T[key][row]  = K . Q^T     32x32x64 scaled, keys' codes against the two numbers of the queries
+//   S^T[key][row]  = K . Q^T     32x32x64 scaled, keys' codes against the three numbers of the queries
 //   O^T[d][row]   += V^T . P^T   32x32x16 bf16, as over the bf16 pool
 // ----------------------------------------------------------------------------------------------
 template <int D>
@@ -393,8 +388,7 @@ constexpr int kStepKeys = 64;
 template <int D>
 struct PrefillWave4 {
   f32x16 o[D / 32];            // O^T accumulators per 32-dimension block
-  u32x6 q[D / 64][2];          // of 64 dimensions: first numbers, remainders
-  unsigned qs;                 // their scale bytes, in that order
+  Query6 q[D / 64];            // of 64 dimensions
   float m, l;                  // reference exponent (base-2 domain); running sum (when the item is done)
   f32x4 sum;                   // running sum of this lane's weights, four times
 };
@@ -419,16 +413,22 @@ __device__ __forceinline__ Keys4<D> read_keys4(const char* stage, int k_lane, in
   return r;
 }
 
-// Matrix instruction number i of a stage's scores: 64 dimensions i / 2, the first numbers or the remainders.  (The empty asm holds it where it is: the
+// Matrix instructions of a stage's scores.
+template <int D>
+constexpr int kScoreProducts = 3 * (D / 64);
+// Number i of them: 64 dimensions i / 3, number i % 3 of the queries.  (The empty asm holds it where it is: the
 // compiler takes it for an ordinary function of its operands and moves it down to where the result is used, out of the softmax it is meant to run beside.)
 template <int D>
 __device__ __forceinline__ void score_product(const PrefillWave4<D>& w, const Keys4<D>& k, int i, f32x16& s) {
-  const i32x8 a = fp4_operand(k.k[i / 2]), b = fp6_operand(w.q[i / 2][i % 2]);
-  const int ks = (int)k.scale, qs = (int)w.qs;
+  const Query6& q = w.q[i / 3];
+  const i32x8 a = fp4_operand(k.k[i / 3]), b = fp6_operand(q.n[i % 3]);
+  const int ks = (int)k.scale, qs = (int)q.scale;
   if (i == 0) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE2M3, 0, ks, 0, qs);
   if (i == 1) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE3M2, 0, ks, 1, qs);
-  if (i == 2) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE2M3, 2, ks, 2, qs);
-  if (i == 3) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE3M2, 2, ks, 3, qs);
+  if (i == 2) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE2M3, 0, ks, 2, qs);
+  if (i == 3) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE2M3, 2, ks, 0, qs);
+  if (i == 4) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE3M2, 2, ks, 1, qs);
+  if (i == 5) s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, s, kE2M1, kE2M3, 2, ks, 2, qs);
   asm volatile("" : "+v"(s));
 }
 
@@ -442,9 +442,9 @@ struct Nothing {
   __device__ __forceinline__ void operator()(int) const {}
 };
 
-// Which weights are formed where (see Share): of a stage's 16 the value phase takes 12 (64-wide heads: 10), the score phase, half as long here, the others at
-// its beginning, so that the rounded weights are known well before it ends.  Two portions go behind each instruction of the score phase.  (8, 10, 12, 14 and
-// 16 in the value phase: long chunks 718.6, 719.7, 715.2, 717.1 and 719.0 us.)
+// Which weights are formed where (see Share): of a stage's 16 the value phase takes 12 (64-wide heads: 10), the score phase, three quarters as long here, the others
+// at its beginning, so that the rounded weights are known well before it ends.  It has its portions spread over its instructions, one or two behind each.  (8, 10, 12 and
+// 14 in the value phase: four chunks of 2048 rows 780.0, 781.1, 780.5 and 780.9 us.)
 template <int D>
 struct Share4;
 template <>
@@ -519,17 +519,17 @@ __device__ __forceinline__ bf16x8 summing_operand(int lane) {
 template <int D, class Between>
 __device__ __forceinline__ f32x16 scores_phase4(const PrefillWave4<D>& w, Keys4<D>& k, int j, bf16x8* frag, const f32x16& cur, Weighing4& wt, float sl2,
                                                 const char* values, int v_lane, Between between) {
-  constexpr int S = D / 16;
+  constexpr int S = D / 16, P = kScoreProducts<D>;
   keys_ready<D>(k, j);
   f32x16 acc;
 #pragma unroll
   for (int v = 0; v < 16; ++v) acc[v] = 0.f;
 #pragma unroll
-  for (int i = 0; i < S / 2; ++i) {
+  for (int i = 0; i < P; ++i) {
     score_product<D>(w, k, i, acc);
     between(i);
 #pragma unroll
-    for (int h = 2 * i; h < 2 * i + 2; ++h) {
+    for (int h = i * S / P; h < (i + 1) * S / P; ++h) {
       frag[h] = value_fragment4<D>(values, h, v_lane);
       wt.portion(h == 0 ? Share4<D>::values[S - 1] : Share4<D>::scores[h - 1], Share4<D>::scores[h], Share4<D>::scores[h + 1], cur, sl2, w.m);
     }
@@ -566,14 +566,8 @@ __device__ __forceinline__ void query_load4(bf16x8 (*x)[4], const __bf16* q, int
 
 template <int D>
 __device__ __forceinline__ void query_rows4(PrefillWave4<D>& w, const bf16x8 (*x)[4]) {
-  w.qs = 0;
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    const Query6 t = split_query(x[i]);
-    w.q[i][0] = t.first;
-    w.q[i][1] = t.rest;
-    w.qs |= t.scale << (16 * i);
-  }
+  for (int i = 0; i < D / 64; ++i) w.q[i] = split_query(x[i]);
 }
 
 __device__ __forceinline__ int item_steps(const HfxItem& it) { return (int)((unsigned)(it.ke - it.kb + kStepKeys - 1) / kStepKeys); }
@@ -839,7 +833,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
 #pragma unroll
     for (int v = 0; v < 16; ++v) s0[v] = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) score_product<D>(w, keys, i, s0);
+    for (int i = 0; i < kScoreProducts<D>; ++i) score_product<D>(w, keys, i, s0);
     keys = read_keys4<D>(smem + raw_g + 2 * L::kRawPage, k_lane, s_lane);
     mask_stage(s0, kt);
     w.m = fmaxf(HFX_M_NONE, row_max(s0, sl2)) + kHeadroom;
