@@ -360,6 +360,7 @@ hfx_status hfx_read_new_kv_mx(const hfx_shape* shape, const void* mx_pool, const
  * results to bf16 (as there) and that of small query values.  Scores and the weighted sum accumulate in fp32.  A query value enters as the sum of three 6-bit numbers with
  * scales per 32 dimensions: exactly, where it is at least 1/248 of the largest of the 32, and otherwise off by at most 1.6e-5 of that one (or 2^-126, if that is
  * more).  A score is off by the sum of these against the keys, times softmax_scale.
+ * A query that is not finite gives NaN to its head and row, and to no other.
  * Same descriptor, workspace, arguments and errors.
  */
 hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, const void* mx_pool, const void* host_desc,

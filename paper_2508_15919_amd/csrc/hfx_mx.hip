@@ -64,7 +64,7 @@ __device__ __forceinline__ Query6 split_query(const bf16x8* q) {
   t.n[1] = __builtin_amdgcn_cvt_scalef32_pk32_bf6_bf16(x, scale(kRestScale));
   rest(__builtin_amdgcn_cvt_scalef32_pk32_f32_bf6(t.n[1], scale(kRestScale)));
   t.n[2] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, scale(kLastScale));
-  t.scale = e | (e - kRestScale) << 8 | (e - kLastScale) << 16;
+  t.scale = top >= 0x7f800000u ? 0xffffffu : e | (e - kRestScale) << 8 | (e - kLastScale) << 16;       // 255 makes the products NaN, which 6 bits cannot say
   return t;
 }
 
@@ -491,19 +491,42 @@ struct Weighing4 {
   }
 };
 
-// The weights of a stage, all known, as operands; taken again where the scores have outgrown the reference exponent.
+// Whether x holds in either lane of a row, n or n + 32.
+__device__ __forceinline__ bool in_row(bool x) {
+  const Pair32 p = swap32(x ? 1.0f : 0.0f);
+  return p.lo + p.hi > 0.0f;
+}
+
+// The weights of a stage, all known, as operands; taken again in the rows whose scores have outgrown the reference exponent.  So does a weight that is
+// not finite look, which the product that sums the weights (summing_operand) would multiply by zero into the sums of other rows: where
+// one is left, by a query that is not finite or a score that overflows, the row's accumulators become NaN for good and its weights zero.  (By integer operations:
+// the file is compiled with -fno-honor-nans.)
 template <int D>
 __device__ __forceinline__ void settle_weights4(PrefillWave4<D>& w, const f32x16& s, bf16x8* pb, const Weighing4& wt, float sl2) {
   pb[0] = wt.fragment(0);
   pb[1] = wt.fragment(1);
   if (__builtin_expect(__builtin_amdgcn_ballot_w64(wt.large()) != 0, 0)) {
-    const float m = fmaxf(w.m, row_max(s, sl2) + kHeadroom);
-    const float alpha = fast_exp2(w.m - m);
-    w.sum *= alpha;
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b) w.o[b] *= alpha;
+    const float raised = fmaxf(w.m, row_max(s, sl2) + kHeadroom);
+    const float m = in_row(wt.large()) ? raised : w.m;
+    unsigned alpha = __builtin_bit_cast(unsigned, fast_exp2(w.m - m));
     w.m = m;
     weights(s, sl2, m, pb);
+    u32x4 p[2] = {__builtin_bit_cast(u32x4, pb[0]), __builtin_bit_cast(u32x4, pb[1])};
+    bool lost = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned u = p[i / 4][i % 4];
+      lost |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
+    }
+    const unsigned keep = in_row(lost) ? 0u : ~0u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) pb[i] = __builtin_bit_cast(bf16x8, p[i] & keep);
+    alpha = (alpha & keep) | (0x7fc00000u & ~keep);
+    asm volatile("" : "+v"(alpha));
+    const float a = __builtin_bit_cast(float, alpha);
+    w.sum *= a;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) w.o[b] *= a;
   }
 }
 

@@ -68,3 +68,36 @@ def test_long_contexts_as_a_ratio(hb, hq, hkv, d, q_len, ctx):
     found = off(got, dense(step, bf16_bits_to_f64(q), pool))
     print(f"{found:.5f} off")
     assert found <= BOUND
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,q_len,ctx", [
+    (8, 2, 128, [1, 40, 1], [333, 1200, 90]),
+    (8, 2, 64, [1, 33, 70], [40, 33, 700]),
+    (4, 1, 128, [130], [900]),                   # prompts alone, an item's steps in two halves
+    (8, 1, 128, [70, 1], [6000, 5000]),          # items split along the keys
+    (4, 4, 64, [100], [100]),
+])
+def test_queries_that_are_not_finite_stay_by_themselves(hb, hq, hkv, d, q_len, ctx):
+    """A head of a row with an infinity or a NaN gives NaN there, as over the bf16 pool; every other head and row keeps its bits.  (One whose scores overflow:
+    nothing is said of it.)"""
+    step = Step(hb, hq, hkv, d, q_len, ctx, 370)
+    pool = step.torch.from_numpy(random_pool(step)).cuda()
+    q = step.bits(step.tokens, hq, d)
+    want = attend(step, q, pool)
+    assert np.isfinite(bf16_bits_to_f64(want)).all()
+    first = int(np.concatenate(([0], np.cumsum(q_len)))[np.argmax(q_len)])         # of the longest chunk
+    bad = {(first, 0): 0x7FC0, (first + 5, 1): 0x7F80, (first + 21, 1): 0xFF80, (first + 20, 2): 0xFFFF, (first + 32, 3): 0x7F80}
+    if first > 0:
+        bad[0, 1] = 0x7FC0                                                         # a decode
+    over = (first + 8, 2)
+    for (row, head), bits in bad.items():
+        q[row, head, (7 * row + head) % d] = bits
+    q[over] = 0x7F7F
+    got = attend(step, q, pool)
+    others = np.ones((step.tokens, hq), bool)
+    others[over] = False
+    for at in bad:
+        others[at] = False
+        assert np.isnan(bf16_bits_to_f64(got[at])).all(), at
+    assert np.array_equal(got[others], want[others]), np.argwhere((got != want).any(-1) & others).tolist()
