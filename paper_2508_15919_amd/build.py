@@ -5,6 +5,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -12,29 +13,42 @@ LIB = os.path.join(HERE, "libhfxattn.so")
 # The name says for which Python it was built, so that another one does not load it.
 CALL_LIB = os.path.join(HERE, "_hfxcall" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["hfx_kernels.hip", "hfx_append.hip", "hfx_mx.hip", "hfx_api.cpp", "hfx_plan.cpp", "hfx_sched.cpp"]
-# -fno-honor-nans: no floating-point operation in the kernels is ever fed a NaN (possibly-NaN scores
-# are masked through integer selects first), and without it every max carries a canonicalising twin.
+# Sources with attention kernels, and their own flag.  -fno-honor-nans: without it every max of a softmax carries a canonicalising twin.  Nothing in them asks a
+# floating-point operation whether a value is NaN: scores that may be (of unused slots, which hold anything) are masked, and weights that may be are told apart, by integer
+# operations on bits that the compiler cannot see through.  Not for the appends over a projection's output, which may hold anything and of which that is asked.
 # Device code only: the host side validates its floating-point arguments with NaN tests.
+ATTENTION = ("hfx_kernels.hip", "hfx_mx.hip")
+ATTENTION_FLAGS = ["-Xarch_device", "-fno-honor-nans"]
 # The atomic optimizer is switched off: it rewrites thread 0's ticket fetch into a form that
 # waits for the counter's reply on the spot, and the reply is only needed an item later.
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Xarch_device", "-fno-honor-nans",
-         "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+
+
+def _checked(ran) -> str:
+    """What the compiler had to say, for (process, stderr) pairs; raises if one failed."""
+    noise = "is not a recognized feature for this target"
+    err = "\n".join(l for _, text in ran for l in text.splitlines() if noise not in l)
+    if any(p.returncode != 0 for p, _ in ran):
+        raise RuntimeError("hipcc failed:\n" + err)
+    return err
 
 
 def build(verbose: bool = False, extra_flags=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *FLAGS, *extra_flags, "-o", LIB]
-    for s in SOURCES:
-        path = os.path.join(CSRC, s)
-        cmd += (["-x", "hip", path] if s.endswith(".cpp") else [path])
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + err)
+    with tempfile.TemporaryDirectory() as tmp:
+        objects, commands = [], []
+        for s in SOURCES:
+            objects.append(os.path.join(tmp, s + ".o"))
+            commands.append([hipcc, *FLAGS, *(ATTENTION_FLAGS if s in ATTENTION else ()), *extra_flags, "-c", "-o", objects[-1],
+                             *(["-x", "hip"] if s.endswith(".cpp") else []), os.path.join(CSRC, s)])
+        link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objects]
+        if verbose:
+            print("\n".join(" ".join(c) for c in commands + [link]), flush=True)
+        running = [subprocess.Popen(c, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True) for c in commands]
+        err = _checked([(p, p.communicate()[1]) for p in running])
+        res = subprocess.run(link, capture_output=True, text=True)
+        err += _checked([(res, res.stderr)])
     if verbose and err.strip():
         print(err, file=sys.stderr)
     build_call(verbose)

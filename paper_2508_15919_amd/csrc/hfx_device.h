@@ -30,7 +30,7 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 __device__ __forceinline__ bf16x8 ld16(const __bf16* p) { return *reinterpret_cast<const bf16x8*>(p); }
 
 // `x` where keep, -inf elsewhere, as a select on the bit pattern: the scores of masked keys may be
-// NaN (unused slots hold anything), and the file is compiled with -fno-honor-nans, under which a
+// NaN (unused slots hold anything), and attention is compiled with -fno-honor-nans, under which a
 // floating-point select of a NaN is not defined.
 __device__ __forceinline__ float keep_or_neg_inf(float x, bool keep) {
   const unsigned u = keep ? __builtin_bit_cast(unsigned, x) : 0xff800000u;
