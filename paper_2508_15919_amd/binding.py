@@ -196,6 +196,8 @@ def make_rope(cos_sin, rot_dim: int, interleaved: bool = False) -> hfx_rope:
     """The rotation by a table [positions, rot_dim] of fp32 on the GPU: the cosines of a position's angles, then their sines."""
     if cos_sin.dim() != 2 or cos_sin.shape[1] != rot_dim or cos_sin.element_size() != 4 or not cos_sin.is_floating_point() or not cos_sin.is_contiguous():
         raise ValueError("cos_sin is a contiguous fp32 table [positions, rot_dim]")
+    if not cos_sin.is_cuda:                        # (the kernels read it: an address in host memory would fault there)
+        raise ValueError("cos_sin is on the GPU")
     rope = hfx_rope(cos_sin.data_ptr(), cos_sin.shape[0], int(rot_dim), int(bool(interleaved)))
     rope.table = cos_sin
     return rope
