@@ -253,17 +253,20 @@ __device__ __forceinline__ DecodeWave decode_wave(const int* __restrict__ bt, co
 
 // Combines a decode item's wavefronts and stores the result: wavefront partials (o[b][v] is dimension 16b + 4j + v of q-head n of the
 // wavefront's kv-head, m and l its reference exponent and running sum) go through LDS, and the token partitions of each head are joined into
-// normalised bf16 rows or, where the item is one split of a group, into (m, l, acc) partial rows.  A wavefront's 16 rows of D + 4 floats lie `stride` bytes
-// behind those of the one before it.
+// normalised bf16 rows or, where the item is one split of a group, into (m, l, acc) partial rows.  A wavefront's 16 rows of D + 4 floats lie Stride bytes
+// behind those of the one before it, or (0) directly.
 constexpr int decode_part_bytes(int D) { return 4 * 16 * (D + 4) * 4; }     // LDS that they take without gaps
-template <int D>
+template <int D, int Stride = 0>
 __device__ __forceinline__ void decode_store(const KArgs& a, const HfxHeader* H, const HfxItem& it, const f32x4* o, float m, float l, int Hq, int G,
-                                             int tid, int wave, int n, int j, char* smem, int stride = decode_part_bytes(D) / 4) {
+                                             int tid, int wave, int n, int j, char* smem) {
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
 
   constexpr int PS = D + 4;
-  auto part = [&](int w, int head) { return reinterpret_cast<float*>(smem + w * stride) + head * PS; };
+  auto part = [&](int w, int head) {
+    if constexpr (Stride == 0) return reinterpret_cast<float*>(smem) + (w * 16 + head) * PS;
+    else return reinterpret_cast<float*>(smem + w * Stride) + head * PS;
+  };
   if (n < G) {
     float* dst = part(wave, n);
 #pragma unroll

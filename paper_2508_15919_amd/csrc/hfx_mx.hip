@@ -351,7 +351,7 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
       at = at == kRing - 2 * kPage ? 0 : at + 2 * kPage;
     }
     tickets_publish(t, pending, s_tk, ctrl, H);
-    decode_store<D>(a, H, it, w.o, w.m, w.l, Hq, G, tid, wave, n, j, smem, kRing);
+    decode_store<D, kRing>(a, H, it, w.o, w.m, w.l, Hq, G, tid, wave, n, j, smem);
     __syncthreads();                  // frees the LDS partials; the ticket was published before the barrier in decode_store
     tickets_take(t, s_tk, n_items);
     if (!carry_on) break;
