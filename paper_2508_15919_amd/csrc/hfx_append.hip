@@ -162,7 +162,7 @@ __device__ __forceinline__ void store_row(uint16_t* p, const u32x4& x) {
 constexpr int kQueries = 4;
 
 // Which (run, kv-head) a workgroup takes.  Workgroups go to the dies by their index modulo 8; of 128 in a row a die takes 16 that follow each other, so
-// that the heads of a run, which share its angles and rows, meet in the same L2 (8224 rows of 32 q-heads: 32.4 us; 34.2 with four in a row, 39.5 with one).
+// that the heads of a run, which share its angles and rows, meet in the same L2 (8224 rows of 32 q-heads on buffers that stay, 32.4 us; 34.2 with four in a row, 39.5 with one).
 __device__ __forceinline__ bool run_and_head(int n_runs, int heads, int& index, int& g) {
   constexpr unsigned kDies = HFX_QUEUE_CLASSES, kRow = 16;
   const unsigned all = (unsigned)heads * (unsigned)n_runs;
@@ -179,9 +179,10 @@ __device__ __forceinline__ bool run_and_head(int n_runs, int heads, int& index, 
 // its loads may be in flight for.  T = 2 D threads have all 16 tokens at once, and pass the values through LDS, where a page has the tokens of a dimension
 // side by side.  T = 64, for steps whose runs are of a few tokens: a wavefront goes round, values go to their bytes straight from the registers, and the
 // two parts are the two wavefronts of one workgroup.
-// Bound by memory where there is much to do (32 q-heads, 8 kv-heads, 128 wide, 8224 rows in long chunks: 206 MB in 39.2 us on changing buffers, 5.3 TB/s; a
-// plain copy has 4.9), and by the chain of its loads (record of the run, then rows and angles) where there is little (four decodes: 3.6 us, of which an empty kernel
-// takes 1.5; 256 decodes into 4-bit pages 5.6).  With keys, values and queries in turn in one wavefront those were 6.0 and 7.5 us.
+// Bound by memory where there is much to do (32 q-heads, 8 kv-heads, 128 wide, 8224 rows in long chunks: 206 MB in 38.6 us on changing buffers, 5.3 TB/s; a
+// plain copy has 4.9), and by two loads that wait for each other (the run's record beside its position, then rows beside angles) and its stores where there is little (four decodes: 3.8 us, of
+// which an empty kernel takes 1.5; 256 decodes into 4-bit pages 5.8).  A run of one token fills 16 of a wavefront's 64 lanes, 8 on 64-wide heads; the others do its work again and store nothing.
+// With keys, values and queries in turn in one wavefront those were 6.0 and 7.5 us.
 template <int D, bool Four, bool Interleaved, int T, bool Past>
 __global__ __launch_bounds__(T == 64 ? 128 : T) void rope_append_kernel(const RopeAppend a) {
   constexpr bool kFew = T == 64;

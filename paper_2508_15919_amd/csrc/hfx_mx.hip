@@ -193,6 +193,8 @@ __device__ __forceinline__ float column_max(float x) {
   return max_xor32(x);
 }
 
+// Eight weights, rounded to bf16 for the product with the values (which with their scales fit no other 16-bit type), and their sum as they were: the roundings, 2^-9 each at
+// most and as many up as down, are those of the bf16 pool's decode items.
 __device__ __forceinline__ float decode_weights(const float* s, float sl2, float m, bf16x8& pb) {
   float p[8];
 #pragma unroll
@@ -365,9 +367,9 @@ __device__ void decode_run4(const KArgs& a, const HfxHeader* H, const HfxItem* _
 // wavefront): the wavefront copies its page's block into a ring of raw slots with direct-to-LDS loads, two steps ahead of its use at least; key codes are
 // read from there as operands by all four, and the value codes are widened to bf16 by the wavefront that copied them, a step ahead of
 // their use, into one of two slots in operand order.  So each value is widened once a workgroup, not once a wavefront.
-// Bound: the clock that power leaves, 1.8 to 1.9 GHz on long chunks; of its cycles the matrix cores are busy for 53 %, the vector unit by its
-// instructions for about as many, LDS for 33 %.  Four chunks of 2048 rows behind 0 to 12288 tokens and 32 decodes, 32 / 8 heads of 128: 695 to 720 us by the card, 1337 to 1385 TFLOP/s (over
-// the bf16 pool 800 to 850; a library product of 16384^3 has 1485); on zeros, which take less power, the same cycles run in 595 us.
+// Bound: on long chunks the matrix cores are busy for 58 % of the cycles, and vector instructions, of which a third widen values, take about as many without overlapping
+// them well; and the clock that power leaves, 1.77 GHz.  Four chunks of 2048 rows behind 0 to 12288 tokens and 32 decodes, 32 / 8 heads of 128: 780 to 788 us, 1222 to 1235 TFLOP/s
+// (over the bf16 pool 828 on the same card; a library product of 16384^3 has 1485); on zeros, which take less power, 619 us.
 //   S^T[key][row]  = K . Q^T     32x32x64 scaled, keys' codes against the three numbers of the queries
 //   O^T[d][row]   += V^T . P^T   32x32x16 bf16, as over the bf16 pool
 // ----------------------------------------------------------------------------------------------
@@ -738,7 +740,7 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
   };
   // The stream of page copies: the steps of the current item and then those of the next.  Page ids come in lots of up to 64 steps, into LDS by the same
   // kind of load as the pages (with a lot in a register the compiler waited for it, and with it for every copy in flight, wherever the paths of
-  // the step loop meet: a 4096-row chunk behind 61440 tokens took 862 us); the next lot is asked for as soon as one is begun.
+  // the step loop meet: a 4096-row chunk behind 61440 tokens took 862 us, 795 without, with queries of two numbers); the next lot is asked for as soon as one is begun.
   NextItem4 nx = next_item(item1);
   int left_to_ask, ask_bt, ask_last, ask_head;
   auto ask_start = [&](const NextItem4& x) {
@@ -797,9 +799,9 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
     }
   };
   // Workgroups b and b + 256 share a CU, and where both have something to issue the older one goes first: left to that, the older half of a long step's
-  // workgroups ended at 710 us and the younger at 895.  So the younger one has the higher priority in two of three of its steps (in one of two, three of
-  // four and all: 816, 819 and 835 us; none: 838; two of three: 803).  Where prefill items do not fill two rounds, the older workgroups have the
-  // largest ones and rightly go first (64-wide heads, 488 prefill items: 41.5 us, 46.5 with turns).
+  // workgroups ended at 710 us and the younger at 895.  So the younger one has the higher priority in two of three of its steps (that step
+  // 869 us; in one of two, three of four and all: 875, 875 and 896; none: 904).  Where prefill items do not fill two rounds, the older workgroups have the
+  // largest ones and rightly go first (a prompt of 2500 tokens 56.4 us, 60.8 with turns; two chunks of 2048 on 64-wide heads, and steps of a few hundred rows beside decodes, either way).
   const bool turns = gridDim.x == HFX_PLAN_WGS && blockIdx.x >= HFX_PLAN_WGS / 2 && H->n_prefill_items >= 2 * HFX_PLAN_WGS;
   int turn = 0;
   PrefillWave4<D> w;
@@ -981,9 +983,9 @@ __device__ void prefill_run4(const KArgs& a, const HfxHeader* H, const HfxItem* 
 
 // Steps whose decode work outweighs their prefill work have a queue that keeps the two on different CUs, for the sake of the decodes' stream of a bf16 pool.
 // Here that stream is a quarter as long, and where every item is dealt (two a workgroup) what counts is that the workgroups end together: prefill
-// items go first, the largest at the front, and the decode items behind them.  (us, the queue's own order and this one: 21 decodes and a 300-token prompt 18.8,
-// 16.6; 32 decodes and 777 tokens 38.0, 32.9; 64-wide heads, 48 decodes and three chunks 41.7, 38.1; 32 decodes of 8k to 64k tokens and 1024
-// rows behind 8192 on 8 / 1 heads 127, 72.  Queues that go on behind the dealt items keep their order: 200 decodes and two chunks 296, 327.)
+// items go first, the largest at the front, and the decode items behind them.  (us, the queue's own order and this one: 21 decodes and a 300-token prompt 19.9,
+// 18.5; 32 decodes and 777 tokens 38.3, 30.8; 64-wide heads, 48 decodes and three chunks 40.9, 38.3; 32 decodes of 8k to 64k tokens and 1024
+// rows behind 8192 on 8 / 1 heads 149, 80.  Queues that go on behind the dealt items keep their order: with queries of two numbers 200 decodes and two chunks took 296, 327.)
 //
 // Place in the queue of item number `rank` in that order.  The queue gives the prefill items the workgroups of the first `pair` CUs, in both rounds, the
 // decode items the others, and what is left over follows.  Any two ranks have different places, whatever the queue is.
@@ -1076,9 +1078,9 @@ hipError_t launch_mixed_attention_mx(const HfxHeader& h, int grid, void* desc, c
   const __bf16* pp = static_cast<const __bf16*>(pool);
   float* wp = static_cast<float*>(ws);
   __bf16* op = static_cast<__bf16*>(out);
-  // Prompts alone whose items leave half of the CUs' wavefronts idle: an item goes to eight wavefronts where there are keys enough to share (32 / 8 heads, us: 777
-  // tokens 19.4 -> 17.7, 400 14.1 -> 13.4, 64 behind 500 15.9 -> 15.0, 200 10.8 -> 10.7, but 100 9.0 -> 9.4 and 40 8.4 -> 9.1; 64-wide heads, 700 behind
-  // 300 19.5 -> 15.9).
+  // Prompts alone whose items leave half of the CUs' wavefronts idle: an item goes to eight wavefronts where there are keys enough to share (32 / 8 heads, us, with four
+  // and with eight: 777 tokens 20.5, 18.6; 400 14.6, 14.1; 64 behind 500 16.5, 15.9; 200 11.4, 11.3; but 100 9.4, 9.8 and 40 8.3, 9.5; 64-wide heads, 700 behind
+  // 300 18.9, 15.7).
   if (h.n_decode_items == 0 && h.n_items <= HFX_PLAN_WGS / 2 && h.max_ctx_len > 4 * kStepKeys) {
     const hipError_t e = launch(h.head_dim == 128 ? prompts_attention_mx_kernel<128> : prompts_attention_mx_kernel<64>, dim3((unsigned)h.n_items),
                                 2 * HFX_WG_THREADS, stream, hk, d, qp, pp, wp, op);
