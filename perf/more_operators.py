@@ -184,7 +184,7 @@ def run(s):
         x, times = s["x"], s.get("times")
         hb.hfx_quantise_rows(hb.HFX_ACT_SILU if entry == "silu_matmul" else hb.HFX_ACT_NONE, rows, k, x, x.stride(0), times,
                              0 if times is None else times.stride(0), None, s["codes"], s["scales"], stream)
-    hb.hfx_matmul_q8(s["handle"], rows, s["codes"], k, s["scales"], s["out"], case["n"], case["fp32"], stream)
+    hb.hfx_matmul_rows(s["handle"], rows, s["codes"], k, s["scales"], s["out"], case["n"], case["fp32"], stream)
     return (s["sum"], s["out"]) if entry == "norm_matmul" else (s["out"],)
 
 
