@@ -368,6 +368,83 @@ hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, c
                                          void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Between two attention calls: the norm of the residual stream, rows in 8 bits, and their products
+ * with weights in 8 bits.
+ *
+ * Rows in 8 bits: codes, int8 [rows][cols], and a scale, fp32, for each row; a value stands as
+ * code * scale.  With top the largest magnitude of the row (2^-100 if it is less) the scale is
+ * top / 127 and a code the nearest whole number, ties to even, to the value times 127 / top, so
+ * codes lie in [-127, 127].  A row with a value that is not finite has NaN for its scale and codes of zero.
+ * Row lengths (cols, k) are multiples of 16 from 16 to 131056; strides are in elements, no less
+ * than the row and at most 4194304; there are at most 2097152 rows.  Calls with no rows do nothing.
+ * ---------------------------------------------------------------------------------------- */
+
+/* A norm's weight. */
+typedef struct {
+  const void* weight;    /* [device] bf16 [cols], 16-byte aligned */
+  int32_t cols;
+  float eps;             /* >= 0 */
+} hfx_norm;
+
+/*
+ * Root-mean-square norm of the residual stream: h = x + residual, rounded to bf16, r = (mean of h^2 + eps)^(-1/2), result h r weight
+ * for each row.  (The step of a layer ahead of its projections, Section 2.1.)  The squares are summed in 64 bits.
+ *   rows         rows of x
+ *   x            [device] bf16, row i at x + i * x_stride; strides are multiples of 8
+ *   residual     [device] bf16, as x; NULL (with sum NULL): h is x
+ *   sum          [device] bf16 [rows][cols]: takes h.  May be x or residual itself if that is packed
+ *   out          [device] bf16 [rows][cols]: takes the result; NULL: not wanted
+ *   codes, scales [device] int8 [rows][cols] and fp32 [rows]: the result in 8 bits; both or none, none only with out.  The code of a
+ *                value is formed from h * weight, exact in fp32 unless that overflows (it then counts as not finite), the factor 127 / top and their product rounded to
+ *                fp32; the scale is that of the row of h * weight, times r.
+ * Buffers are 16-byte aligned (scales: 4) and overlap in no other way.  Asynchronous on `stream`; allocates nothing.
+ * Errors: HFX_ERR_NULL, HFX_ERR_SHAPE (rows < 0; cols, eps or a stride not as above), HFX_ERR_ALIGN (also: a stride that is no
+ * multiple of 8), HFX_ERR_DEVICE.
+ */
+hfx_status hfx_rms_norm(const hfx_norm* norm, int32_t rows, const void* x, int64_t x_stride,
+                        const void* residual, int64_t residual_stride, void* sum, void* out,
+                        void* codes, float* scales, void* stream);
+
+/* What hfx_quantise_rows does to a value v first: nothing, or v / (1 + e^-v). */
+enum { HFX_ACT_NONE = 0, HFX_ACT_SILU = 1 };
+
+/*
+ * Rows of bf16 through an activation, times other rows, in fp32, and from there to bf16 and to 8 bits.  (Ahead of the projections that do not follow a norm:
+ * attention's rows, and the gate and up rows of a feed-forward.)  The rows of a weight [n][k] become those of an hfx_weight_q8 this way.
+ *   x, times     [device] bf16, rows x_stride and times_stride apart (multiples of 8); times NULL: no factor
+ *   out          [device] bf16 [rows][cols]; NULL: not wanted
+ *   codes, scales [device] int8 [rows][cols] and fp32 [rows]; both or none, none only with out
+ * out may be x or times itself if that is packed and codes are not wanted; otherwise buffers overlap in no way but x and times.
+ * Asynchronous on `stream`; allocates nothing.  Errors as hfx_rms_norm (HFX_ERR_SHAPE also for an activation that is none of the above).
+ */
+hfx_status hfx_quantise_rows(int32_t activation, int32_t rows, int32_t cols, const void* x,
+                             int64_t x_stride, const void* times, int64_t times_stride, void* out,
+                             void* codes, float* scales, void* stream);
+
+/* A weight in 8 bits, a scale for each output channel. */
+typedef struct {
+  const void* codes;     /* [device] int8, channel j's row of k at codes + j * stride, 16-byte aligned           */
+  const float* scales;   /* [device] fp32 [n]                                                                   */
+  const void* bias;      /* [device] bf16 [n], or NULL                                                          */
+  int32_t n, k;          /* output channels (1 .. 2097152), values they sum over                                */
+  int64_t stride;        /* a multiple of 16                                                                    */
+} hfx_weight_q8;
+
+/*
+ * out[i][j] = (sum over k of codes[i][k] * weight->codes[j][k]) * scales[i] * weight->scales[j] + bias[j]: a projection of a step's rows.  The sum
+ * is exact (codes of -128 included); it is rounded to fp32, as is each product behind it, and the result to bf16 if that is asked for.
+ *   rows         rows * n is at most 2^38
+ *   codes        [device] int8, row i at codes + i * codes_stride (a multiple of 16), 16-byte aligned
+ *   scales       [device] fp32 [rows]
+ *   out          [device] bf16, or (fp32 = 1) fp32, row i at i * out_stride elements, 16-byte aligned; any stride of at least n
+ * Results may not overlap what is read.  Asynchronous on `stream`; allocates nothing, and needs no workspace.
+ * Errors: HFX_ERR_NULL, HFX_ERR_SHAPE, HFX_ERR_ALIGN, HFX_ERR_DEVICE.
+ */
+hfx_status hfx_matmul_rows(const hfx_weight_q8* weight, int32_t rows, const void* codes,
+                         int64_t codes_stride, const float* scales, void* out, int64_t out_stride,
+                         int32_t fp32, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Step composition (host only): the closed forms of Section 3.3.1 that decide how many
  * prompt tokens a step may carry, and a one-instance form of the dispatching steps that
  * turns a waiting queue into the arrays hfx_build_batch_desc takes.

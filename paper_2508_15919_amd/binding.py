@@ -21,10 +21,12 @@ HFX_ERR_NULL, HFX_ERR_SHAPE, HFX_ERR_KIND, HFX_ERR_LEN, HFX_ERR_PAGES = -1, -2, 
 HFX_ERR_PAGE_ID, HFX_ERR_BUFSIZE, HFX_ERR_DEVICE, HFX_ERR_DESC, HFX_ERR_ALIGN = -6, -7, -8, -9, -10
 HFX_ERR_MODEL = -11
 HFX_DECODE, HFX_PREFILL = 0, 1
+HFX_ACT_NONE, HFX_ACT_SILU = 0, 1
 
 EXPORTS = ["hfx_status_string", "hfx_version", "hfx_batch_desc_sizes", "hfx_build_batch_desc",
            "hfx_fill_batch_desc", "hfx_mixed_paged_attention", "hfx_mixed_paged_attention_static", "hfx_gather_kv", "hfx_append_kv",
            "hfx_copy_pages", "hfx_rope_append_kv", "hfx_mx_pool_bytes", "hfx_rope_append_kv_mx", "hfx_read_new_kv_mx", "hfx_mixed_paged_attention_mx",
+           "hfx_rms_norm", "hfx_quantise_rows", "hfx_matmul_rows",
            "hfx_token_budget", "hfx_maturity_time", "hfx_fit_latency_model", "hfx_compose_step"]
 
 
@@ -41,6 +43,25 @@ class hfx_rope(ctypes.Structure):
     def __init__(self, *args):
         super().__init__(*args)
         self.address = ctypes.addressof(self)      # (asked for by every call)
+
+
+class hfx_norm(ctypes.Structure):
+    """Keeps the weight it was made with alive (see make_norm)."""
+    _fields_ = [("weight", ctypes.c_void_p), ("cols", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+    def __init__(self, *args):
+        super().__init__(*args)
+        self.address = ctypes.addressof(self)
+
+
+class hfx_weight_q8(ctypes.Structure):
+    """Keeps the tensors it was made with alive (see make_weight_q8)."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("n", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("stride", ctypes.c_int64)]
+
+    def __init__(self, *args):
+        super().__init__(*args)
+        self.address = ctypes.addressof(self)
 
 
 class hfx_latency_model(ctypes.Structure):
@@ -106,6 +127,12 @@ def load() -> ctypes.CDLL:
         lib.hfx_read_new_kv_mx.restype = ctypes.c_int32
         lib.hfx_mixed_paged_attention_mx.argtypes = [shp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp]
         lib.hfx_mixed_paged_attention_mx.restype = ctypes.c_int32
+        lib.hfx_rms_norm.argtypes = [ctypes.POINTER(hfx_norm), ctypes.c_int32, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+        lib.hfx_rms_norm.restype = ctypes.c_int32
+        lib.hfx_quantise_rows.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, i64, vp, i64, vp, vp, vp, vp]
+        lib.hfx_quantise_rows.restype = ctypes.c_int32
+        lib.hfx_matmul_rows.argtypes = [ctypes.POINTER(hfx_weight_q8), ctypes.c_int32, vp, i64, vp, vp, i64, ctypes.c_int32, vp]
+        lib.hfx_matmul_rows.restype = ctypes.c_int32
         dbl, dblp = ctypes.c_double, ctypes.POINTER(ctypes.c_double)
         i64p, lmp = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(hfx_latency_model)
         lib.hfx_token_budget.argtypes = [dbl, dbl, lmp, i64p]
@@ -143,7 +170,9 @@ def _serving() -> types.SimpleNamespace:
             attention_static=caller(lib.hfx_mixed_paged_attention_static, "SPPPPPs"), gather=caller(lib.hfx_gather_kv, "SPPPiPPs"),
             append=caller(lib.hfx_append_kv, "SPPPPPs"), copy_pages=caller(lib.hfx_copy_pages, "SPPikaPPzs"),
             rope_append=caller(lib.hfx_rope_append_kv, "SPPzPzPzPPPPs"), rope_append4=caller(lib.hfx_rope_append_kv_mx, "SPPzPzPzPPPPs"),
-            read_new4=caller(lib.hfx_read_new_kv_mx, "SPPPPPs"), attention4=caller(lib.hfx_mixed_paged_attention_mx, "SPPPPBPs"))
+            read_new4=caller(lib.hfx_read_new_kv_mx, "SPPPPPs"), attention4=caller(lib.hfx_mixed_paged_attention_mx, "SPPPPBPs"),
+            rms_norm=caller(lib.hfx_rms_norm, "PiPzPzPPPPs"), quantise_rows=caller(lib.hfx_quantise_rows, "iiiPzPzPPPs"),
+            matmul_rows=caller(lib.hfx_matmul_rows, "PiPzPPzis"))
     return _calls
 
 
@@ -201,6 +230,32 @@ def make_rope(cos_sin, rot_dim: int, interleaved: bool = False) -> hfx_rope:
     rope = hfx_rope(cos_sin.data_ptr(), cos_sin.shape[0], int(rot_dim), int(bool(interleaved)))
     rope.table = cos_sin
     return rope
+
+
+def make_norm(weight, eps: float) -> hfx_norm:
+    """The norm with `weight`, bf16 [cols] on the GPU."""
+    if weight.dim() != 1 or weight.element_size() != 2 or str(weight.dtype) != "torch.bfloat16" or not weight.is_contiguous():
+        raise ValueError("weight is contiguous bf16 [cols]")
+    if not weight.is_cuda:                         # (as for the table of make_rope)
+        raise ValueError("weight is on the GPU")
+    norm = hfx_norm(weight.data_ptr(), weight.shape[0], float(eps))
+    norm.tensor = weight
+    return norm
+
+
+def make_weight_q8(codes, scales, bias=None) -> hfx_weight_q8:
+    """The weight of codes [n, k] (int8, rows apart by any multiple of 16), scales [n] (fp32) and, if there is one, a bias [n] (bf16), all on the GPU."""
+    if codes.dim() != 2 or str(codes.dtype) != "torch.int8" or codes.stride(1) != 1:
+        raise ValueError("codes are int8 [n, k], the values of a row side by side")
+    n, k = codes.shape
+    for x, dtype, name in ((scales, "torch.float32", "scales are contiguous fp32 [n]"), (bias, "torch.bfloat16", "bias is contiguous bf16 [n]")):
+        if x is not None and (tuple(x.shape) != (n,) or str(x.dtype) != dtype or not x.is_contiguous()):
+            raise ValueError(name)
+    if not codes.is_cuda or not scales.is_cuda or (bias is not None and not bias.is_cuda):
+        raise ValueError("codes, scales and bias are on the GPU")
+    weight = hfx_weight_q8(codes.data_ptr(), scales.data_ptr(), None if bias is None else bias.data_ptr(), n, k, codes.stride(0))
+    weight.tensors = codes, scales, bias
+    return weight
 
 
 def hfx_status_string(code: int) -> str:
@@ -315,6 +370,24 @@ def hfx_mixed_paged_attention_mx(shape: hfx_shape, q, mx_pool, host_desc, device
     rc = (_calls or _serving()).attention4(shape, q, mx_pool, host_desc, device_desc, workspace, out, stream)
     if rc != HFX_OK:
         raise HfxError(rc, "hfx_mixed_paged_attention_mx")
+
+
+def hfx_rms_norm(norm: hfx_norm, rows: int, x, x_stride: int, residual, residual_stride: int, sum, out, codes, scales, stream=None) -> None:
+    rc = (_calls or _serving()).rms_norm(norm.address if norm else None, rows, x, x_stride, residual, residual_stride, sum, out, codes, scales, stream)
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_rms_norm")
+
+
+def hfx_quantise_rows(activation: int, rows: int, cols: int, x, x_stride: int, times, times_stride: int, out, codes, scales, stream=None) -> None:
+    rc = (_calls or _serving()).quantise_rows(activation, rows, cols, x, x_stride, times, times_stride, out, codes, scales, stream)
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_quantise_rows")
+
+
+def hfx_matmul_rows(weight: hfx_weight_q8, rows: int, codes, codes_stride: int, scales, out, out_stride: int, fp32: bool = False, stream=None) -> None:
+    rc = (_calls or _serving()).matmul_rows(weight.address if weight else None, rows, codes, codes_stride, scales, out, out_stride, fp32, stream)
+    if rc != HFX_OK:
+        raise HfxError(rc, "hfx_matmul_rows")
 
 
 def hfx_token_budget(ttft: float, tpot: float, model: hfx_latency_model) -> int:

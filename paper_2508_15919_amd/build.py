@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhfxattn.so")
 # The name says for which Python it was built, so that another one does not load it.
 CALL_LIB = os.path.join(HERE, "_hfxcall" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["hfx_kernels.hip", "hfx_append.hip", "hfx_mx.hip", "hfx_api.cpp", "hfx_plan.cpp", "hfx_sched.cpp"]
+SOURCES = ["hfx_kernels.hip", "hfx_append.hip", "hfx_mx.hip", "hfx_rows.hip", "hfx_matmul.hip", "hfx_api.cpp", "hfx_plan.cpp", "hfx_sched.cpp"]
 # Sources with attention kernels, and their own flag.  -fno-honor-nans: without it every max of a softmax carries a canonicalising twin.  Nothing in them asks a
 # floating-point operation whether a value is NaN: scores that may be (of unused slots, which hold anything) are masked, and weights that may be are told apart, by integer
 # operations on bits that the compiler cannot see through.  Not for the appends over a projection's output, which may hold anything and of which that is asked.

@@ -13,6 +13,14 @@
 namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// What the operators between attention calls take.  128^2 times the longest row is less than 2^31; the largest stride times the rows of a tile is an
+// offset of 32 bits; workgroups times threads of a launch are less than 2^32.
+constexpr int kLongestRow = 131056, kMostRows = 1 << 21;
+constexpr int64_t kLargestStride = 1 << 22, kMostResults = 1ll << 38;
+bool rows_ok(int32_t rows, int32_t cols) { return rows >= 0 && rows <= kMostRows && cols >= 16 && cols <= kLongestRow && cols % 16 == 0; }
+bool stride_ok(int64_t stride, int32_t cols) { return stride >= cols && stride <= kLargestStride; }
 
 // header of a descriptor this library wrote, matching `shape`
 hfx_status check_header(const hfx_shape* shape, const void* host_desc, HfxHeader* out) {
@@ -276,6 +284,77 @@ hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, c
   hfx_status st = check_header(shape, host_desc, &h);
   if (st != HFX_OK) return st;
   return run_attention(h, true, q, mx_pool, device_desc, workspace, workspace_bytes, out, stream);
+}
+
+hfx_status hfx_rms_norm(const hfx_norm* norm, int32_t rows, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* sum,
+                        void* out, void* codes, float* scales, void* stream) {
+  if (!norm || !norm->weight || !x || (residual == nullptr) != (sum == nullptr) || (codes == nullptr) != (scales == nullptr) || (!out && !codes))
+    return HFX_ERR_NULL;
+  if (!rows_ok(rows, norm->cols) || !(norm->eps >= 0.0f && norm->eps <= 3.0e38f)) return HFX_ERR_SHAPE;
+  if (!stride_ok(x_stride, norm->cols) || (residual && !stride_ok(residual_stride, norm->cols))) return HFX_ERR_SHAPE;
+  if (!aligned16(norm->weight) || !aligned16(x) || !aligned16(residual) || !aligned16(sum) || !aligned16(out) || !aligned16(codes) || !aligned4(scales) ||
+      (x_stride | (residual ? residual_stride : 0)) % 8 != 0)
+    return HFX_ERR_ALIGN;
+  if (rows == 0) return HFX_OK;
+  hfx::RmsNorm a = {};
+  a.x = static_cast<const uint16_t*>(x);
+  a.residual = static_cast<const uint16_t*>(residual);
+  a.weight = static_cast<const uint16_t*>(norm->weight);
+  a.sum = static_cast<uint16_t*>(sum);
+  a.out = static_cast<uint16_t*>(out);
+  a.codes = static_cast<int8_t*>(codes);
+  a.scales = scales;
+  a.x_stride = (long)x_stride;
+  a.residual_stride = (long)residual_stride;
+  a.cols = norm->cols;
+  a.eps = norm->eps;
+  return hfx::launch_rms_norm(a, rows, static_cast<hipStream_t>(stream)) == hipSuccess ? HFX_OK : HFX_ERR_DEVICE;
+}
+
+hfx_status hfx_quantise_rows(int32_t activation, int32_t rows, int32_t cols, const void* x, int64_t x_stride, const void* times, int64_t times_stride,
+                             void* out, void* codes, float* scales, void* stream) {
+  if (!x || (codes == nullptr) != (scales == nullptr) || (!out && !codes)) return HFX_ERR_NULL;
+  if ((activation != HFX_ACT_NONE && activation != HFX_ACT_SILU) || !rows_ok(rows, cols)) return HFX_ERR_SHAPE;
+  if (!stride_ok(x_stride, cols) || (times && !stride_ok(times_stride, cols))) return HFX_ERR_SHAPE;
+  if (!aligned16(x) || !aligned16(times) || !aligned16(out) || !aligned16(codes) || !aligned4(scales) || (x_stride | (times ? times_stride : 0)) % 8 != 0)
+    return HFX_ERR_ALIGN;
+  if (rows == 0) return HFX_OK;
+  hfx::QuantiseRows a = {};
+  a.x = static_cast<const uint16_t*>(x);
+  a.times = static_cast<const uint16_t*>(times);
+  a.out = static_cast<uint16_t*>(out);
+  a.codes = static_cast<int8_t*>(codes);
+  a.scales = scales;
+  a.x_stride = (long)x_stride;
+  a.times_stride = (long)times_stride;
+  a.cols = cols;
+  a.activation = activation;
+  return hfx::launch_quantise_rows(a, rows, static_cast<hipStream_t>(stream)) == hipSuccess ? HFX_OK : HFX_ERR_DEVICE;
+}
+
+hfx_status hfx_matmul_rows(const hfx_weight_q8* weight, int32_t rows, const void* codes, int64_t codes_stride, const float* scales, void* out,
+                         int64_t out_stride, int32_t fp32, void* stream) {
+  if (!weight || !weight->codes || !weight->scales || !codes || !scales || !out) return HFX_ERR_NULL;
+  if (!rows_ok(rows, weight->k) || weight->n < 1 || weight->n > kMostRows || (int64_t)rows * weight->n > kMostResults || (fp32 != 0 && fp32 != 1)) return HFX_ERR_SHAPE;
+  if (!stride_ok(codes_stride, weight->k) || !stride_ok(weight->stride, weight->k) || !stride_ok(out_stride, weight->n)) return HFX_ERR_SHAPE;
+  if (!aligned16(weight->codes) || !aligned4(weight->scales) || (reinterpret_cast<uintptr_t>(weight->bias) & 1u) != 0 || !aligned16(codes) ||
+      !aligned4(scales) || !aligned16(out) || (codes_stride | weight->stride) % 16 != 0)
+    return HFX_ERR_ALIGN;
+  if (rows == 0) return HFX_OK;
+  hfx::MatmulRows a = {};
+  a.codes = static_cast<const int8_t*>(codes);
+  a.weight = static_cast<const int8_t*>(weight->codes);
+  a.scales = scales;
+  a.weight_scales = weight->scales;
+  a.bias = static_cast<const uint16_t*>(weight->bias);
+  a.out = out;
+  a.codes_stride = (long)codes_stride;
+  a.weight_stride = (long)weight->stride;
+  a.out_stride = (long)out_stride;
+  a.rows = rows;
+  a.n = weight->n;
+  a.k = weight->k;
+  return hfx::launch_matmul_rows(a, fp32 != 0, static_cast<hipStream_t>(stream)) == hipSuccess ? HFX_OK : HFX_ERR_DEVICE;
 }
 
 hfx_status hfx_copy_pages(const hfx_shape* shape, const void* src_pool, void* dst_pool, int32_t dst_num_pages,

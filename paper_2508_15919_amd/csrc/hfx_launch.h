@@ -34,6 +34,40 @@ struct RopeAppend {
 hipError_t launch_rope_append(const HfxHeader& h, const void* desc, RopeAppend a, bool four, hipStream_t stream);
 hipError_t launch_read_new_kv_mx(const HfxHeader& h, const void* desc, const void* pool, void* k_out, void* v_out, hipStream_t stream);
 
+// What the norm takes.  residual (and with it sum), out and codes (with scales) may be null.
+struct RmsNorm {
+  const uint16_t *x, *residual, *weight;
+  uint16_t *sum, *out;       // [rows][cols]
+  int8_t* codes;             // [rows][cols]
+  float* scales;
+  long x_stride, residual_stride;
+  int cols;
+  float eps;
+};
+hipError_t launch_rms_norm(const RmsNorm& a, int rows, hipStream_t stream);
+
+// What the rows' way to 8 bits takes.  times, out and codes (with scales) may be null.
+struct QuantiseRows {
+  const uint16_t *x, *times;
+  uint16_t* out;             // [rows][cols]
+  int8_t* codes;             // [rows][cols]
+  float* scales;
+  long x_stride, times_stride;
+  int cols, activation;
+};
+hipError_t launch_quantise_rows(const QuantiseRows& a, int rows, hipStream_t stream);
+
+// What a product takes: codes [rows][k] and [n][k], their scales, results [rows][n].  bias may be null.
+struct MatmulRows {
+  const int8_t *codes, *weight;
+  const float *scales, *weight_scales;
+  const uint16_t* bias;
+  void* out;
+  long codes_stride, weight_stride, out_stride;
+  int rows, n, k;
+};
+hipError_t launch_matmul_rows(const MatmulRows& a, bool fp32, hipStream_t stream);
+
 // The header as an attention kernel gets it.
 HfxHeader launch_header(const HfxHeader& header, int grid);
 // The attention launch over a 4-bit page pool; arguments as launch_mixed_attention.

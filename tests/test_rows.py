@@ -1,0 +1,507 @@
+"""The operators between a layer's attention calls -- norm of the residual stream, rows in 8 bits, their products -- against plain forms in 64 bits (numpy).
+
+Tolerances, from the arithmetic:
+ * codes of the norm and of rows without activation, the stream's sum, and products: the operators fix every rounding, so bits are equal to those of the oracle
+   with the same roundings.
+ * scales: the norm's factor is formed in 64 bits and the scale rounded once, 2^-24 (the oracle's sum may be in another order, 64 bits again: 2^-40);
+   that of other rows is one division, equal bits.
+ * bf16 results of the norm: the factor, its product with h and that with the weight are rounded to fp32, 2^-24 each, and the result to bf16, 2^-8.
+ * silu in fp32, x t / (1 + t) below zero and x / (1 + t) above, t = e^-|x|: the exponential 2^-22 (two units in the last place), its argument is exact, the product, the sum,
+   the division and the product with the factor 2^-24 each: 2^-22 + 4 * 2^-24 = 2^-21 of the value.  A code is then within half a step, plus 127 times 2^-21 twice (of the value and of the
+   row's largest) and the rounding of factor and product (2^-24 each): 0.5 + 1.4e-4 steps.
+"""
+import numpy as np
+import pytest
+
+from paper_2508_15919_amd import binding as hb
+from paper_2508_15919_amd.synth import bf16_bits_to_f64, f32_to_bf16_bits
+
+HALF_BF16 = 2.0 ** -8
+
+
+def bf16(x):
+    """Values rounded to bf16, in 64 bits."""
+    return bf16_bits_to_f64(f32_to_bf16_bits(np.asarray(x, np.float32)))
+
+
+def to_codes(v):
+    """Rows of fp32 numbers -> codes and largest magnitudes, with the operators' roundings."""
+    v = np.asarray(v, np.float32)
+    with np.errstate(invalid="ignore", over="ignore"):
+        top = np.maximum(np.abs(v).max(1, keepdims=True), np.float32(2.0 ** -100))
+        bad = ~np.isfinite(v).all(1, keepdims=True)
+        t = np.where(bad, np.float32(0), np.where(bad, np.float32(0), v) * (np.float32(127) / np.where(bad, np.float32(1), top)))
+    return np.rint(t).astype(np.int8), np.where(bad, np.nan, top.astype(np.float64))
+
+
+def device(torch, x, dtype=None):
+    """bf16 values (64 bits on the host) on the GPU."""
+    t = torch.from_numpy(np.ascontiguousarray(x))
+    return t.to(dtype or torch.bfloat16).cuda()
+
+
+def strided(torch, x, extra):
+    """The rows of a tensor in a wider buffer, which holds NaN (or 77) beside them."""
+    rows, cols = x.shape
+    fill = 77 if x.dtype == torch.int8 else float("nan")
+    wide = torch.full((rows, cols + extra), fill, dtype=x.dtype, device="cuda")
+    wide[:, :cols] = x
+    return wide
+
+
+# ------------------------------------------------------------------ norm
+def norm_oracle(x, residual, weight, eps):
+    """Sum, result in 64 bits, codes, scales in 64 bits."""
+    h = x if residual is None else bf16(x.astype(np.float32) + residual.astype(np.float32))
+    with np.errstate(invalid="ignore", over="ignore"):
+        r = 1.0 / np.sqrt((h * h).mean(1, keepdims=True) + float(np.float32(eps)))
+        codes, top = to_codes(h.astype(np.float32) * weight.astype(np.float32))
+        return h, h * r * weight, codes, (top * r / 127.0)[:, 0]
+
+
+def run_norm(torch, x, residual, weight, eps, extra=0, behind=2):
+    rows, cols = x.shape
+    dx = strided(torch, device(torch, x), extra)
+    dr = None if residual is None else strided(torch, device(torch, residual), extra)
+    total = None if residual is None else torch.full((rows + behind, cols), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((rows + behind, cols), 7.0, dtype=torch.bfloat16, device="cuda")
+    codes = torch.full((rows + behind, cols), 99, dtype=torch.int8, device="cuda")
+    scales = torch.full((rows + behind,), 7.0, dtype=torch.float32, device="cuda")
+    norm = hb.make_norm(device(torch, weight), eps)
+    hb.hfx_rms_norm(norm, rows, dx, cols + extra, dr, cols + extra, total, out, codes, scales, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for t, was in ((total, 7.0), (out, 7.0), (codes, 99), (scales, 7.0)):      # rows behind the last
+        assert t is None or bool((t[rows:] == was).all())
+    return [None if t is None else t[:rows].cpu().double().numpy() for t in (total, out, codes, scales)]
+
+
+def check_norm(got, want):
+    total, out, codes, scales = got
+    h, y, want_codes, want_scales = want
+    assert total is None or np.array_equal(total, h, equal_nan=True)
+    assert np.array_equal(codes, want_codes)
+    assert np.array_equal(np.isnan(scales), np.isnan(want_scales))
+    fine = ~np.isnan(scales)
+    assert (np.abs(scales - want_scales)[fine] <= (2.0 ** -24 + 2.0 ** -40) * want_scales[fine] + 2.0 ** -149).all()
+    off = np.abs(out - y)[fine]
+    assert (off <= (HALF_BF16 + 3 * 2.0 ** -24) * np.abs(y[fine]) + 2.0 ** -133).all()
+    return fine
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("with_residual", [True, False])
+@pytest.mark.parametrize("rows,cols,extra", [(1, 16, 0), (3, 48, 8), (70, 512, 0), (5, 1024, 24), (4, 1040, 0), (33, 2048, 8), (2, 4096, 0), (3, 8192, 0), (2, 8208, 8),
+                                             (1, 32768, 0), (2, 40016, 16), (1, 131056, 0)])
+def test_norm(rows, cols, extra, with_residual):
+    import torch
+    g = np.random.default_rng(rows * 131 + cols)
+    x = bf16(g.standard_normal((rows, cols)))
+    residual = bf16(3.0 * g.standard_normal((rows, cols))) if with_residual else None
+    weight = bf16(1.0 + 0.3 * g.standard_normal(cols))
+    fine = check_norm(run_norm(torch, x, residual, weight, 1e-6, extra), norm_oracle(x, residual, weight, 1e-6))
+    assert fine.all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [64, 4096, 9008])
+def test_norm_of_extreme_rows(cols):
+    """Zeros, subnormal and largest numbers, squares past the range of 32 bits, one value among zeros, ties, and rows that are not finite beside all of them."""
+    import torch
+    g = np.random.default_rng(cols)
+    x = bf16(g.standard_normal((12, cols)))
+    weight = np.ones(cols)
+    x[0] = 0.0
+    x[1] = 0.0
+    x[1, 5] = -2.0 ** -133                                      # the smallest bf16 number
+    x[2] = bf16(1e-36 * x[2])
+    x[3] = bf16(1e30 * x[3])
+    x[4, 3] = 3.3e38
+    x[4] = bf16(x[4])
+    x[5] = 0.0
+    x[5, cols - 1] = 1.0
+    x[6] = (np.arange(cols) % 64) + 0.5                         # codes halfway between two numbers under a largest one of 127
+    x[6, 7], x[6, 8] = 127.0, -63.5
+    x[7, 1] = np.inf
+    x[8, cols - 2] = np.nan
+    x[9, 0] = -np.inf
+    x[9, 1] = np.inf
+    residual = np.zeros_like(x)
+    residual[10] = -x[10]                                       # a sum of zeros
+    for r in (None, residual):
+        got, want = run_norm(torch, x, r, weight, 1e-6), norm_oracle(x, r, weight, 1e-6)
+        fine = check_norm(got, want)
+        assert fine.tolist() == [True] * 7 + [False] * 3 + [True] * 2
+        assert not got[2][7:10].any() and np.isnan(got[1][8]).all()
+    assert set(np.abs(got[2][6]) % 2) == {0.0, 1.0} and got[2][6, 0] == 0 and got[2][6, 1] == 2 and got[2][6, 8] == -64
+    with pytest.raises(hb.HfxError):
+        run_norm(torch, x, None, weight, float("nan"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(3, 2048), (2, 40000)])
+def test_norm_in_place_and_by_parts(rows, cols):
+    """The sum over x or over the residual; results in bf16 alone and in 8 bits alone: the same bits."""
+    import torch
+    g = np.random.default_rng(5)
+    x, residual = device(torch, g.standard_normal((rows, cols))), device(torch, g.standard_normal((rows, cols)))
+    norm = hb.make_norm(device(torch, 1.0 + 0.1 * g.standard_normal(cols)), 1e-5)
+    stream = torch.cuda.current_stream()
+
+    def call(x, residual, total, want_out, want_codes):
+        out = torch.empty_like(x) if want_out else None
+        codes, scales = (torch.empty((rows, cols), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")) if want_codes else (None, None)
+        hb.hfx_rms_norm(norm, rows, x, cols, residual, cols, total, out, codes, scales, stream)
+        torch.cuda.synchronize()
+        return total, out, codes, scales
+    total, out, codes, scales = call(x, residual, torch.empty_like(x), True, True)
+    a, b = x.clone(), residual.clone()
+    assert torch.equal(call(a, b, a, True, False)[1], out) and torch.equal(a, total) and torch.equal(b, residual)
+    a = x.clone()
+    got = call(a, b, b, False, True)
+    assert torch.equal(got[2], codes) and torch.equal(got[3], scales) and torch.equal(b, total) and torch.equal(a, x)
+    assert torch.equal(call(total, None, None, True, False)[1], out)
+
+
+# ------------------------------------------------------------------ rows to 8 bits
+def run_rows(torch, activation, x, times, extra=0, want_out=True, behind=2):
+    rows, cols = x.shape
+    dx = strided(torch, device(torch, x), extra)
+    dt = None if times is None else strided(torch, device(torch, times), extra)
+    out = torch.full((rows + behind, cols), 7.0, dtype=torch.bfloat16, device="cuda") if want_out else None
+    codes = torch.full((rows + behind, cols), 99, dtype=torch.int8, device="cuda")
+    scales = torch.full((rows + behind,), 7.0, dtype=torch.float32, device="cuda")
+    hb.hfx_quantise_rows(activation, rows, cols, dx, cols + extra, dt, cols + extra, out, codes, scales, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for t, was in ((out, 7.0), (codes, 99), (scales, 7.0)):
+        assert t is None or bool((t[rows:] == was).all())
+    return [None if t is None else t[:rows].cpu().double().numpy() for t in (out, codes, scales)]
+
+
+SIZES = [(1, 16, 0), (3, 80, 8), (40, 1024, 0), (5, 1376, 8), (2, 8192, 0), (3, 14336, 0), (2, 33008, 8), (1, 131056, 0)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("with_times", [False, True])
+@pytest.mark.parametrize("rows,cols,extra", SIZES)
+def test_rows_as_they_are(rows, cols, extra, with_times):
+    import torch
+    g = np.random.default_rng(rows + cols)
+    x, times = bf16(g.standard_normal((rows, cols))), bf16(g.standard_normal((rows, cols))) if with_times else None
+    v = (x if times is None else x * times).astype(np.float32)          # exact: 8 bits times 8 bits
+    codes, top = to_codes(v)
+    out, got, scales = run_rows(torch, hb.HFX_ACT_NONE, x, times, extra)
+    assert np.array_equal(got, codes)
+    assert np.array_equal(scales, (top[:, 0].astype(np.float32) / np.float32(127)).astype(np.float64))
+    assert np.array_equal(out, bf16(v))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("with_times", [False, True])
+@pytest.mark.parametrize("rows,cols,extra", SIZES)
+def test_rows_through_silu(rows, cols, extra, with_times):
+    import torch
+    g = np.random.default_rng(rows * 7 + cols)
+    x, times = bf16(4.0 * g.standard_normal((rows, cols))), bf16(g.standard_normal((rows, cols))) if with_times else None
+    x[0, :4] = 90.0, -90.0, 0.0, -1e-30
+    v = x / (1.0 + np.exp(-x))
+    if times is not None:
+        v = v * times
+    top = np.abs(v).max(1)
+    out, codes, scales = run_rows(torch, hb.HFX_ACT_SILU, x, times, extra)
+    assert (np.abs(scales - top / 127.0) <= 2.0 ** -20 * top / 127.0).all()
+    assert (np.abs(codes) <= 127).all() and (np.abs(codes).max(1) == 127).all()
+    assert (np.abs(codes - v * 127.0 / top[:, None]) <= 0.5 + 1.4e-4).all()
+    assert (np.abs(out - v) <= (HALF_BF16 + 2.0 ** -20) * np.abs(v) + 2.0 ** -126).all()
+    assert np.array_equal(run_rows(torch, hb.HFX_ACT_SILU, x, times, extra, want_out=False)[1], codes)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("activation", [hb.HFX_ACT_NONE, hb.HFX_ACT_SILU])
+def test_rows_that_are_zero_tiny_huge_or_not_finite(activation):
+    import torch
+    g = np.random.default_rng(2)
+    x = bf16(g.standard_normal((8, 1040)))
+    x[0] = 0.0
+    x[1] = bf16(1e-37 * x[1])                                   # below 2^-100: codes of zero
+    x[2] = bf16(np.abs(1e37 * x[2]))
+    x[3, 900] = np.inf
+    x[4, 2] = np.nan
+    x[5] = -np.abs(x[5])
+    x[5, 7] = -np.inf                                           # silu of it is not a number
+    out, codes, scales = run_rows(torch, activation, x, None)
+    assert not codes[[0, 1, 3, 4, 5]].any()
+    assert np.isnan(scales[3:6]).all() and np.isfinite(scales[[0, 1, 2, 6, 7]]).all()
+    assert scales[0] == scales[1] == float(np.float32(2.0 ** -100) / np.float32(127))
+    assert np.abs(codes[2]).max() == 127 and np.abs(codes[6]).max() == 127
+
+
+@pytest.mark.gpu
+def test_rows_in_place():
+    import torch
+    x, t = device(torch, np.random.default_rng(0).standard_normal((2, 5, 2048)))
+    stream = torch.cuda.current_stream()
+    want = torch.empty_like(x)
+    hb.hfx_quantise_rows(hb.HFX_ACT_SILU, 5, 2048, x, 2048, t, 2048, want, None, None, stream)
+    a, b = x.clone(), t.clone()
+    hb.hfx_quantise_rows(hb.HFX_ACT_SILU, 5, 2048, a, 2048, t, 2048, a, None, None, stream)
+    hb.hfx_quantise_rows(hb.HFX_ACT_SILU, 5, 2048, x, 2048, b, 2048, b, None, None, stream)
+    assert torch.equal(a, want) and torch.equal(b, want)
+
+
+# ------------------------------------------------------------------ products
+def product_oracle(codes, scales, weight, weight_scales, bias, fp32):
+    """With the operator's roundings; the sums by a product in 64 bits, which holds them exactly."""
+    y = (codes.astype(np.float64) @ weight.astype(np.float64).T).astype(np.float32)
+    with np.errstate(invalid="ignore"):
+        y = y * scales[:, None] * weight_scales[None]
+    if bias is not None:
+        y = y + bias.astype(np.float32)
+    return y.astype(np.float64) if fp32 else bf16(y)
+
+
+def run_product(torch, codes, scales, weight, weight_scales, bias, fp32, extra=(0, 0, 0), behind=3):
+    """extra: elements between the rows of codes, weight and results."""
+    rows, k = codes.shape
+    n = len(weight)
+    dc, dw = strided(torch, device(torch, codes, torch.int8), extra[0]), strided(torch, device(torch, weight, torch.int8), extra[1])
+    handle = hb.make_weight_q8(dw[:, :k], device(torch, weight_scales, torch.float32), None if bias is None else device(torch, bias))
+    out = torch.full((rows + behind, n + extra[2]), 7.0, dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda")
+    hb.hfx_matmul_rows(handle, rows, dc, k + extra[0], device(torch, scales, torch.float32), out, n + extra[2], fp32, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert bool((out[rows:] == 7.0).all()) and bool((out[:, n:] == 7.0).all())
+    return out[:rows, :n].cpu().double().numpy()
+
+
+def product_inputs(g, rows, n, k, with_bias):
+    codes, weight = g.integers(-128, 128, (rows, k)).astype(np.int8), g.integers(-128, 128, (n, k)).astype(np.int8)
+    scales, weight_scales = (np.exp(g.standard_normal(m)).astype(np.float32) / np.float32(70.0 * k ** 0.25) for m in (rows, n))
+    return codes, scales, weight, weight_scales, bf16(g.standard_normal(n)) if with_bias else None
+
+
+def check_product(torch, rows, n, k, with_bias, fp32, extra=(0, 0, 0), seed=0):
+    a = product_inputs(np.random.default_rng([rows, n, k, seed]), rows, n, k, with_bias)
+    got, want = run_product(torch, *a, fp32, extra), product_oracle(*a, fp32)
+    wrong = np.argwhere(got != want)
+    assert not len(wrong), (rows, n, k, len(wrong), wrong[:4].tolist(), got[tuple(wrong[0])], want[tuple(wrong[0])])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 32, 33, 48, 63, 64, 65, 96, 128, 129, 200, 256, 257, 520, 1030])
+def test_products_of_any_number_of_rows(rows):
+    import torch
+    for n, k, fp32 in ((640, 512, False), (1000, 1040, True), (37, 2064, False)):
+        check_product(torch, rows, n, k, rows % 2 == 0, fp32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 2, 3, 15, 16, 17, 31, 33, 63, 65, 127, 128, 129, 255, 257, 1001])
+def test_products_of_any_number_of_channels(n):
+    import torch
+    for rows, k, fp32 in ((1, 256, True), (20, 144, False), (70, 400, True), (300, 256, False)):
+        check_product(torch, rows, n, k, n % 2 == 1, fp32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [16, 32, 48, 64, 80, 112, 128, 144, 240, 256, 272, 384, 496, 768, 1008, 4096, 4112])
+def test_products_over_any_length(k):
+    import torch
+    for rows, n, fp32 in ((1, 70, False), (16, 130, True), (50, 300, False), (150, 270, False), (400, 515, True)):
+        check_product(torch, rows, n, k, False, fp32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,n,k,extra", [(5, 300, 528, (16, 32, 1)), (33, 64, 256, (48, 0, 8)), (130, 257, 1040, (16, 16, 7)), (700, 768, 640, (0, 64, 128)), (64, 4096, 64, (4080, 16, 3))])
+def test_products_of_rows_that_lie_apart(rows, n, k, extra):
+    import torch
+    for fp32 in (False, True):
+        check_product(torch, rows, n, k, True, fp32, extra)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 40, 300])
+@pytest.mark.parametrize("n,k", [(4096, 4096), (1280, 8192), (5001, 2048)])
+def test_products_of_a_layers_size(rows, n, k):
+    import torch
+    check_product(torch, rows, n, k, True, False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 30, 80, 260])
+def test_the_longest_sums(rows):
+    """All codes -128 over the longest row: 2^31 - 2^18, the largest sum there is; and the smallest."""
+    import torch
+    k, n = 131056, 260
+    codes, weight = np.full((rows, k), -128, np.int8), np.full((n, k), -128, np.int8)
+    weight[1::2] = 127
+    one = np.ones(rows, np.float32), np.ones(n, np.float32)
+    got = run_product(torch, codes, one[0], weight, one[1], None, True)
+    assert (got[:, 0::2] == float(np.float32(128 * 128 * k))).all() and (got[:, 1::2] == float(np.float32(-128 * 127 * k))).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [3, 40, 270])
+def test_scales_that_are_not_numbers_stay_in_their_row_and_channel(rows):
+    import torch
+    a = list(product_inputs(np.random.default_rng(rows), rows, 300, 256, False))
+    a[1][rows // 2], a[3][17] = np.nan, np.nan
+    got, want = run_product(torch, *a, False), product_oracle(*a, False)
+    assert np.array_equal(got, want, equal_nan=True)
+    assert np.isnan(got).sum() == rows + 300 - 1
+
+
+@pytest.mark.gpu
+def test_products_past_4_gb():
+    """Weights, rows and results whose offsets pass 32 bits: their last parts against the same parts alone."""
+    import torch
+    stream = torch.cuda.current_stream()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def codes(*shape):
+        return torch.randint(-128, 128, shape, dtype=torch.int8, device="cuda", generator=gen)
+    for rows, n, k, w_stride, c_stride in ((70, 70000, 64, 65536, 64), (70000, 70, 64, 64, 65536), (50000, 50000, 64, 64, 64)):
+        w = torch.zeros((n, w_stride), dtype=torch.int8, device="cuda")
+        c = torch.zeros((rows, c_stride), dtype=torch.int8, device="cuda")
+        w[:, :k], c[:, :k] = codes(n, k), codes(rows, k)
+        ws, cs = torch.rand(n, device="cuda", generator=gen), torch.rand(rows, device="cuda", generator=gen)
+        out = torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda")
+        assert max(w.numel(), c.numel(), 2 * out.numel()) > 1 << 32
+        hb.hfx_matmul_rows(hb.make_weight_q8(w[:, :k], ws), rows, c, c_stride, cs, out, n, False, stream)
+        for r, j in ((slice(rows - 65, rows), slice(n - 65, n)), (slice(0, 33), slice(n - 33, n)), (slice(rows - 33, rows), slice(0, 70))):
+            y = (c[r, :k].double() @ w[j, :k].double().T).float() * cs[r, None] * ws[j]
+            assert torch.equal(out[r, j], y.to(torch.bfloat16))
+        del w, c, out
+
+
+@pytest.mark.gpu
+def test_a_layers_calls_on_a_stream_and_in_a_graph():
+    """Norm, projection, activation, projection: eager, on another stream, and captured; the graph's inputs change between its replays."""
+    import torch
+    rows, hidden, wide = 37, 1024, 1792
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def normal(*shape):
+        return torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    norm = hb.make_norm(normal(hidden), 1e-6)
+
+    def weight(n, k):
+        codes, scales = torch.empty((n, k), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+        hb.hfx_quantise_rows(hb.HFX_ACT_NONE, n, k, normal(n, k) * k ** -0.5, k, None, 0, None, codes, scales, torch.cuda.current_stream())
+        return hb.make_weight_q8(codes, scales)
+    up, down = weight(2 * wide, hidden), weight(hidden, wide)
+    x, residual = normal(rows, hidden), normal(rows, hidden)
+
+    def buffers():
+        return dict(sum=torch.empty_like(x), c1=torch.empty((rows, hidden), dtype=torch.int8, device="cuda"), s1=torch.empty(rows, device="cuda"),
+                    both=torch.empty((rows, 2 * wide), dtype=torch.bfloat16, device="cuda"), c2=torch.empty((rows, wide), dtype=torch.int8, device="cuda"),
+                    s2=torch.empty(rows, device="cuda"), out=torch.empty_like(x))
+
+    def layer(b, stream):
+        hb.hfx_rms_norm(norm, rows, x, hidden, residual, hidden, b["sum"], None, b["c1"], b["s1"], stream)
+        hb.hfx_matmul_rows(up, rows, b["c1"], hidden, b["s1"], b["both"], 2 * wide, False, stream)
+        hb.hfx_quantise_rows(hb.HFX_ACT_SILU, rows, wide, b["both"], 2 * wide, b["both"][:, wide:], 2 * wide, None, b["c2"], b["s2"], stream)
+        hb.hfx_matmul_rows(down, rows, b["c2"], wide, b["s2"], b["out"], hidden, False, stream)
+    eager, other, captured = buffers(), buffers(), buffers()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        layer(other, side)
+    layer(eager, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(eager[n], other[n]) for n in eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        layer(captured, torch.cuda.current_stream())
+    for turn in range(4):
+        x.normal_(generator=gen)
+        residual.mul_(0.5 + turn)
+        layer(eager, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        for b in captured.values():
+            b.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(eager[n], captured[n]) for n in eager)
+        assert bool(torch.isfinite(eager["out"]).all()) and float(eager["out"].float().std()) > 0.01
+
+
+# ------------------------------------------------------------------ refusals, on the host
+class Fake:
+    """A norm or weight without memory: its numbers are addresses."""
+
+    def __init__(self, kind, *args):
+        self.held = kind(*args)
+        self.address = self.held.address
+
+
+def refused(call, code):
+    with pytest.raises(hb.HfxError) as e:
+        call()
+    assert e.value.code == code
+
+
+def test_what_the_norm_refuses():
+    ok = dict(norm=(16, 64, 1e-6), rows=2, x=32, x_stride=64, residual=None, residual_stride=0, sum=None, out=48, codes=None, scales=None)
+
+    def call(**change):
+        a = {**ok, **change}
+        norm = a.pop("norm")
+        hb.hfx_rms_norm(Fake(hb.hfx_norm, *norm) if norm else None, *a.values())
+    call(rows=0)                                                # nothing to do
+    call(rows=0, residual=64, residual_stride=64, sum=32, codes=64, scales=4)
+    for change in (dict(norm=None), dict(norm=(None, 64, 1e-6)), dict(x=None), dict(residual=16), dict(sum=16), dict(out=None), dict(codes=16), dict(scales=16), dict(out=None, codes=16)):
+        refused(lambda: call(**change), hb.HFX_ERR_NULL)
+    for change in (dict(rows=-1), dict(rows=(1 << 21) + 1), dict(norm=(16, 0, 1e-6)), dict(norm=(16, 72, 1e-6), x_stride=72), dict(norm=(16, 131072, 1e-6), x_stride=131072), dict(norm=(16, -16, 1e-6)),
+                   dict(norm=(16, 64, -1.0)), dict(norm=(16, 64, float("nan"))), dict(norm=(16, 64, float("inf"))), dict(x_stride=56), dict(x_stride=-64),
+                   dict(x_stride=(1 << 22) + 8), dict(residual=16, sum=64, residual_stride=63)):
+        refused(lambda: call(**change), hb.HFX_ERR_SHAPE)
+    for change in (dict(x=24), dict(norm=(8, 64, 1e-6)), dict(out=40), dict(x_stride=68), dict(residual=18, sum=64, residual_stride=64), dict(residual=16, sum=72, residual_stride=64),
+                   dict(residual=16, sum=64, residual_stride=70), dict(codes=8, scales=4), dict(codes=16, scales=2)):
+        refused(lambda: call(**change), hb.HFX_ERR_ALIGN)
+
+
+def test_what_the_rows_to_8_bits_refuse():
+    ok = dict(activation=hb.HFX_ACT_SILU, rows=2, cols=64, x=32, x_stride=64, times=None, times_stride=0, out=None, codes=48, scales=4)
+
+    def call(**change):
+        hb.hfx_quantise_rows(*{**ok, **change}.values())
+    call(rows=0)
+    call(rows=0, times=64, times_stride=128)
+    for change in (dict(x=None), dict(codes=None), dict(scales=None), dict(codes=None, scales=None)):
+        refused(lambda: call(**change), hb.HFX_ERR_NULL)
+    for change in (dict(activation=2), dict(activation=-1), dict(rows=-3), dict(cols=8), dict(cols=24), dict(cols=131072, x_stride=131072), dict(x_stride=63), dict(times=16, times_stride=0),
+                   dict(times=16, times_stride=(1 << 22) + 16)):
+        refused(lambda: call(**change), hb.HFX_ERR_SHAPE)
+    for change in (dict(x=40), dict(times=40, times_stride=64), dict(times=32, times_stride=68), dict(out=8), dict(codes=50), dict(scales=6), dict(x_stride=66)):
+        refused(lambda: call(**change), hb.HFX_ERR_ALIGN)
+
+
+def test_what_the_products_refuse():
+    good = dict(codes=16, scales=4, bias=None, n=32, k=64, stride=64)
+    ok = dict(weight={}, rows=2, codes=32, codes_stride=64, scales=8, out=48, out_stride=32, fp32=False)
+
+    def call(**change):
+        a = {**ok, **change}
+        weight = a.pop("weight")
+        hb.hfx_matmul_rows(None if weight is None else Fake(hb.hfx_weight_q8, *{**good, **weight}.values()), *a.values())
+    call(rows=0)
+    for change in (dict(weight=None), dict(weight=dict(codes=None)), dict(weight=dict(scales=None)), dict(codes=None), dict(scales=None), dict(out=None)):
+        refused(lambda: call(**change), hb.HFX_ERR_NULL)
+    for change in (dict(rows=-1), dict(rows=(1 << 21) + 1), dict(weight=dict(n=0)), dict(weight=dict(n=(1 << 21) + 1), out_stride=1 << 22), dict(weight=dict(k=0)), dict(weight=dict(k=56)),
+                   dict(weight=dict(k=131072, stride=131072), codes_stride=131072), dict(weight=dict(stride=48)), dict(weight=dict(stride=1 << 23)), dict(codes_stride=48), dict(codes_stride=-64),
+                   dict(out_stride=31), dict(out_stride=1 << 23), dict(fp32=2), dict(rows=1 << 21, weight=dict(n=1 << 18), out_stride=1 << 18)):
+        refused(lambda: call(**change), hb.HFX_ERR_SHAPE)
+    for change in (dict(weight=dict(codes=24)), dict(weight=dict(scales=6)), dict(weight=dict(bias=5)), dict(weight=dict(stride=72)), dict(codes=40), dict(codes_stride=72), dict(scales=2), dict(out=24)):
+        refused(lambda: call(**change), hb.HFX_ERR_ALIGN)
+
+
+def test_handles_refuse_other_tensors():
+    import torch
+    for weight in (torch.zeros(64), torch.zeros(64, dtype=torch.float16), torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros(128, dtype=torch.bfloat16)[::2],
+                   torch.zeros(64, dtype=torch.bfloat16)):                                   # (the last: in host memory)
+        with pytest.raises(ValueError):
+            hb.make_norm(weight, 1e-6)
+    codes, scales, bias = torch.zeros((8, 64), dtype=torch.int8), torch.zeros(8), torch.zeros(8, dtype=torch.bfloat16)
+    for args in ((codes[0], scales), (codes.float(), scales), (codes.T, scales), (codes, scales[:7]), (codes, scales.double()), (codes, torch.zeros(16)[::2]), (codes, scales, bias[:3]),
+                 (codes, scales, bias.float()), (codes, scales, bias)):
+        with pytest.raises(ValueError):
+            hb.make_weight_q8(*args)
