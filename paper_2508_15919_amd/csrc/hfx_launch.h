@@ -65,8 +65,9 @@ struct MatmulRows {
   void* out;
   long codes_stride, weight_stride, out_stride;
   int rows, n, k;
+  bool past;                 // results go past the caches; filled in by launch_matmul_rows
 };
-hipError_t launch_matmul_rows(const MatmulRows& a, bool fp32, hipStream_t stream);
+hipError_t launch_matmul_rows(MatmulRows a, bool fp32, hipStream_t stream);
 
 // The header as an attention kernel gets it.
 HfxHeader launch_header(const HfxHeader& header, int grid);
