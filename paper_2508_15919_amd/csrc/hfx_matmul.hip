@@ -10,6 +10,8 @@
 
 namespace hfx {
 
+constexpr int kComputeUnits = 256;
+
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
@@ -56,71 +58,59 @@ __device__ __forceinline__ void store_line(const MatmulRows& a, int m, int n, co
 }
 
 // ---------------------------------------------------------------- few rows
-// 16 N channels by 16 R rows to a workgroup, the sum cut into steps of 128 that its W wavefronts take in turn; both operands go straight to registers, U steps ahead.  A lane
-// has 32 bytes in a row of a step, which two matrix instructions take one half each (any order of the values will do that is the same in both operands), so that
-// four lanes ask for a whole line.
-template <int N, int R, int W, int U, bool Fp32>
-__global__ __launch_bounds__(64 * W) void matmul_few_kernel(const MatmulRows a, int tiles_n) {
-  __shared__ i32x4 part[W][N * R][64];
+// 16 channels by up to 16 rows to a workgroup, the sum cut into steps of 128 values that its 16 wavefronts take in turn; both operands go straight to registers, two steps ahead.  A
+// lane has 32 bytes in a row of a step, which two matrix instructions take one half each (any order of the values will do that is the same in both operands), so that
+// four lanes ask for a whole line.  Rows that are not there are the last one again, which costs no further lines.
+// Bound by the weight's way from memory: one row of 4096 to 16384 channels (67 MB) 14.9 us, 5.3 TB/s behind the 2.1 us of a launch.  Four rows to 6144
+// channels 8.8 us; eight wavefronts four steps ahead 9.3.
+template <bool Fp32>
+__global__ __launch_bounds__(1024) void matmul_few_kernel(const MatmulRows a) {
+  constexpr int kWaves = 16, kAhead = 2;
+  __shared__ i32x4 part[kWaves][64];
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), r = lane & 15, j = lane >> 4;
-  const int tile_m = uniform((int)blockIdx.x / tiles_n), tile_n = (int)blockIdx.x - tile_m * tiles_n, n0 = tile_n * 16 * N, m0 = tile_m * 16 * R;
-  const int8_t *w[N], *x[R];
-#pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = a.weight + (long)min(n0 + 16 * i + r, a.n - 1) * a.weight_stride;
-#pragma unroll
-  for (int i = 0; i < R; ++i) x[i] = a.codes + (long)min(m0 + 16 * i + r, a.rows - 1) * a.codes_stride;
-  i32x4 acc[N][R] = {};
-  i32x4 fw[U][N][2], fx[U][R][2];
+  const int n0 = (int)blockIdx.x * 16;
+  const int8_t* const w = a.weight + (long)min(n0 + r, a.n - 1) * a.weight_stride;
+  const int8_t* const x = a.codes + (long)min(r, a.rows - 1) * a.codes_stride;
+  i32x4 acc = {0, 0, 0, 0};
+  i32x4 fw[kAhead][2], fx[kAhead][2];
   auto load = [&](int u, int s) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       int k = s * 128 + 32 * j + 16 * h;
       if (s * 128 + 128 > a.k) k = k < a.k ? k : 0;
-#pragma unroll
-      for (int i = 0; i < N; ++i) fw[u][i][h] = *reinterpret_cast<const i32x4*>(w[i] + k);
-#pragma unroll
-      for (int i = 0; i < R; ++i) fx[u][i][h] = *reinterpret_cast<const i32x4*>(x[i] + k);
+      fw[u][h] = *reinterpret_cast<const i32x4*>(w + k);
+      fx[u][h] = *reinterpret_cast<const i32x4*>(x + k);
     }
   };
   auto multiply = [&](int u, int s) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (s * 128 + 128 > a.k && s * 128 + 32 * j + 16 * h >= a.k) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) fx[u][i][h] = i32x4{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int q = 0; q < R; ++q) acc[i][q] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][i][h], fx[u][q][h], acc[i][q], 0, 0, 0);
+      if (s * 128 + 128 > a.k && s * 128 + 32 * j + 16 * h >= a.k) fx[u][h] = i32x4{0, 0, 0, 0};
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][h], fx[u][h], acc, 0, 0, 0);
     }
   };
   const int steps = (a.k + 127) >> 7;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (wave + u * W < steps) load(u, wave + u * W);
-  for (int s = wave; s < steps; s += U * W) {
+  for (int u = 0; u < kAhead; ++u)
+    if (wave + u * kWaves < steps) load(u, wave + u * kWaves);
+  for (int s = wave; s < steps; s += kAhead * kWaves) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (s + u * W < steps) multiply(u, s + u * W);
-      if (s + (u + U) * W < steps) load(u, s + (u + U) * W);
+    for (int u = 0; u < kAhead; ++u) {
+      if (s + u * kWaves < steps) multiply(u, s + u * kWaves);
+      if (s + (u + kAhead) * kWaves < steps) load(u, s + (u + kAhead) * kWaves);
     }
   }
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int q = 0; q < R; ++q) part[wave][i * R + q][lane] = acc[i][q];
+  part[wave][lane] = acc;
   __syncthreads();
-  for (int b = wave; b < N * R; b += W) {
-    const int m = m0 + 16 * (b % R) + r, n = n0 + 16 * (b / R) + 4 * j;
-    i32x4 c = part[0][b][lane];
+  if (wave != 0) return;
+  const int n = n0 + 4 * j;
+  i32x4 c = part[0][lane];
 #pragma unroll
-    for (int i = 1; i < W; ++i) c += part[i][b][lane];
-    f32x4 weight_scale;
+  for (int i = 1; i < kWaves; ++i) c += part[i][lane];
+  f32x4 weight_scale;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) weight_scale[e] = a.weight_scales[min(n + e, a.n - 1)];
-    if (m < a.rows) store_results<Fp32>(a, m, n, results(c, a.scales[m], weight_scale, a.bias, n, a.n - 1));
-  }
+  for (int e = 0; e < 4; ++e) weight_scale[e] = a.weight_scales[min(n + e, a.n - 1)];
+  if (r < a.rows) store_results<Fp32>(a, r, n, results(c, a.scales[r], weight_scale, a.bias, n, a.n - 1));
 }
 
 // ---------------------------------------------------------------- tiles
@@ -150,16 +140,16 @@ __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned of
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
 }
 
-// A workgroup's BN channels by BM rows.  Stages of B values of the sum go straight from memory to LDS, S of them in a ring; a row's 16-byte pieces
-// are permuted by its number, so that 16 lanes that read the same piece of 16 rows meet all banks.  (WN channels by WM rows, and of a
+// A workgroup's BN channels by BM rows, one tile.  Stages of 128 values of the sum, a line of each row, go straight from memory to LDS, S of them in a ring; a row's eight 16-byte pieces
+// are permuted by bits 1 to 3 of its number, so that 16 lanes that read the same piece of 16 rows meet all banks.  (WN channels by WM rows, and of a
 // stage one part of K, belong to a wavefront.)  The operands of 32 values are read while the matrix instructions of the 32 before them run; the workgroup meets
 // once a stage, ahead of the last of these, when all of the stage has been read: its place is then free for the copies of the stage S behind it.
-template <int BN, int BM, int WN, int WM, int K, int B, int S, bool Fp32>
+template <int BN, int BM, int WN, int WM, int K, int S, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
-  constexpr int kWaves = BN / WN * (BM / WM) * K, kBytes = (BN + BM) * B, kRows = 1024 / B;      // (rows that a copy instruction takes)
-  constexpr int LN = BN / kRows / kWaves, LM = BM / kRows / kWaves, TN = WN / 32, TM = WM / 32, P = B / 32 / K;
-  static_assert(LN * kRows * kWaves == BN && LM * kRows * kWaves == BM, "each wavefront copies whole blocks of rows of both");
-  static_assert((B == 64 || B == 128) && P >= 1 && S * kBytes <= 160 * 1024, "");
+  constexpr int kWaves = BN / WN * (BM / WM) * K, kBytes = (BN + BM) * 128;
+  constexpr int LN = BN / 8 / kWaves, LM = BM / 8 / kWaves, TN = WN / 32, TM = WM / 32, P = 4 / K;
+  static_assert(LN * 8 * kWaves == BN && LM * 8 * kWaves == BM, "each wavefront copies whole blocks of eight rows of both");
+  static_assert(P == 1 || P == 2 || P == 4, "");
   constexpr int kScaleN = S * kBytes, kScaleM = kScaleN + (BN + 63) / 64 * 256, kAll = kScaleM + (BM + 63) / 64 * 256;
   static_assert(kAll <= 160 * 1024, "");
   __shared__ __attribute__((aligned(1024))) char smem[kAll];
@@ -171,23 +161,23 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   const int8_t* const weight = a.weight + (long)n0 * a.weight_stride;
   const int8_t* const codes = a.codes + (long)m0 * a.codes_stride;
   const unsigned lds0 = (unsigned)(uintptr_t)smem;
-  const int stages = (a.k + B - 1) / B, whole = a.k / B, rest = a.k % B;
+  const int stages = (a.k + 127) >> 7, whole = a.k >> 7, rest = a.k & 127;
 
-  // A lane copies one piece of row lane / (B / 16) of a block, the one that belongs in its place.  In a stage with fewer than B values pieces behind them are piece 0 again.
+  // A lane copies one piece of row lane / 8 of a block, the one that belongs in its place.  In a stage with fewer than 128 values the pieces behind them are piece 0 again.
   auto offset = [&](int i, int last, long stride, int values) {
-    const int row = (wave + i * kWaves) * kRows + lane / (B / 16), piece = (lane % (B / 16)) ^ (row >> (B == 128 ? 1 : 2) & (B / 16 - 1));
+    const int row = (wave + i * kWaves) * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
     return (unsigned)min(row, last) * (unsigned)stride + (unsigned)(piece * 16 < values ? piece * 16 : 0);
   };
   unsigned off_n[LN], off_m[LM];
 #pragma unroll
-  for (int i = 0; i < LN; ++i) off_n[i] = offset(i, a.n - 1 - n0, a.weight_stride, B);
+  for (int i = 0; i < LN; ++i) off_n[i] = offset(i, a.n - 1 - n0, a.weight_stride, 128);
 #pragma unroll
-  for (int i = 0; i < LM; ++i) off_m[i] = offset(i, a.rows - 1 - m0, a.codes_stride, B);
+  for (int i = 0; i < LM; ++i) off_m[i] = offset(i, a.rows - 1 - m0, a.codes_stride, 128);
   // copy instruction i of LN + LM of a whole stage
   auto copy = [&](int stage, int slot, int i) {
     const unsigned to = lds0 + slot * kBytes + wave * 1024;
-    if (i < LN) copy_to_lds(weight + (long)stage * B, off_n[i < LN ? i : 0], to + i * kWaves * 1024);
-    else copy_to_lds(codes + (long)stage * B, off_m[i < LN ? 0 : i - LN], to + BN * B + (i - LN) * kWaves * 1024);
+    if (i < LN) copy_to_lds(weight + (long)stage * 128, off_n[i < LN ? i : 0], to + i * kWaves * 1024);
+    else copy_to_lds(codes + (long)stage * 128, off_m[i < LN ? 0 : i - LN], to + BN * 128 + (i - LN) * kWaves * 1024);
   };
   auto copy_any = [&](int stage, int slot) {
     if (stage < whole) {
@@ -196,9 +186,9 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
     } else {
       const unsigned to = lds0 + slot * kBytes + wave * 1024;
 #pragma unroll
-      for (int i = 0; i < LN; ++i) copy_to_lds(weight + (long)stage * B, offset(i, a.n - 1 - n0, a.weight_stride, rest), to + i * kWaves * 1024);
+      for (int i = 0; i < LN; ++i) copy_to_lds(weight + (long)stage * 128, offset(i, a.n - 1 - n0, a.weight_stride, rest), to + i * kWaves * 1024);
 #pragma unroll
-      for (int i = 0; i < LM; ++i) copy_to_lds(codes + (long)stage * B, offset(i, a.rows - 1 - m0, a.codes_stride, rest), to + BN * B + i * kWaves * 1024);
+      for (int i = 0; i < LM; ++i) copy_to_lds(codes + (long)stage * 128, offset(i, a.rows - 1 - m0, a.codes_stride, rest), to + BN * 128 + i * kWaves * 1024);
     }
   };
 
@@ -206,14 +196,14 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   struct Operands {
     i32x4 n[TN], m[TM];
   };
-  const int swizzle = lane >> (B == 128 ? 1 : 2) & (B / 16 - 1), half = lane >> 5;
-  const int at_n = (wn * WN + (lane & 31)) * B, at_m = BN * B + (wm * WM + (lane & 31)) * B;
+  const int swizzle = (lane >> 1) & 7, half = lane >> 5;
+  const int at_n = (wn * WN + (lane & 31)) * 128, at_m = BN * 128 + (wm * WM + (lane & 31)) * 128;
   auto read = [&](Operands& f, int slot, int kk) {
     const char* const from = smem + slot * kBytes + (((2 * kk + half) ^ swizzle) * 16);
 #pragma unroll
-    for (int t = 0; t < TN; ++t) f.n[t] = *reinterpret_cast<const i32x4*>(from + at_n + t * 32 * B);
+    for (int t = 0; t < TN; ++t) f.n[t] = *reinterpret_cast<const i32x4*>(from + at_n + t * 4096);
 #pragma unroll
-    for (int t = 0; t < TM; ++t) f.m[t] = *reinterpret_cast<const i32x4*>(from + at_m + t * 32 * B);
+    for (int t = 0; t < TM; ++t) f.m[t] = *reinterpret_cast<const i32x4*>(from + at_m + t * 4096);
   };
   auto multiply = [&](const Operands& f, int t) {
 #pragma unroll
@@ -268,12 +258,11 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
     ++s;
     slot = behind;
   };
-  static_assert(P == 1 || P % 2 == 0, "a stage begins with the first of the two sets of operands");
   while (s + S < whole) stage(std::true_type());
   while (s < whole) stage(std::false_type());
   if (rest != 0) {
 #pragma unroll 1
-    for (int kk = kpart; kk < B / 32; kk += K) {
+    for (int kk = kpart; kk < 4; kk += K) {
       read(f[0], slot, kk);
       const int keep = (2 * kk + half) * 16 < rest ? -1 : 0;
 #pragma unroll
@@ -346,7 +335,7 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
         const int r = i * kAtOnce + lane / kPieces, piece = lane % kPieces, m = m1 + u * 32 + r;
         u32x4 line = *reinterpret_cast<const u32x4*>(box + r * (2 * WN) + (piece ^ (r / kShare & (kPieces - 1))) * 16);
         if (r >= 16) line = u32x4{line[2], line[3], line[0], line[1]};
-        if (m < a.rows) store_channels<8>(static_cast<__bf16*>(a.out) + m * a.out_stride, reinterpret_cast<const __bf16*>(&line), n1 + piece * 8, a.n);
+        if (m < a.rows) store_line(a, m, n1 + piece * 8, line);
       }
       asm volatile("" ::: "memory");
     }
@@ -574,6 +563,7 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * 64) void matmul_large_kernel(
       channel[c] = weight_scale[t];
       channel[WN + c] = bias[t];
     }
+    asm volatile("" ::: "memory");                  // (other lanes read them; LDS serves a wavefront in order)
     const int row = lane & 31;
     char* const to = box + row * (2 * kWide) + (half ^ (row >> 4)) * 8;
 #pragma unroll
@@ -622,70 +612,78 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * 64) void matmul_large_kernel(
   }
 }
 
+typedef hipError_t (*Launch)(const MatmulRows&, bool, hipStream_t);
+
+static hipError_t launch_few(const MatmulRows& a, bool fp32, hipStream_t stream) {
+  return launch(fp32 ? matmul_few_kernel<true> : matmul_few_kernel<false>, dim3((unsigned)(a.n + 15) / 16), 1024, stream, a);
+}
+template <int BN, int BM, int WN, int WM, int K, int S>
+static hipError_t launch_tiles(const MatmulRows& a, bool fp32, hipStream_t stream) {
+  const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM;
+  return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, S, true> : matmul_tile_kernel<BN, BM, WN, WM, K, S, false>, dim3((unsigned)tiles_n * (unsigned)tiles_m),
+                BN / WN * (BM / WM) * K * 64, stream, a, tiles_n, tiles_m);
+}
+// Workgroups of a large kernel: one for each compute unit.  Where the sum has fewer stages than a ring each takes one tile, because the copies go on into the next tile and not past it.
 template <int BN, int BM, int WN, int WM, int RN, int RM>
 static hipError_t launch_large(const MatmulRows& a, bool fp32, hipStream_t stream) {
-  constexpr int kUnits = 256 * (160 * 1024 / (RN * BN * 128 + RM * BM * 128));
   const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM, tiles = tiles_n * tiles_m;
-  // (the copies of a tile go on into the next one, not past it)
-  const int grid = (a.k + 127) / 128 < RN ? tiles : std::min(tiles, kUnits);
-  return launch(fp32 ? matmul_large_kernel<BN, BM, WN, WM, RN, RM, true> : matmul_large_kernel<BN, BM, WN, WM, RN, RM, false>, dim3((unsigned)grid), BN / WN * (BM / WM) * 64, stream, a,
-                tiles_n, tiles_m);
+  return launch(fp32 ? matmul_large_kernel<BN, BM, WN, WM, RN, RM, true> : matmul_large_kernel<BN, BM, WN, WM, RN, RM, false>,
+                dim3((unsigned)((a.k + 127) / 128 < RN ? tiles : std::min(tiles, kComputeUnits))), BN / WN * (BM / WM) * 64, stream, a, tiles_n, tiles_m);
 }
 
-template <int BN, int BM, int WN, int WM, int K, int B, int S>
-static hipError_t launch_tiles(const MatmulRows& a, bool fp32, hipStream_t stream) {
-  constexpr unsigned kThreads = BN / WN * (BM / WM) * K * 64;
-  const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM;
-  return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, B, S, true> : matmul_tile_kernel<BN, BM, WN, WM, K, B, S, false>, dim3((unsigned)tiles_n * (unsigned)tiles_m),
-                kThreads, stream, a, tiles_n, tiles_m);
-}
-
-template <int N, int R, int W, int U>
-static hipError_t launch_few(const MatmulRows& a, bool fp32, hipStream_t stream) {
-  const int tiles_n = (a.n + 16 * N - 1) / (16 * N), tiles_m = (a.rows + 16 * R - 1) / (16 * R);
-  return launch(fp32 ? matmul_few_kernel<N, R, W, U, true> : matmul_few_kernel<N, R, W, U, false>, dim3((unsigned)tiles_n * (unsigned)tiles_m), 64 * W, stream, a, tiles_n);
-}
-
-#ifdef HFX_PROBE
-int g_variant = -1;
-extern "C" void hfx_probe_variant(int v) { g_variant = v; }
-static hipError_t probe(const MatmulRows& a, bool fp32, hipStream_t stream) {
-  switch (g_variant) {
-    case 2: return launch_tiles<32, 64, 32, 32, 2, 128, 6>(a, fp32, stream);
-    case 3: return launch_tiles<64, 64, 32, 32, 1, 128, 4>(a, fp32, stream);
-    case 4: return launch_tiles<128, 128, 64, 32, 1, 128, 2>(a, fp32, stream);
-    case 5: return launch_large<128, 128, 32, 64, 4, 4>(a, fp32, stream);
-    case 6: return launch_large<256, 128, 64, 64, 3, 3>(a, fp32, stream);
-    case 8: return launch_large<256, 160, 32, 160, 3, 3>(a, fp32, stream);
-    case 9: return launch_large<256, 192, 64, 96, 3, 2>(a, fp32, stream);
-    case 10: return launch_large<256, 256, 64, 128, 3, 2>(a, fp32, stream);
-    case 13: return launch_tiles<64, 128, 32, 64, 1, 128, 3>(a, fp32, stream);
-    case 15: return launch_few<1, 1, 16, 2>(a, fp32, stream);
-    case 16: return launch_tiles<32, 32, 32, 32, 4, 128, 6>(a, fp32, stream);
-    case 17: return launch_tiles<64, 64, 32, 32, 1, 128, 3>(a, fp32, stream);
-    case 18: return launch_tiles<32, 64, 32, 32, 2, 128, 4>(a, fp32, stream);
-    case 19: return launch_tiles<32, 32, 32, 32, 4, 128, 4>(a, fp32, stream);
-    case 20: return launch_tiles<128, 64, 64, 32, 1, 128, 2>(a, fp32, stream);
-    case 21: return launch_tiles<64, 128, 32, 64, 1, 128, 2>(a, fp32, stream);
-    case 22: return launch_tiles<128, 128, 64, 64, 1, 128, 2>(a, fp32, stream);
-    case 23: return launch_tiles<64, 64, 64, 32, 1, 128, 4>(a, fp32, stream);
-    case 24: return launch_tiles<64, 64, 64, 64, 4, 128, 4>(a, fp32, stream);
-    case 25: return launch_tiles<64, 64, 32, 64, 2, 128, 4>(a, fp32, stream);
-  }
-  return hipErrorInvalidValue;
-}
-#endif
+// What a product takes with each kernel, in us: `start`, and for each round of tiles over the chip `round` and each stage of 128 values of the sum
+// stage[t - 1], t being the tiles that meet on a compute unit (`most` at most).  Fitted to 2300 times of 190 products (1 to 8224 rows, 1280 to 16384 channels, sums of 512 to 16384 values, buffers that
+// change from call to call): off by 7 to 15 % (mean square), and the kernel that it names takes 1.01 times the fastest one's time on average, 1.33 at worst.  Why there are several, in us
+// (rows, k, channels; that kernel, then the next best one among the others):
+//   one row 4096 16384      few   14.9   32x32   17.2        37    8192  1280   32x32    9.1   32x64   11.2
+//   64  4096  6144       32x64   11.0   32x32   11.9        128   4096  6144   64x64   13.0   32x64   15.4
+//   256 1024  8192      128x64    6.3   64x64    6.6        777   1024  8192   128x128, two to a unit 13.3   256x128 14.1
+//   777 8192  4096     128x128   39.4  128x64   45.9        1500  8192  4096  128x192   53.4   256x128  57.8
+//   512 4096  16384    256x128   38.4  128x128  41.1        8224  4096  6144  256x160  198.9   256x256 205.5
+//   4128 4096 16384    256x192  251.4  256x256 263.4        8192  8192  8192  256x256  434     256x192 494
+// (channels x rows of a tile).  A product fills the chip with the largest tiles that leave little of a last round empty: the larger ones ask for fewer lines, of which a compute unit gets 45 to 75 GB/s.
+struct Way {
+  Launch launch;
+  int bn, bm, threads, most;
+  float start, round, stage[3];
+};
+static const Way kWays[] = {
+    {launch_few, 16, 16, 1024, 2, 2.1f, 0.42f, {0.10f, 0.21f}},
+    {launch_tiles<32, 32, 32, 32, 4, 6>, 32, 32, 256, 3, 2.0f, 0.94f, {0.13f, 0.22f, 0.29f}},
+    {launch_tiles<32, 64, 32, 32, 2, 6>, 32, 64, 256, 2, 1.9f, 1.25f, {0.16f, 0.31f}},
+    {launch_tiles<64, 64, 32, 32, 1, 4>, 64, 64, 256, 2, 1.2f, 1.6f, {0.24f, 0.42f}},
+    {launch_tiles<128, 64, 64, 32, 1, 3>, 128, 64, 256, 2, 0.4f, 2.6f, {0.40f, 0.67f}},
+    {launch_tiles<128, 128, 64, 32, 1, 2>, 128, 128, 512, 2, 0.0f, 3.05f, {0.78f, 1.05f}},
+    {launch_large<128, 128, 32, 64, 4, 4>, 128, 128, 512, 1, 2.5f, 2.0f, {0.53f}},
+    {launch_large<128, 192, 32, 96, 3, 3>, 128, 192, 512, 1, 1.8f, 3.1f, {0.68f}},
+    {launch_large<256, 128, 64, 64, 3, 3>, 256, 128, 512, 1, 2.4f, 3.6f, {0.80f}},
+    {launch_large<256, 160, 32, 160, 3, 3>, 256, 160, 512, 1, 1.8f, 5.1f, {0.94f}},
+    {launch_large<256, 192, 64, 96, 3, 2>, 256, 192, 512, 1, 3.0f, 4.3f, {1.17f}},
+    {launch_large<256, 256, 64, 128, 3, 2>, 256, 256, 512, 1, 4.4f, 4.6f, {1.43f}},
+};
 
 hipError_t launch_matmul_rows(MatmulRows a, bool fp32, hipStream_t stream) {
+  // Results of more than 64 MB go past the caches, where they push out what the tiles share: 4128 rows to 16384 channels 268 -> 255 us, 8192 rows over 1024 values to 8192
+  // channels 109 -> 89 (21 MB of results: 80.6 and 79.8).
   a.past = !fp32 && a.out_stride % 8 == 0 && 2l * a.rows * a.n > (64l << 20);
-#ifdef HFX_PROBE
-  if (g_variant >= 0) return probe(a, fp32, stream);
-#endif
-  if (a.rows <= 16) return launch_few<1, 1, 8, 4>(a, fp32, stream);
-  if (a.rows <= 32) return launch_few<1, 2, 8, 4>(a, fp32, stream);
-  if ((long)a.rows * a.n <= 64l * 64 * 512) return launch_tiles<64, 64, 32, 32, 1, 128, 4>(a, fp32, stream);
-  if ((long)a.rows * a.n <= 128l * 128 * 512) return launch_tiles<128, 128, 64, 32, 1, 128, 2>(a, fp32, stream);
-  return launch_large<256, 256, 64, 128, 3, 2>(a, fp32, stream);
+  const int stages = (a.k + 127) / 128;
+  const Way* best = nullptr;
+  float least = 0.0f;
+  for (const Way& w : kWays) {
+    if (w.launch == launch_few && a.rows > 16) continue;
+    const long tiles = (long)((a.n + w.bn - 1) / w.bn) * ((a.rows + w.bm - 1) / w.bm), chip = (long)kComputeUnits * w.most;
+    if (tiles * w.threads >= 1l << 32) continue;
+    const long rounds = tiles / chip, left = tiles - rounds * chip;
+    float us = w.start + (float)rounds * (w.round + (float)stages * w.stage[w.most - 1]);
+    if (left) us += w.round + (float)stages * w.stage[(left - 1) / kComputeUnits];
+    // up to eight rows ask for fewer lines (4 rows of 4096 to 16384 channels 16.0 us, 16 rows 20.6)
+    if (w.launch == launch_few && a.rows <= 8) us *= 0.85f;
+    if (!best || us < least) {
+      best = &w;
+      least = us;
+    }
+  }
+  return best->launch(a, fp32, stream);
 }
 
 }  // namespace hfx

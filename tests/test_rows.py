@@ -325,12 +325,37 @@ def test_products_of_a_layers_size(rows, n, k):
     check_product(torch, rows, n, k, True, False)
 
 
+# Sizes at which the tiles of every kernel come up, with parts of tiles at both edges, sums of one stage and up, whole and not, one tile to a workgroup and several.
+FILLING = [(771, 8208, 4099), (1491, 4112, 4100), (4100, 400, 4100), (4100, 384, 4100), (3000, 144, 3000), (3000, 784, 6100), (2047, 1040, 16390), (5000, 512, 5000), (5000, 384, 5003),
+           (5000, 272, 5000), (1500, 1040, 8200), (8219, 256, 6147), (8219, 528, 6147), (777, 1024, 8192), (1000, 2000, 1500), (2050, 400, 9000), (600, 512, 12000), (1030, 512, 9001),
+           (6000, 16, 7001), (2000, 128, 5000), (4096, 1024, 4096), (520, 8192, 4096), (3100, 2064, 2050)]
+
+
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows", [1, 30, 80, 260])
-def test_the_longest_sums(rows):
+@pytest.mark.parametrize("rows,k,n", FILLING)
+def test_products_that_fill_the_chip(rows, k, n):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows + n)
+    codes, weight = (torch.randint(-128, 128, (m, k), dtype=torch.int8, device="cuda", generator=gen) for m in (rows, n))
+    scales, weight_scales = (torch.rand(m, device="cuda", generator=gen) + 0.01 for m in (rows, n))
+    bias = torch.empty(n, dtype=torch.bfloat16, device="cuda").normal_(0.0, 1000.0, generator=gen)
+    sums = (codes.double() @ weight.double().T).float()         # exact in 64 bits, rounded once
+    for fp32, with_bias in ((False, False), (True, False), (False, True)):
+        want = sums * scales[:, None] * weight_scales
+        if with_bias:
+            want = want + bias.float()
+        out = torch.full((rows + 2, n), 7.0, dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda")
+        hb.hfx_matmul_rows(hb.make_weight_q8(weight, weight_scales, bias if with_bias else None), rows, codes, k, scales, out, n, fp32, torch.cuda.current_stream())
+        assert bool((out[rows:] == 7.0).all())
+        assert torch.equal(out[:rows], want.to(out.dtype))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,n", [(1, 260), (30, 260), (80, 260), (260, 260), (700, 4100)])
+def test_the_longest_sums(rows, n):
     """All codes -128 over the longest row: 2^31 - 2^18, the largest sum there is; and the smallest."""
     import torch
-    k, n = 131056, 260
+    k = 131056
     codes, weight = np.full((rows, k), -128, np.int8), np.full((n, k), -128, np.int8)
     weight[1::2] = 127
     one = np.ones(rows, np.float32), np.ones(n, np.float32)
