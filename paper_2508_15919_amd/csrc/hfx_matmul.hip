@@ -130,6 +130,8 @@ __device__ __forceinline__ const int8_t* uniform_address(const int8_t* p) {
   const uint64_t x = (uint64_t)p;
   return (const int8_t*)((uint64_t)(unsigned)uniform((int)(x >> 32)) << 32 | (unsigned)uniform((int)x));
 }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"      // m0 is reserved, and clobbered all the same
 // Copies 64 pieces of 16 bytes to LDS, lane after lane from `lds` on.
 __device__ __forceinline__ void copy_to_lds(const int8_t* base, unsigned offset, unsigned lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(uniform_address(base)), "s"(uniform((int)lds)) : "memory", "m0");
@@ -139,6 +141,7 @@ __device__ __forceinline__ void copy_to_lds(const int8_t* base, unsigned offset,
 __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned offset, unsigned lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // A workgroup's BN channels by BM rows, one tile.  Stages of 128 values of the sum, a line of each row, go straight from memory to LDS, S of them in a ring; a row's eight 16-byte pieces
 // are permuted by bits 1 to 3 of its number, so that 16 lanes that read the same piece of 16 rows meet all banks.  (WN channels by WM rows, and of a
