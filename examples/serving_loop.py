@@ -3,10 +3,12 @@
 A decoder with random weights serves a queue of prompts: `hfx_compose_step` admits prompts beside the running requests' next tokens, one descriptor
 is built per step and used by every layer, and each layer runs its projection, `hfx_rope_append_kv(_mx)` (rotation, queries packed, keys and values into
 their pages) and `hfx_mixed_paged_attention(_mx)`.  Both pools serve the same requests; the second takes the tokens that the first chose, so that their
-logits can be compared.
+logits can be compared.  With `--weights 8` the projections are those of `hfx_matmul_rows`: weights and the rows that meet them in 8 bits, which `hfx_rms_norm`
+(with the residual's addition) and `hfx_quantise_rows` (attention's rows, the activation) write.
 
     python examples/serving_loop.py                      # 2 layers of 32 / 8 heads of 128, 24 prompts, 32 tokens each
     python examples/serving_loop.py --layers 4 --requests 64 --new-tokens 64
+    python examples/serving_loop.py --weights 8
 """
 from __future__ import annotations
 
@@ -42,6 +44,22 @@ class Decoder:
         angle = torch.arange(max_positions, device="cuda", dtype=torch.float64)[:, None] * 10000.0 ** (
             -torch.arange(d // 2, device="cuda", dtype=torch.float64) / (d // 2))
         self.rope = hb.make_rope(torch.cat((angle.cos(), angle.sin()), 1).float(), d)
+
+
+class Weights8:
+    """A decoder's weights in 8 bits, a scale for each output channel, and its norms."""
+
+    def __init__(self, model):
+        hidden, stream = model.hq * model.d, torch.cuda.current_stream()
+
+        def handle(weight):
+            n, k = weight.shape
+            codes, scales = torch.empty((n, k), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+            hb.hfx_quantise_rows(hb.HFX_ACT_NONE, n, k, weight, k, None, 0, None, codes, scales, stream)
+            return hb.make_weight_q8(codes, scales)
+        self.qkv, self.out, self.up, self.down = ([handle(w) for w in ws] for ws in (model.qkv, model.out, model.up, model.down))
+        self.embedding = handle(model.embedding)
+        self.norm = hb.make_norm(torch.ones(hidden, dtype=torch.bfloat16, device="cuda"), 1e-6)
 
 
 def norm(x):
@@ -97,9 +115,45 @@ def forward(model, cache, step, tokens, last_rows, held=None):
     return norm(x[last_rows]).float() @ model.embedding.float().T
 
 
-def serve(model, cache, prompts, new_tokens, forced=None, held=None):
+def forward_8(model, weights, cache, step, tokens, last_rows):
+    """`forward` with the projections in 8 bits."""
+    stream = torch.cuda.current_stream()
+    hq, hkv, d, n = model.hq, model.hkv, model.d, len(tokens)
+    hidden = hq * d
+
+    def rows(cols, dtype=torch.bfloat16, count=n):
+        return torch.empty((count, cols), dtype=dtype, device="cuda")
+    x = model.embedding[tokens]
+    q, attended, qkv, up, added = rows(hidden), rows(hidden), rows((hq + 2 * hkv) * d), rows(2 * hidden), rows(hidden)
+    codes, wide_codes, scales = rows(hidden, torch.int8), rows(2 * hidden, torch.int8), torch.empty(n, device="cuda")
+    qs, ks, vs = qkv.split((hidden, hkv * d, hkv * d), 1)
+
+    def product(weight, codes, k, out):
+        hb.hfx_matmul_rows(weight, n, codes, k, scales, out, out.shape[1], False, stream)
+    for layer in range(model.layers):
+        if layer == 0:
+            hb.hfx_rms_norm(weights.norm, n, x, hidden, None, 0, None, None, codes, scales, stream)
+        else:
+            hb.hfx_rms_norm(weights.norm, n, added, hidden, x, hidden, x, None, codes, scales, stream)      # x takes what the layer before added
+        product(weights.qkv[layer], codes, hidden, qkv)
+        cache.append(cache.shape, model.rope, qs, qs.stride(0), ks, ks.stride(0), vs, vs.stride(0), q, cache.pools[layer], step.host, step.device, stream)
+        cache.attend(cache.shape, q, cache.pools[layer], step.host, step.device, step.workspace, attended, stream)
+        hb.hfx_quantise_rows(hb.HFX_ACT_NONE, n, hidden, attended, hidden, None, 0, None, codes, scales, stream)
+        product(weights.out[layer], codes, hidden, added)
+        hb.hfx_rms_norm(weights.norm, n, added, hidden, x, hidden, x, None, codes, scales, stream)
+        product(weights.up[layer], codes, hidden, up)
+        hb.hfx_quantise_rows(hb.HFX_ACT_SILU, n, 2 * hidden, up, 2 * hidden, None, 0, None, wide_codes, scales, stream)
+        product(weights.down[layer], wide_codes, 2 * hidden, added)
+    count = len(last_rows)
+    x, added, logits = x[last_rows], added[last_rows], rows(len(model.embedding), torch.float32, count)
+    hb.hfx_rms_norm(weights.norm, count, added, hidden, x, hidden, x, None, codes, scales, stream)
+    hb.hfx_matmul_rows(weights.embedding, count, codes, hidden, scales, logits, logits.shape[1], True, stream)
+    return logits
+
+
+def serve(model, cache, prompts, new_tokens, forced=None, held=None, weights=None):
     """Serves the prompts (lists of token ids) until each has `new_tokens` tokens.  Returns their tokens, their logits and the steps' times in seconds.
-    forced: tokens to go on with in place of the likeliest ones."""
+    forced: tokens to go on with in place of the likeliest ones.  weights: the model's Weights8, to serve with those."""
     latency = hb.hfx_latency_model(1e-3, 2e-5, 2e-2)              # seconds: of a prefill batch, of each of its tokens, of a decode iteration
     waiting = list(range(len(prompts)))
     running, pages, length = [], {}, {}
@@ -124,7 +178,8 @@ def serve(model, cache, prompts, new_tokens, forced=None, held=None):
             have += [cache.free.pop() for _ in range(need)]
         step = Step(cache, kind, q_len, ctx_len, [pages[r] for r in batch])
         packed = [t for r in batch for t in (tokens[r][-1:] if r in running else prompts[r])]
-        rows = forward(model, cache, step, torch.tensor(packed, device="cuda"), torch.from_numpy(np.cumsum(q_len) - 1).cuda(), held)
+        packed, last_rows = torch.tensor(packed, device="cuda"), torch.from_numpy(np.cumsum(q_len) - 1).cuda()
+        rows = forward_8(model, weights, cache, step, packed, last_rows) if weights else forward(model, cache, step, packed, last_rows, held)
         picked = rows.argmax(1).tolist()                          # (waits for the step)
         times.append(time.perf_counter() - started)
         for i, r in enumerate(batch):
@@ -148,6 +203,7 @@ def main(argv=None):
     ap.add_argument("--requests", type=int, default=24)
     ap.add_argument("--longest-prompt", type=int, default=1500)
     ap.add_argument("--new-tokens", type=int, default=32)
+    ap.add_argument("--weights", type=int, default=16, choices=(16, 8), help="bits of the projections' weights and rows")
     ap.add_argument("--seed", type=int, default=0)
     a = ap.parse_args(argv)
     rng = np.random.default_rng(a.seed)
@@ -155,20 +211,21 @@ def main(argv=None):
     prompts = [rng.integers(0, vocab, rng.integers(1, a.longest_prompt + 1)).tolist() for _ in range(a.requests)]
     num_pages = sum(-(-(len(p) + a.new_tokens) // PAGE) for p in prompts)
     model = Decoder(a.q_heads, a.kv_heads, a.head_dim, a.layers, vocab, a.longest_prompt + a.new_tokens, a.seed)
+    weights = Weights8(model) if a.weights == 8 else None
     served, held = {}, []
     for four_bits in (False, True):
         cache = Cache(model, num_pages, four_bits)
         forced = served[False][0] if four_bits else None
-        tokens, logits, times = served[four_bits] = serve(model, cache, prompts, a.new_tokens, forced, held)
+        tokens, logits, times = served[four_bits] = serve(model, cache, prompts, a.new_tokens, forced, held, weights)
         assert len(cache.free) == num_pages
         print("%-5s pool: %7.1f MB, %d steps, median %.2f ms a step" % (
             "4-bit" if four_bits else "bf16", sum(p.numel() for p in cache.pools) / 1e6, len(times), 1e3 * float(np.median(times))), flush=True)
     x, y = (torch.cat([served[f][1][r] for r in range(a.requests)]) for f in (False, True))
     off = float((x - y).norm() / x.norm())
     same = float((x.argmax(1) == y.argmax(1)).float().mean())
-    print("logits over the 4-bit pool against those over the bf16 pool: %.3f off (relative), the same likeliest token in %.1f %% of %d; "
-          "values in the pool %.3f off" % (off, 100 * same, len(x), max(held)))
-    return {"off": off, "same": same, "values_off": max(held), "tokens": {f: served[f][0] for f in served}}
+    print("logits over the 4-bit pool against those over the bf16 pool: %.3f off (relative), the same likeliest token in %.1f %% of %d%s" % (
+        off, 100 * same, len(x), "; values in the pool %.3f off" % max(held) if held else ""))
+    return {"off": off, "same": same, "values_off": max(held) if held else None, "tokens": {f: served[f][0] for f in served}}
 
 
 if __name__ == "__main__":
