@@ -636,7 +636,7 @@ static hipError_t launch_large(const MatmulRows& a, bool fp32, hipStream_t strea
 
 // What a product takes with each kernel, in us: `start`, and for each round of tiles over the chip `round` and each stage of 128 values of the sum
 // stage[t - 1], t being the tiles that meet on a compute unit (`most` at most).  Fitted to 2300 times of 190 products (1 to 8224 rows, 1280 to 16384 channels, sums of 512 to 16384 values, buffers that
-// change from call to call): off by 7 to 15 % (mean square), and the kernel that it names takes 1.01 times the fastest one's time on average, 1.33 at worst.  Why there are several, in us
+// change from call to call): the kernel that it names takes 1.01 times the fastest one's time on average, 1.17 at worst.  Why there are several, in us
 // (rows, k, channels; that kernel, then the next best one among the others):
 //   one row 4096 16384      few   14.9   32x32   17.2        37    8192  1280   32x32    9.1   32x64   11.2
 //   64  4096  6144       32x64   11.0   32x32   11.9        128   4096  6144   64x64   13.0   32x64   15.4
@@ -651,18 +651,18 @@ struct Way {
   float start, round, stage[3];
 };
 static const Way kWays[] = {
-    {launch_few, 16, 16, 1024, 2, 2.1f, 0.42f, {0.10f, 0.21f}},
-    {launch_tiles<32, 32, 32, 32, 4, 6>, 32, 32, 256, 3, 2.0f, 0.94f, {0.13f, 0.22f, 0.29f}},
-    {launch_tiles<32, 64, 32, 32, 2, 6>, 32, 64, 256, 2, 1.9f, 1.25f, {0.16f, 0.31f}},
-    {launch_tiles<64, 64, 32, 32, 1, 4>, 64, 64, 256, 2, 1.2f, 1.6f, {0.24f, 0.42f}},
-    {launch_tiles<128, 64, 64, 32, 1, 3>, 128, 64, 256, 2, 0.4f, 2.6f, {0.40f, 0.67f}},
-    {launch_tiles<128, 128, 64, 32, 1, 2>, 128, 128, 512, 2, 0.0f, 3.05f, {0.78f, 1.05f}},
-    {launch_large<128, 128, 32, 64, 4, 4>, 128, 128, 512, 1, 2.5f, 2.0f, {0.53f}},
-    {launch_large<128, 192, 32, 96, 3, 3>, 128, 192, 512, 1, 1.8f, 3.1f, {0.68f}},
-    {launch_large<256, 128, 64, 64, 3, 3>, 256, 128, 512, 1, 2.4f, 3.6f, {0.80f}},
-    {launch_large<256, 160, 32, 160, 3, 3>, 256, 160, 512, 1, 1.8f, 5.1f, {0.94f}},
-    {launch_large<256, 192, 64, 96, 3, 2>, 256, 192, 512, 1, 3.0f, 4.3f, {1.17f}},
-    {launch_large<256, 256, 64, 128, 3, 2>, 256, 256, 512, 1, 4.4f, 4.6f, {1.43f}},
+    {launch_few, 16, 16, 1024, 2, 2.0f, 0.48f, {0.10f, 0.20f}},
+    {launch_tiles<32, 32, 32, 32, 4, 6>, 32, 32, 256, 3, 2.0f, 1.0f, {0.13f, 0.21f, 0.29f}},
+    {launch_tiles<32, 64, 32, 32, 2, 6>, 32, 64, 256, 2, 1.5f, 1.6f, {0.175f, 0.275f}},
+    {launch_tiles<64, 64, 32, 32, 1, 4>, 64, 64, 256, 2, 1.4f, 1.4f, {0.255f, 0.405f}},
+    {launch_tiles<128, 64, 64, 32, 1, 3>, 128, 64, 256, 2, 0.5f, 2.6f, {0.41f, 0.655f}},
+    {launch_tiles<128, 128, 64, 32, 1, 2>, 128, 128, 512, 2, 0.0f, 3.6f, {0.735f, 1.065f}},
+    {launch_large<128, 128, 32, 64, 4, 4>, 128, 128, 512, 1, 5.8f, 1.5f, {0.52f}},
+    {launch_large<128, 192, 32, 96, 3, 3>, 128, 192, 512, 1, 3.2f, 3.0f, {0.695f}},
+    {launch_large<256, 128, 64, 64, 3, 3>, 256, 128, 512, 1, 4.7f, 3.0f, {0.83f}},
+    {launch_large<256, 160, 32, 160, 3, 3>, 256, 160, 512, 1, 2.2f, 4.7f, {1.0f}},
+    {launch_large<256, 192, 64, 96, 3, 2>, 256, 192, 512, 1, 6.7f, 2.5f, {1.225f}},
+    {launch_large<256, 256, 64, 128, 3, 2>, 256, 256, 512, 1, 7.7f, 3.4f, {1.46f}},
 };
 
 hipError_t launch_matmul_rows(MatmulRows a, bool fp32, hipStream_t stream) {
