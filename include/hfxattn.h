@@ -376,7 +376,8 @@ hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, c
  * top / 127 and a code the nearest whole number, ties to even, to the value times 127 / top, so
  * codes lie in [-127, 127].  A row with a value that is not finite has NaN for its scale and codes of zero.
  * Row lengths (cols, k) are multiples of 16 from 16 to 131056; strides are in elements, no less
- * than the row and at most 4194304; there are at most 2097152 rows.  Calls with no rows do nothing.
+ * than the row and at most 4194304; there are at most 2097152 rows.  Calls with no rows do nothing, and ask nothing of the
+ * buffers of rows.
  * ---------------------------------------------------------------------------------------- */
 
 /* A norm's weight. */
@@ -398,7 +399,7 @@ typedef struct {
  *                value is formed from h * weight, exact in fp32 unless that overflows (it then counts as not finite), the factor 127 / top and their product rounded to
  *                fp32; the scale is that of the row of h * weight, times r.
  * Buffers are 16-byte aligned (scales: 4) and overlap in no other way.  Asynchronous on `stream`; allocates nothing.
- * Errors: HFX_ERR_NULL, HFX_ERR_SHAPE (rows < 0; cols, eps or a stride not as above), HFX_ERR_ALIGN (also: a stride that is no
+ * Errors: HFX_ERR_NULL, HFX_ERR_SHAPE (rows < 0; cols, eps or a stride not as above; in place and not packed), HFX_ERR_ALIGN (also: a stride that is no
  * multiple of 8), HFX_ERR_DEVICE.
  */
 hfx_status hfx_rms_norm(const hfx_norm* norm, int32_t rows, const void* x, int64_t x_stride,

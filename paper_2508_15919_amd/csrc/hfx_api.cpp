@@ -288,14 +288,15 @@ hfx_status hfx_mixed_paged_attention_mx(const hfx_shape* shape, const void* q, c
 
 hfx_status hfx_rms_norm(const hfx_norm* norm, int32_t rows, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* sum,
                         void* out, void* codes, float* scales, void* stream) {
-  if (!norm || !norm->weight || !x || (residual == nullptr) != (sum == nullptr) || (codes == nullptr) != (scales == nullptr) || (!out && !codes))
-    return HFX_ERR_NULL;
+  if (!norm || !norm->weight) return HFX_ERR_NULL;
   if (!rows_ok(rows, norm->cols) || !(norm->eps >= 0.0f && norm->eps <= 3.0e38f)) return HFX_ERR_SHAPE;
+  if (rows == 0) return HFX_OK;      // (buffers of no rows may have no address)
+  if (!x || (residual == nullptr) != (sum == nullptr) || (codes == nullptr) != (scales == nullptr) || (!out && !codes)) return HFX_ERR_NULL;
   if (!stride_ok(x_stride, norm->cols) || (residual && !stride_ok(residual_stride, norm->cols))) return HFX_ERR_SHAPE;
+  if (rows > 1 && sum && ((sum == x && x_stride != norm->cols) || (sum == residual && residual_stride != norm->cols))) return HFX_ERR_SHAPE;
   if (!aligned16(norm->weight) || !aligned16(x) || !aligned16(residual) || !aligned16(sum) || !aligned16(out) || !aligned16(codes) || !aligned4(scales) ||
       (x_stride | (residual ? residual_stride : 0)) % 8 != 0)
     return HFX_ERR_ALIGN;
-  if (rows == 0) return HFX_OK;
   hfx::RmsNorm a = {};
   a.x = static_cast<const uint16_t*>(x);
   a.residual = static_cast<const uint16_t*>(residual);
@@ -313,12 +314,13 @@ hfx_status hfx_rms_norm(const hfx_norm* norm, int32_t rows, const void* x, int64
 
 hfx_status hfx_quantise_rows(int32_t activation, int32_t rows, int32_t cols, const void* x, int64_t x_stride, const void* times, int64_t times_stride,
                              void* out, void* codes, float* scales, void* stream) {
-  if (!x || (codes == nullptr) != (scales == nullptr) || (!out && !codes)) return HFX_ERR_NULL;
   if ((activation != HFX_ACT_NONE && activation != HFX_ACT_SILU) || !rows_ok(rows, cols)) return HFX_ERR_SHAPE;
+  if (rows == 0) return HFX_OK;
+  if (!x || (codes == nullptr) != (scales == nullptr) || (!out && !codes)) return HFX_ERR_NULL;
   if (!stride_ok(x_stride, cols) || (times && !stride_ok(times_stride, cols))) return HFX_ERR_SHAPE;
+  if (out && ((out == x && (codes || (rows > 1 && x_stride != cols))) || (out == times && (codes || (rows > 1 && times_stride != cols))))) return HFX_ERR_SHAPE;
   if (!aligned16(x) || !aligned16(times) || !aligned16(out) || !aligned16(codes) || !aligned4(scales) || (x_stride | (times ? times_stride : 0)) % 8 != 0)
     return HFX_ERR_ALIGN;
-  if (rows == 0) return HFX_OK;
   hfx::QuantiseRows a = {};
   a.x = static_cast<const uint16_t*>(x);
   a.times = static_cast<const uint16_t*>(times);
@@ -334,13 +336,14 @@ hfx_status hfx_quantise_rows(int32_t activation, int32_t rows, int32_t cols, con
 
 hfx_status hfx_matmul_rows(const hfx_weight_q8* weight, int32_t rows, const void* codes, int64_t codes_stride, const float* scales, void* out,
                          int64_t out_stride, int32_t fp32, void* stream) {
-  if (!weight || !weight->codes || !weight->scales || !codes || !scales || !out) return HFX_ERR_NULL;
+  if (!weight || !weight->codes || !weight->scales) return HFX_ERR_NULL;
   if (!rows_ok(rows, weight->k) || weight->n < 1 || weight->n > kMostRows || (int64_t)rows * weight->n > kMostResults || (fp32 != 0 && fp32 != 1)) return HFX_ERR_SHAPE;
+  if (rows == 0) return HFX_OK;
+  if (!codes || !scales || !out) return HFX_ERR_NULL;
   if (!stride_ok(codes_stride, weight->k) || !stride_ok(weight->stride, weight->k) || !stride_ok(out_stride, weight->n)) return HFX_ERR_SHAPE;
   if (!aligned16(weight->codes) || !aligned4(weight->scales) || (reinterpret_cast<uintptr_t>(weight->bias) & 1u) != 0 || !aligned16(codes) ||
       !aligned4(scales) || !aligned16(out) || (codes_stride | weight->stride) % 16 != 0)
     return HFX_ERR_ALIGN;
-  if (rows == 0) return HFX_OK;
   hfx::MatmulRows a = {};
   a.codes = static_cast<const int8_t*>(codes);
   a.weight = static_cast<const int8_t*>(weight->codes);

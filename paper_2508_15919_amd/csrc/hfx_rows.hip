@@ -193,7 +193,7 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
   }
   reduce_row<T, true>(top, sum);
   const double r = 1.0 / __builtin_sqrt(sum / (double)a.cols + (double)a.eps);
-  const float rf = (float)r;
+  const float up = r > 0x1p100 ? 0x1p64f : 1.0f, rf = (float)(r / (double)up);      // (rows of the smallest numbers, without eps, have an r past the range of fp32)
   const Scaling s = scaling_of(top);
   if (a.codes && threadIdx.x == 0) a.scales[row] = (float)((double)s.top * r / 127.0);
   auto second = [&](int c, const float* v) {
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
     }
     if (a.out) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = v[e] * rf * w[e];
+      for (int e = 0; e < 8; ++e) y[e] = v[e] * up * rf * w[e];
       *reinterpret_cast<u32x4*>(a.out + row * a.cols + c) = narrow8(y);
     }
   };

@@ -138,6 +138,55 @@ def test_norm_of_extreme_rows(cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cols", [64, 4096])
+def test_norm_of_tiny_rows_without_eps(cols):
+    """1 / sqrt(mean) past the range of 32 bits; the codes' scale is that of a largest magnitude of 2^-100."""
+    import torch
+    g = np.random.default_rng(cols)
+    x = bf16(g.standard_normal((5, cols)))
+    for i, size in enumerate((2.0 ** -126, 2.0 ** -131, 2.0 ** -110, 2.0 ** -99)):
+        x[i] = bf16(size * x[i])
+    weight = bf16(1.0 + 0.3 * g.standard_normal(cols))
+    got, want = run_norm(torch, x, None, weight, 0.0), norm_oracle(x, None, weight, 0.0)
+    assert (np.abs(got[1] - want[1]) <= (HALF_BF16 + 3 * 2.0 ** -24) * np.abs(want[1])).all()
+    assert np.array_equal(got[2], want[2]) and not got[2][:2].any() and got[2][3:].any()      # (127 2^100 of 2^-110 is an eighth: four of those are a code of 1)
+
+
+@pytest.mark.gpu
+def test_the_most_rows_and_channels():
+    import torch
+    g, stream, most = torch.Generator(device="cuda").manual_seed(3), torch.cuda.current_stream(), 1 << 21
+    x = torch.randn((most, 16), generator=g, device="cuda").bfloat16()
+    codes, scales = torch.empty((most, 16), dtype=torch.int8, device="cuda"), torch.empty(most, device="cuda")
+    hb.hfx_rms_norm(hb.make_norm(torch.ones(16, dtype=torch.bfloat16, device="cuda"), 0.0), most, x, 16, None, 0, None, None, codes, scales, stream)
+    by_norm = codes.clone()
+    hb.hfx_quantise_rows(hb.HFX_ACT_NONE, most, 16, x, 16, None, 0, None, codes, scales, stream)
+    top = x.float().abs().amax(1, keepdim=True)
+    full = torch.full_like(top, 127.0)                          # (a division by a Python number is not one)
+    assert torch.equal(codes, torch.round(x.float() * (full / top)).to(torch.int8)) and torch.equal(codes, by_norm) and torch.equal(scales, (top / full)[:, 0])
+    for rows, n in ((most, 1), (most, 33), (1, most), (16, most), (33, most)):
+        out = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+        hb.hfx_matmul_rows(hb.make_weight_q8(codes[:n], scales[:n]), rows, codes, 16, scales, out, n, False, stream)
+        sums = codes[:rows].float() @ codes[:n].float().T           # (exact: no sum passes 2^24)
+        assert torch.equal(out, (sums * scales[:rows, None] * scales[None, :n]).bfloat16())
+        del out, sums
+
+
+@pytest.mark.gpu
+def test_empty_tensors():
+    import torch
+    def empty(cols, dtype):
+        return torch.empty((0, cols), dtype=dtype, device="cuda")
+    codes, scales, stream = empty(64, torch.int8), torch.empty(0, device="cuda"), torch.cuda.current_stream()
+    x = empty(64, torch.bfloat16)
+    hb.hfx_rms_norm(hb.make_norm(torch.ones(64, dtype=torch.bfloat16, device="cuda"), 0.0), 0, x, 64, x, 64, x, None, codes, scales, stream)
+    hb.hfx_quantise_rows(hb.HFX_ACT_SILU, 0, 64, x, 64, None, 0, None, codes, scales, stream)
+    weight = hb.make_weight_q8(torch.ones((5, 64), dtype=torch.int8, device="cuda"), torch.ones(5, device="cuda"))
+    hb.hfx_matmul_rows(weight, 0, codes, 64, scales, empty(5, torch.float32), 5, True, stream)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,cols", [(3, 2048), (2, 40000)])
 def test_norm_in_place_and_by_parts(rows, cols):
     """The sum over x or over the residual; results in bf16 alone and in 8 bits alone: the same bits."""
@@ -475,11 +524,13 @@ def test_what_the_norm_refuses():
         hb.hfx_rms_norm(Fake(hb.hfx_norm, *norm) if norm else None, *a.values())
     call(rows=0)                                                # nothing to do
     call(rows=0, residual=64, residual_stride=64, sum=32, codes=64, scales=4)
+    call(rows=0, x=None, out=None)
     for change in (dict(norm=None), dict(norm=(None, 64, 1e-6)), dict(x=None), dict(residual=16), dict(sum=16), dict(out=None), dict(codes=16), dict(scales=16), dict(out=None, codes=16)):
         refused(lambda: call(**change), hb.HFX_ERR_NULL)
     for change in (dict(rows=-1), dict(rows=(1 << 21) + 1), dict(norm=(16, 0, 1e-6)), dict(norm=(16, 72, 1e-6), x_stride=72), dict(norm=(16, 131072, 1e-6), x_stride=131072), dict(norm=(16, -16, 1e-6)),
                    dict(norm=(16, 64, -1.0)), dict(norm=(16, 64, float("nan"))), dict(norm=(16, 64, float("inf"))), dict(x_stride=56), dict(x_stride=-64),
-                   dict(x_stride=(1 << 22) + 8), dict(residual=16, sum=64, residual_stride=63)):
+                   dict(x_stride=(1 << 22) + 8), dict(residual=16, sum=64, residual_stride=63), dict(residual=16, residual_stride=64, sum=32, x_stride=72),
+                   dict(residual=16, residual_stride=72, sum=16)):
         refused(lambda: call(**change), hb.HFX_ERR_SHAPE)
     for change in (dict(x=24), dict(norm=(8, 64, 1e-6)), dict(out=40), dict(x_stride=68), dict(residual=18, sum=64, residual_stride=64), dict(residual=16, sum=72, residual_stride=64),
                    dict(residual=16, sum=64, residual_stride=70), dict(codes=8, scales=4), dict(codes=16, scales=2)):
@@ -493,10 +544,12 @@ def test_what_the_rows_to_8_bits_refuse():
         hb.hfx_quantise_rows(*{**ok, **change}.values())
     call(rows=0)
     call(rows=0, times=64, times_stride=128)
+    call(rows=0, x=None, codes=None, scales=None)
     for change in (dict(x=None), dict(codes=None), dict(scales=None), dict(codes=None, scales=None)):
         refused(lambda: call(**change), hb.HFX_ERR_NULL)
     for change in (dict(activation=2), dict(activation=-1), dict(rows=-3), dict(cols=8), dict(cols=24), dict(cols=131072, x_stride=131072), dict(x_stride=63), dict(times=16, times_stride=0),
-                   dict(times=16, times_stride=(1 << 22) + 16)):
+                   dict(times=16, times_stride=(1 << 22) + 16), dict(out=32), dict(times=16, times_stride=64, out=16), dict(out=32, codes=None, scales=None, x_stride=72),
+                   dict(times=16, times_stride=72, out=16, codes=None, scales=None)):
         refused(lambda: call(**change), hb.HFX_ERR_SHAPE)
     for change in (dict(x=40), dict(times=40, times_stride=64), dict(times=32, times_stride=68), dict(out=8), dict(codes=50), dict(scales=6), dict(x_stride=66)):
         refused(lambda: call(**change), hb.HFX_ERR_ALIGN)
@@ -511,6 +564,7 @@ def test_what_the_products_refuse():
         weight = a.pop("weight")
         hb.hfx_matmul_rows(None if weight is None else Fake(hb.hfx_weight_q8, *{**good, **weight}.values()), *a.values())
     call(rows=0)
+    call(rows=0, codes=None, scales=None, out=None)
     for change in (dict(weight=None), dict(weight=dict(codes=None)), dict(weight=dict(scales=None)), dict(codes=None), dict(scales=None), dict(out=None)):
         refused(lambda: call(**change), hb.HFX_ERR_NULL)
     for change in (dict(rows=-1), dict(rows=(1 << 21) + 1), dict(weight=dict(n=0)), dict(weight=dict(n=(1 << 21) + 1), out_stride=1 << 22), dict(weight=dict(k=0)), dict(weight=dict(k=56)),
