@@ -143,16 +143,19 @@ __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned of
 }
 #pragma clang diagnostic pop
 
-// A workgroup's BN channels by BM rows, one tile.  Stages of 128 values of the sum, a line of each row, go straight from memory to LDS, S of them in a ring; a row's eight 16-byte pieces
-// are permuted by bits 1 to 3 of its number, so that 16 lanes that read the same piece of 16 rows meet all banks.  (WN channels by WM rows, and of a
+// A workgroup's BN channels by BM rows, one tile.  Stages of U times 128 values of the sum, U lines of each row, go straight from memory to LDS, S of them in a ring; a row's eight
+// 16-byte pieces are permuted by bits 1 to 3 of its number, so that 16 lanes that read the same piece of 16 rows meet all banks.  (WN channels by WM rows, and of a
 // stage one part of K, belong to a wavefront.)  The operands of 32 values are read while the matrix instructions of the 32 before them run; the workgroup meets
 // once a stage, ahead of the last of these, when all of the stage has been read: its place is then free for the copies of the stage S behind it.
-template <int BN, int BM, int WN, int WM, int K, int S, bool Fp32>
+// Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 85 GB/s for each, 256 rows of 4096 to 6144 channels 17.2 us where weights come from memory and
+// 12.8 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels: two lines 10.1 us, one 11.2, in a ring of
+// the same bytes 13.1), and eight wavefronts of 32 by 32 serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels 15.3 and 15.6 us).
+template <int BN, int BM, int WN, int WM, int K, int S, int U, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
-  constexpr int kWaves = BN / WN * (BM / WM) * K, kBytes = (BN + BM) * 128;
-  constexpr int LN = BN / 8 / kWaves, LM = BM / 8 / kWaves, TN = WN / 32, TM = WM / 32, P = 4 / K;
+  constexpr int kWaves = BN / WN * (BM / WM) * K, kSub = (BN + BM) * 128, kBytes = U * kSub, kStage = U * 128;
+  constexpr int LN = BN / 8 / kWaves, LM = BM / 8 / kWaves, TN = WN / 32, TM = WM / 32, P = 4 * U / K, kEach = U * (LN + LM);
   static_assert(LN * 8 * kWaves == BN && LM * 8 * kWaves == BM, "each wavefront copies whole blocks of eight rows of both");
-  static_assert(P == 1 || P == 2 || P == 4, "");
+  static_assert(P % 2 == 0, "");
   constexpr int kScaleN = S * kBytes, kScaleM = kScaleN + (BN + 63) / 64 * 256, kAll = kScaleM + (BM + 63) / 64 * 256;
   static_assert(kAll <= 160 * 1024, "");
   __shared__ __attribute__((aligned(1024))) char smem[kAll];
@@ -164,7 +167,7 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   const int8_t* const weight = a.weight + (long)n0 * a.weight_stride;
   const int8_t* const codes = a.codes + (long)m0 * a.codes_stride;
   const unsigned lds0 = (unsigned)(uintptr_t)smem;
-  const int stages = (a.k + 127) >> 7, whole = a.k >> 7, rest = a.k & 127;
+  const int stages = (a.k + kStage - 1) / kStage, whole = a.k / kStage, rest = a.k % kStage;
 
   // A lane copies one piece of row lane / 8 of a block, the one that belongs in its place.  In a stage with fewer than 128 values the pieces behind them are piece 0 again.
   auto offset = [&](int i, int last, long stride, int values) {
@@ -176,22 +179,29 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   for (int i = 0; i < LN; ++i) off_n[i] = offset(i, a.n - 1 - n0, a.weight_stride, 128);
 #pragma unroll
   for (int i = 0; i < LM; ++i) off_m[i] = offset(i, a.rows - 1 - m0, a.codes_stride, 128);
-  // copy instruction i of LN + LM of a whole stage
+  // copy instruction i of a whole stage
   auto copy = [&](int stage, int slot, int i) {
-    const unsigned to = lds0 + slot * kBytes + wave * 1024;
-    if (i < LN) copy_to_lds(weight + (long)stage * 128, off_n[i < LN ? i : 0], to + i * kWaves * 1024);
-    else copy_to_lds(codes + (long)stage * 128, off_m[i < LN ? 0 : i - LN], to + BN * 128 + (i - LN) * kWaves * 1024);
+    const int u = i / (LN + LM), j = i % (LN + LM);
+    const unsigned to = lds0 + slot * kBytes + u * kSub + wave * 1024;
+    const long k = (long)stage * kStage + u * 128;
+    if (j < LN) copy_to_lds(weight + k, off_n[j < LN ? j : 0], to + j * kWaves * 1024);
+    else copy_to_lds(codes + k, off_m[j < LN ? 0 : j - LN], to + BN * 128 + (j - LN) * kWaves * 1024);
   };
   auto copy_any = [&](int stage, int slot) {
     if (stage < whole) {
 #pragma unroll
-      for (int i = 0; i < LN + LM; ++i) copy(stage, slot, i);
+      for (int i = 0; i < kEach; ++i) copy(stage, slot, i);
     } else {
-      const unsigned to = lds0 + slot * kBytes + wave * 1024;
 #pragma unroll
-      for (int i = 0; i < LN; ++i) copy_to_lds(weight + (long)stage * 128, offset(i, a.n - 1 - n0, a.weight_stride, rest), to + i * kWaves * 1024);
+      for (int u = 0; u < U; ++u) {
+        const unsigned to = lds0 + slot * kBytes + u * kSub + wave * 1024;
+        const int first = u * 128 < rest ? u * 128 : 0, values = min(rest - first, 128);
+        const long k = (long)stage * kStage + first;
 #pragma unroll
-      for (int i = 0; i < LM; ++i) copy_to_lds(codes + (long)stage * 128, offset(i, a.rows - 1 - m0, a.codes_stride, rest), to + BN * 128 + i * kWaves * 1024);
+        for (int i = 0; i < LN; ++i) copy_to_lds(weight + k, offset(i, a.n - 1 - n0, a.weight_stride, values), to + i * kWaves * 1024);
+#pragma unroll
+        for (int i = 0; i < LM; ++i) copy_to_lds(codes + k, offset(i, a.rows - 1 - m0, a.codes_stride, values), to + BN * 128 + i * kWaves * 1024);
+      }
     }
   };
 
@@ -202,7 +212,7 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   const int swizzle = (lane >> 1) & 7, half = lane >> 5;
   const int at_n = (wn * WN + (lane & 31)) * 128, at_m = BN * 128 + (wm * WM + (lane & 31)) * 128;
   auto read = [&](Operands& f, int slot, int kk) {
-    const char* const from = smem + slot * kBytes + (((2 * kk + half) ^ swizzle) * 16);
+    const char* const from = smem + slot * kBytes + (kk >> 2) * kSub + (((2 * (kk & 3) + half) ^ swizzle) * 16);
 #pragma unroll
     for (int t = 0; t < TN; ++t) f.n[t] = *reinterpret_cast<const i32x4*>(from + at_n + t * 4096);
 #pragma unroll
@@ -219,7 +229,7 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
 #pragma unroll
   for (int s = 0; s < S; ++s)
     if (s < stages) copy_any(s, s);
-  if (stages >= S) HFX_WAIT_VMCNT((S - 1) * (LN + LM));
+  if (stages >= S) HFX_WAIT_VMCNT((S - 1) * kEach);
   else HFX_WAIT_VMCNT(0);
   ring_barrier();
   Operands f[2];
@@ -230,12 +240,11 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
     const int behind = slot == S - 1 ? 0 : slot + 1;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      Operands& now = f[p & 1];
-      Operands& then = P == 1 ? f[1] : f[(p + 1) & 1];
+      Operands &now = f[p & 1], &then = f[(p + 1) & 1];
       if (p < P - 1) {
         read(then, slot, (p + 1) * K + kpart);
       } else if (more || s + 1 < stages) {
-        if (more || s + S <= stages) HFX_WAIT_VMCNT((S - 2) * (LN + LM));      // the stages behind the next one may still be on their way
+        if (more || s + S <= stages) HFX_WAIT_VMCNT((S - 2) * kEach);      // the stages behind the next one may still be on their way
         else HFX_WAIT_VMCNT(0);
         ring_barrier();
         read(then, behind, kpart);
@@ -250,13 +259,12 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
         if constexpr (decltype(more)::value) {
           if (p == P - 1) {
 #pragma unroll
-            for (int i = 0; i < LN + LM; ++i)
-              if (i * TN / (LN + LM) == t) copy(s + S, slot, i);
+            for (int i = 0; i < kEach; ++i)
+              if (i * TN / kEach == t) copy(s + S, slot, i);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (P == 1) f[0] = f[1];
     }
     ++s;
     slot = behind;
@@ -265,7 +273,7 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   while (s < whole) stage(std::false_type());
   if (rest != 0) {
 #pragma unroll 1
-    for (int kk = kpart; kk < 4; kk += K) {
+    for (int kk = kpart; kk < 4 * U; kk += K) {
       read(f[0], slot, kk);
       const int keep = (2 * kk + half) * 16 < rest ? -1 : 0;
 #pragma unroll
@@ -620,10 +628,10 @@ typedef hipError_t (*Launch)(const MatmulRows&, bool, hipStream_t);
 static hipError_t launch_few(const MatmulRows& a, bool fp32, hipStream_t stream) {
   return launch(fp32 ? matmul_few_kernel<true> : matmul_few_kernel<false>, dim3((unsigned)(a.n + 15) / 16), 1024, stream, a);
 }
-template <int BN, int BM, int WN, int WM, int K, int S>
+template <int BN, int BM, int WN, int WM, int K, int S, int U>
 static hipError_t launch_tiles(const MatmulRows& a, bool fp32, hipStream_t stream) {
   const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM;
-  return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, S, true> : matmul_tile_kernel<BN, BM, WN, WM, K, S, false>, dim3((unsigned)tiles_n * (unsigned)tiles_m),
+  return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, S, U, true> : matmul_tile_kernel<BN, BM, WN, WM, K, S, U, false>, dim3((unsigned)tiles_n * (unsigned)tiles_m),
                 BN / WN * (BM / WM) * K * 64, stream, a, tiles_n, tiles_m);
 }
 // Workgroups of a large kernel: one for each compute unit.  Where the sum has fewer stages than a ring each takes one tile, because the copies go on into the next tile and not past it.
@@ -636,33 +644,34 @@ static hipError_t launch_large(const MatmulRows& a, bool fp32, hipStream_t strea
 
 // What a product takes with each kernel, in us: `start`, and for each round of tiles over the chip `round` and each stage of 128 values of the sum
 // stage[t - 1], t being the tiles that meet on a compute unit (`most` at most).  Fitted to 2300 times of 190 products (1 to 8224 rows, 1280 to 16384 channels, sums of 512 to 16384 values, buffers that
-// change from call to call): the kernel that it names takes 1.01 times the fastest one's time on average, 1.17 at worst.  Why there are several, in us
+// change from call to call): the kernel that it names takes 1.005 times the fastest one's time on average, more than 1.15 times in one (777 rows of 8192 to 1280 channels, 260 tiles of 64 by 64, whose
+// last four cost less than a second layer of tiles: 29 and 22.5 us).  Why there are several, in us
 // (rows, k, channels; that kernel, then the next best one among the others):
-//   one row 4096 16384      few   14.9   32x32   17.2        37    8192  1280   32x32    9.1   32x64   11.2
-//   64  4096  6144       32x64   11.0   32x32   11.9        128   4096  6144   64x64   13.0   32x64   15.4
-//   256 1024  8192      128x64    6.3   64x64    6.6        777   1024  8192   128x128, two to a unit 13.3   256x128 14.1
-//   777 8192  4096     128x128   39.4  128x64   45.9        1500  8192  4096  128x192   53.4   256x128  57.8
-//   512 4096  16384    256x128   38.4  128x128  41.1        8224  4096  6144  256x160  198.9   256x256 205.5
-//   4128 4096 16384    256x192  251.4  256x256 263.4        8192  8192  8192  256x256  434     256x192 494
-// (channels x rows of a tile).  A product fills the chip with the largest tiles that leave little of a last round empty: the larger ones ask for fewer lines, of which a compute unit gets 45 to 75 GB/s.
+//   4    8192  4096        few    9.6   32x32   12.7        37    8192  1280   32x32    8.0   32x64    9.7
+//   64   4096  6144      32x64   10.9   32x32   11.6        128   4096  6144   64x64   13.1   32x64   16.0
+//   256  1024  8192     128x64    6.3   64x64    6.9        777   1024  8192   128x128, two to a unit 14.6   256x128 14.8
+//   777  8192  4096    128x128   39.4  128x64   47.7        1500  8192  4096  128x192   58.0   256x128  60.5
+//   1024 4096  6144    256x128   34.2  128x128, two to a unit 36.1
+//   8224 4096  6144    256x160  204.3  256x256 209.4        4128  4096 16384  256x192  251.4   256x256 263.4        8192  8192  8192  256x256  434     256x192 494
+// (channels x rows of a tile).  A product fills the chip with the largest tiles that leave little of a last round empty: the larger ones ask for fewer lines.
 struct Way {
   Launch launch;
   int bn, bm, threads, most;
-  float start, round, stage[3];
+  float start, round, stage[2];
 };
 static const Way kWays[] = {
-    {launch_few, 16, 16, 1024, 2, 2.0f, 0.48f, {0.10f, 0.20f}},
-    {launch_tiles<32, 32, 32, 32, 4, 6>, 32, 32, 256, 3, 2.0f, 1.0f, {0.13f, 0.21f, 0.29f}},
-    {launch_tiles<32, 64, 32, 32, 2, 6>, 32, 64, 256, 2, 1.5f, 1.6f, {0.175f, 0.275f}},
-    {launch_tiles<64, 64, 32, 32, 1, 4>, 64, 64, 256, 2, 1.4f, 1.4f, {0.255f, 0.405f}},
-    {launch_tiles<128, 64, 64, 32, 1, 3>, 128, 64, 256, 2, 0.5f, 2.6f, {0.41f, 0.655f}},
-    {launch_tiles<128, 128, 64, 32, 1, 2>, 128, 128, 512, 2, 0.0f, 3.6f, {0.735f, 1.065f}},
-    {launch_large<128, 128, 32, 64, 4, 4>, 128, 128, 512, 1, 5.8f, 1.5f, {0.52f}},
-    {launch_large<128, 192, 32, 96, 3, 3>, 128, 192, 512, 1, 3.2f, 3.0f, {0.695f}},
-    {launch_large<256, 128, 64, 64, 3, 3>, 256, 128, 512, 1, 4.7f, 3.0f, {0.83f}},
-    {launch_large<256, 160, 32, 160, 3, 3>, 256, 160, 512, 1, 2.2f, 4.7f, {1.0f}},
-    {launch_large<256, 192, 64, 96, 3, 2>, 256, 192, 512, 1, 6.7f, 2.5f, {1.225f}},
-    {launch_large<256, 256, 64, 128, 3, 2>, 256, 256, 512, 1, 7.7f, 3.4f, {1.46f}},
+    {launch_few, 16, 16, 1024, 2, 2.5f, 0.5f, {0.115f, 0.235f}},
+    {launch_tiles<32, 32, 32, 32, 4, 4, 2>, 32, 32, 256, 2, 2.1f, 0.9f, {0.11f, 0.215f}},
+    {launch_tiles<32, 64, 32, 32, 2, 4, 2>, 32, 64, 256, 1, 1.8f, 1.2f, {0.17f}},
+    {launch_tiles<64, 64, 32, 32, 1, 4, 1>, 64, 64, 256, 2, 1.2f, 1.8f, {0.257f, 0.42f}},
+    {launch_tiles<128, 64, 32, 32, 1, 3, 1>, 128, 64, 512, 2, 0.4f, 2.6f, {0.413f, 0.695f}},
+    {launch_tiles<128, 128, 64, 32, 1, 2, 1>, 128, 128, 512, 2, 0.2f, 3.9f, {0.725f, 1.055f}},
+    {launch_tiles<128, 128, 64, 32, 1, 4, 1>, 128, 128, 512, 1, 0.4f, 3.6f, {0.553f}},
+    {launch_large<128, 192, 32, 96, 3, 3>, 128, 192, 512, 1, 3.7f, 3.2f, {0.707f}},
+    {launch_large<256, 128, 64, 64, 3, 3>, 256, 128, 512, 1, 4.2f, 3.7f, {0.85f}},
+    {launch_large<256, 160, 32, 160, 3, 3>, 256, 160, 512, 1, 2.1f, 5.3f, {1.03f}},
+    {launch_large<256, 192, 64, 96, 3, 2>, 256, 192, 512, 1, 6.5f, 3.4f, {1.24f}},
+    {launch_large<256, 256, 64, 128, 3, 2>, 256, 256, 512, 1, 6.7f, 4.4f, {1.5f}},
 };
 
 hipError_t launch_matmul_rows(MatmulRows a, bool fp32, hipStream_t stream) {
