@@ -150,7 +150,10 @@ __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned of
 // Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 85 GB/s for each, 256 rows of 4096 to 6144 channels 17.2 us where weights come from memory and
 // 12.8 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels: two lines 10.1 us, one 11.2, in a ring of
 // the same bytes 13.1), and eight wavefronts of 32 by 32 serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels 15.3 and 15.6 us).
-template <int BN, int BM, int WN, int WM, int K, int S, int U, bool Fp32>
+// Turned: small tiles that fill the chip take the whole stages in a ring of their own, each eighth column of them (a die's next one) from three stages further on: rows that lie a power of two apart
+// have the same stage in the same few channels of the L2, where all the die's workgroups would ask for it at once (64 rows of 8192 to 4096 channels, 42 MB that the last level's cache holds, 13.8 -> 9.4
+// us, 13.4 -> 13.2 from memory; 64 of 4096 to 16384 from memory 18.9 -> 16.6).
+template <int BN, int BM, int WN, int WM, int K, int S, int U, bool Turned, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
   constexpr int kWaves = BN / WN * (BM / WM) * K, kSub = (BN + BM) * 128, kBytes = U * kSub, kStage = U * 128;
   constexpr int LN = BN / 8 / kWaves, LM = BM / 8 / kWaves, TN = WN / 32, TM = WM / 32, P = 4 * U / K, kEach = U * (LN + LM);
@@ -168,6 +171,7 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   const int8_t* const codes = a.codes + (long)m0 * a.codes_stride;
   const unsigned lds0 = (unsigned)(uintptr_t)smem;
   const int stages = (a.k + kStage - 1) / kStage, whole = a.k / kStage, rest = a.k % kStage;
+  const int turn = Turned && whole > 0 ? uniform((int)((unsigned)tile_n / 8u * 3u % (unsigned)whole)) : 0;
 
   // A lane copies one piece of row lane / 8 of a block, the one that belongs in its place.  In a stage with fewer than 128 values the pieces behind them are piece 0 again.
   auto offset = [&](int i, int last, long stride, int values) {
@@ -183,7 +187,8 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
   auto copy = [&](int stage, int slot, int i) {
     const int u = i / (LN + LM), j = i % (LN + LM);
     const unsigned to = lds0 + slot * kBytes + u * kSub + wave * 1024;
-    const long k = (long)stage * kStage + u * 128;
+    const int at = Turned ? stage + turn : stage;
+    const long k = (long)(Turned && at >= whole ? at - whole : at) * kStage + u * 128;
     if (j < LN) copy_to_lds(weight + k, off_n[j < LN ? j : 0], to + j * kWaves * 1024);
     else copy_to_lds(codes + k, off_m[j < LN ? 0 : j - LN], to + BN * 128 + (j - LN) * kWaves * 1024);
   };
@@ -628,11 +633,18 @@ typedef hipError_t (*Launch)(const MatmulRows&, bool, hipStream_t);
 static hipError_t launch_few(const MatmulRows& a, bool fp32, hipStream_t stream) {
   return launch(fp32 ? matmul_few_kernel<true> : matmul_few_kernel<false>, dim3((unsigned)(a.n + 15) / 16), 1024, stream, a);
 }
+template <int BN, int BM, int WN, int WM, int K, int S, int U, bool Turned>
+static hipError_t launch_tiles_as(const MatmulRows& a, bool fp32, hipStream_t stream) {
+  const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM;
+  return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, S, U, Turned, true> : matmul_tile_kernel<BN, BM, WN, WM, K, S, U, Turned, false>,
+                dim3((unsigned)tiles_n * (unsigned)tiles_m), BN / WN * (BM / WM) * K * 64, stream, a, tiles_n, tiles_m);
+}
 template <int BN, int BM, int WN, int WM, int K, int S, int U>
 static hipError_t launch_tiles(const MatmulRows& a, bool fp32, hipStream_t stream) {
-  const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM;
-  return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, S, U, true> : matmul_tile_kernel<BN, BM, WN, WM, K, S, U, false>, dim3((unsigned)tiles_n * (unsigned)tiles_m),
-                BN / WN * (BM / WM) * K * 64, stream, a, tiles_n, tiles_m);
+  // (taking the stages in turns costs the others more than it gives: 37 rows of 8192 to 1280 channels by 32x32 8.1 and 8.4 us, 128 rows of 4096 to 6144 by 64x64 9.4 and 10.2)
+  if constexpr (BN == BM && BN <= 64)
+    if ((long)((a.n + BN - 1) / BN) * ((a.rows + BM - 1) / BM) >= kComputeUnits) return launch_tiles_as<BN, BM, WN, WM, K, S, U, true>(a, fp32, stream);
+  return launch_tiles_as<BN, BM, WN, WM, K, S, U, false>(a, fp32, stream);
 }
 // Workgroups of a large kernel: one for each compute unit.  Where the sum has fewer stages than a ring each takes one tile, because the copies go on into the next tile and not past it.
 template <int BN, int BM, int WN, int WM, int RN, int RM>
@@ -644,8 +656,8 @@ static hipError_t launch_large(const MatmulRows& a, bool fp32, hipStream_t strea
 
 // What a product takes with each kernel, in us: `start`, and for each round of tiles over the chip `round` and each stage of 128 values of the sum
 // stage[t - 1], t being the tiles that meet on a compute unit (`most` at most).  Fitted to 2300 times of 190 products (1 to 8224 rows, 1280 to 16384 channels, sums of 512 to 16384 values, buffers that
-// change from call to call): the kernel that it names takes 1.005 times the fastest one's time on average, more than 1.15 times in one (777 rows of 8192 to 1280 channels, 260 tiles of 64 by 64, whose
-// last four cost less than a second layer of tiles: 29 and 22.5 us).  Why there are several, in us
+// change from call to call): the kernel that it names takes 1.006 times the fastest one's time on average, more than 1.1 times in one (777 rows of 8192 to 1280 channels, 260 tiles of 64 by 64, whose
+// last four cost less than a second layer of tiles: 29 and 21 us).  Why there are several, in us
 // (rows, k, channels; that kernel, then the next best one among the others):
 //   4    8192  4096        few    9.6   32x32   12.7        37    8192  1280   32x32    8.0   32x64    9.7
 //   64   4096  6144      32x64   10.9   32x32   11.6        128   4096  6144   64x64   13.1   32x64   16.0
