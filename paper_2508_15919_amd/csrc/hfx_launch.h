@@ -43,8 +43,9 @@ struct RmsNorm {
   long x_stride, residual_stride;
   int cols;
   float eps;
+  double part;               // 1 / cols; filled in by launch_rms_norm
 };
-hipError_t launch_rms_norm(const RmsNorm& a, int rows, hipStream_t stream);
+hipError_t launch_rms_norm(RmsNorm a, int rows, hipStream_t stream);
 
 // What the rows' way to 8 bits takes.  times, out and codes (with scales) may be null.
 struct QuantiseRows {

@@ -150,6 +150,16 @@ __device__ __forceinline__ void silu(float* v) {
   }
 }
 
+// a^(-1/2), by the hardware's estimate and two steps of Newton's method (a square root and divisions in 64 bits are chains of forty dependent operations).
+__device__ __forceinline__ double inverse_root(double a) {
+  double y = __builtin_amdgcn_rsq(a);
+  if (a > 0.0 && a < __builtin_inf()) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y = __builtin_fma(y * 0.5, __builtin_fma(-a * y, y, 1.0), y);
+  }
+  return y;
+}
+
 // One workgroup of T threads per row, eight values of it to a thread at a time; the first P of those stay in registers between the two passes, the ones behind
 // (rows of more than 8 T P values) are read again.  The row of x and the residual is rounded to bf16 before anything else is formed from it: the norm is that of
 // the stream as it is kept.  Squares of bf16 numbers are exact in fp32 but may pass its range, and are summed in 64 bits.  A value's code is the
@@ -161,9 +171,11 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
   const uint16_t* const residual = a.residual ? a.residual + row * a.residual_stride : nullptr;
   uint16_t* const kept = a.residual ? a.sum + row * a.cols : nullptr;
   float h[P][8];
+  u32x4 weight[P];
   unsigned top = 0;
   double sum = 0.0;
-  auto first = [&](int c, float* v) {
+  auto first = [&](int c, float* v, u32x4& wide) {
+    wide = *reinterpret_cast<const u32x4*>(a.weight + c);
     widen8(load_piece<Past>(x + c), v);
     if (residual) {
       float z[8];
@@ -175,7 +187,7 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
       widen8(r, v);
     }
     float w[8];
-    widen8(*reinterpret_cast<const u32x4*>(a.weight + c), w);
+    widen8(wide, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       sum += (double)v[e] * (double)v[e];
@@ -185,20 +197,21 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int c = (p * T + (int)threadIdx.x) * 8;
-    if (c < a.cols) first(c, h[p]);
+    if (c < a.cols) first(c, h[p], weight[p]);
   }
   for (int c = (P * T + (int)threadIdx.x) * 8; c < a.cols; c += T * 8) {
     float v[8];
-    first(c, v);
+    u32x4 w;
+    first(c, v, w);
   }
   reduce_row<T, true>(top, sum);
-  const double r = 1.0 / __builtin_sqrt(sum / (double)a.cols + (double)a.eps);
+  const double r = inverse_root(__builtin_fma(sum, a.part, (double)a.eps));
   const float up = r > 0x1p100 ? 0x1p64f : 1.0f, rf = (float)(r / (double)up);      // (rows of the smallest numbers, without eps, have an r past the range of fp32)
   const Scaling s = scaling_of(top);
-  if (a.codes && threadIdx.x == 0) a.scales[row] = (float)((double)s.top * r / 127.0);
-  auto second = [&](int c, const float* v) {
+  if (a.codes && threadIdx.x == 0) a.scales[row] = (float)((double)s.top * r * (1.0 / 127.0));
+  auto second = [&](int c, const float* v, const u32x4& wide) {
     float w[8], y[8];
-    widen8(*reinterpret_cast<const u32x4*>(a.weight + c), w);
+    widen8(wide, w);
     if (a.codes) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = v[e] * w[e];
@@ -213,12 +226,12 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int c = (p * T + (int)threadIdx.x) * 8;
-    if (c < a.cols) second(c, h[p]);
+    if (c < a.cols) second(c, h[p], weight[p]);
   }
   for (int c = (P * T + (int)threadIdx.x) * 8; c < a.cols; c += T * 8) {
     float v[8];
     widen8(*reinterpret_cast<const u32x4*>((kept ? kept : x) + c), v);
-    second(c, v);
+    second(c, v, *reinterpret_cast<const u32x4*>(a.weight + c));
   }
 }
 
@@ -296,7 +309,8 @@ static hipError_t launch_rows(const A& a, int rows, long bytes, hipStream_t stre
   return run(std::integral_constant<int, 1024>(), four);
 }
 
-hipError_t launch_rms_norm(const RmsNorm& a, int rows, hipStream_t stream) {
+hipError_t launch_rms_norm(RmsNorm a, int rows, hipStream_t stream) {
+  a.part = 1.0 / a.cols;
   return launch_rows(a, rows, (long)rows * a.cols * ((a.residual ? 6 : 2) + (a.out ? 2 : 0) + (a.codes ? 1 : 0)), stream, [](auto t, auto p, auto past) {
     return rms_norm_kernel<decltype(t)::value, decltype(p)::value, decltype(past)::value>;
   });
