@@ -150,9 +150,8 @@ __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned of
 // Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 85 GB/s for each, 256 rows of 4096 to 6144 channels 17.2 us where weights come from memory and
 // 12.8 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels: two lines 10.1 us, one 11.2, in a ring of
 // the same bytes 13.1), and eight wavefronts of 32 by 32 serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels 15.3 and 15.6 us).
-// Turned: small tiles that fill the chip take the whole stages in a ring of their own, each eighth column of them (a die's next one) from three stages further on: rows that lie a power of two apart
-// have the same stage in the same few channels of the L2, where all the die's workgroups would ask for it at once (64 rows of 8192 to 4096 channels, 42 MB that the last level's cache holds, 13.8 -> 9.4
-// us, 13.4 -> 13.2 from memory; 64 of 4096 to 16384 from memory 18.9 -> 16.6).
+// Turned: the whole stages are taken in a ring of their own, for each eighth column of tiles (a die's next one) from three stages further on: rows that lie a multiple of 4096 bytes apart
+// have the same stage in the same few channels of the L2, where all the die's workgroups would ask for it at once.
 template <int BN, int BM, int WN, int WM, int K, int S, int U, bool Turned, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
   constexpr int kWaves = BN / WN * (BM / WM) * K, kSub = (BN + BM) * 128, kBytes = U * kSub, kStage = U * 128;
@@ -641,9 +640,10 @@ static hipError_t launch_tiles_as(const MatmulRows& a, bool fp32, hipStream_t st
 }
 template <int BN, int BM, int WN, int WM, int K, int S, int U>
 static hipError_t launch_tiles(const MatmulRows& a, bool fp32, hipStream_t stream) {
-  // (taking the stages in turns costs the others more than it gives: 37 rows of 8192 to 1280 channels by 32x32 8.1 and 8.4 us, 128 rows of 4096 to 6144 by 64x64 9.4 and 10.2)
+  // Stages in turns, plain and so: 64 rows of 8192 to 4096 channels by 32x32 13.7 and 9.4 us, 96 of 16384 35.3 and 30.8, 32 of 4096 to 16384 by 64x64, from memory, 18.2 and 15.2.  Elsewhere they cost
+  // more than they give: 256 rows of 8192 to 4096 by 64x64 16.2 and 18.4, 64 of 5120 to 5120 by 32x32 8.8 and 9.4, 37 of 8192 to 1280 (80 tiles) 8.1 and 8.4.
   if constexpr (BN == BM && BN <= 64)
-    if ((long)((a.n + BN - 1) / BN) * ((a.rows + BM - 1) / BM) >= kComputeUnits) return launch_tiles_as<BN, BM, WN, WM, K, S, U, true>(a, fp32, stream);
+    if (a.rows <= 128 && a.weight_stride % 4096 == 0 && (long)((a.n + BN - 1) / BN) * ((a.rows + BM - 1) / BM) >= kComputeUnits) return launch_tiles_as<BN, BM, WN, WM, K, S, U, true>(a, fp32, stream);
   return launch_tiles_as<BN, BM, WN, WM, K, S, U, false>(a, fp32, stream);
 }
 // Workgroups of a large kernel: one for each compute unit.  Where the sum has fewer stages than a ring each takes one tile, because the copies go on into the next tile and not past it.

@@ -359,7 +359,8 @@ def test_products_over_any_length(k):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,n,k,extra", [(5, 300, 528, (16, 32, 1)), (33, 64, 256, (48, 0, 8)), (130, 257, 1040, (16, 16, 7)), (700, 768, 640, (0, 64, 128)), (64, 4096, 64, (4080, 16, 3))])
+@pytest.mark.parametrize("rows,n,k,extra", [(5, 300, 528, (16, 32, 1)), (33, 64, 256, (48, 0, 8)), (130, 257, 1040, (16, 16, 7)), (700, 768, 640, (0, 64, 128)), (64, 4096, 64, (4080, 16, 3)),
+                                            (64, 4090, 8080, (0, 112, 0)), (100, 8200, 4000, (16, 96, 1)), (24, 8200, 4096, (0, 0, 0)), (7, 16400, 272, (0, 3824, 0)), (40, 8200, 144, (0, 3952, 8))])
 def test_products_of_rows_that_lie_apart(rows, n, k, extra):
     import torch
     for fp32 in (False, True):
