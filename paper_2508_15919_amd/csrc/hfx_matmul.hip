@@ -58,11 +58,12 @@ __device__ __forceinline__ void store_line(const MatmulRows& a, int m, int n, co
 }
 
 // ---------------------------------------------------------------- few rows
-// 16 channels by up to 16 rows to a workgroup, the sum cut into steps of 128 values that its 16 wavefronts take in turn; both operands go straight to registers, two steps ahead.  A
+// 16 channels by up to 8 rows to a workgroup, the sum cut into steps of 128 values that its 16 wavefronts take in turn; both operands go straight to registers, two steps ahead.  A
 // lane has 32 bytes in a row of a step, which two matrix instructions take one half each (any order of the values will do that is the same in both operands), so that
-// four lanes ask for a whole line.  Rows that are not there are the last one again, which costs no further lines.
+// four lanes ask for a whole line.  Rows that are not there are the last one again, which costs no further lines
+// (16 rows of 4096 to 16384 channels 20.6 us where 4 take 16.0: 9 and more go by tiles of 32 rows, 16.3).
 // Bound by the weight's way from memory: one row of 4096 to 16384 channels (67 MB) 14.9 us, 5.3 TB/s behind the 2.1 us of a launch.  Four rows to 6144
-// channels 8.8 us; eight wavefronts four steps ahead 9.3.
+// channels 8.8 us, with eight wavefronts four steps ahead 9.3.
 template <bool Fp32>
 __global__ __launch_bounds__(1024) void matmul_few_kernel(const MatmulRows a) {
   constexpr int kWaves = 16, kAhead = 2;
@@ -363,6 +364,9 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
 // 16 rows meet all banks.  The operands of 32 values are read while the matrix instructions of the 32 before them run.  The workgroup meets once a
 // stage, ahead of the last of these, when all of the stage has been read: its places are then free for the copies of the stages RM and RN behind it.  These go on into the next tile, so
 // that its first stages arrive while the results of this one leave.
+// Bound by the clock that power leaves the matrix cores: 8224 rows of 4096 to 6144 channels 195 to 204 us, 2.0 to 2.1 POP/s (a library's product 227), the matrix cores busy in 51 % of the cycles of a clock of 1.9 to 2.0
+// GHz; 8192 of 8192 to 8192 434 us, 2.54 POP/s.  Nothing but these instructions, on operands in registers, runs at 3.4 POP/s with random operands and at 4.5 with zeros.  (Tiles whose copies end with them, in one ring for both
+// operands: 219 us.)
 template <int BN, int BM, int WN, int WM, int RN, int RM, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * 64) void matmul_large_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
   constexpr int kWaves = BN / WN * (BM / WM), TN = WN / 32, TM = WM / 32;
@@ -672,7 +676,7 @@ struct Way {
   float start, round, stage[2];
 };
 static const Way kWays[] = {
-    {launch_few, 16, 16, 1024, 2, 2.5f, 0.5f, {0.115f, 0.235f}},
+    {launch_few, 16, 8, 1024, 2, 2.1f, 0.43f, {0.098f, 0.2f}},
     {launch_tiles<32, 32, 32, 32, 4, 4, 2>, 32, 32, 256, 2, 2.1f, 0.9f, {0.11f, 0.215f}},
     {launch_tiles<32, 64, 32, 32, 2, 4, 2>, 32, 64, 256, 1, 1.8f, 1.2f, {0.17f}},
     {launch_tiles<64, 64, 32, 32, 1, 4, 1>, 64, 64, 256, 2, 1.2f, 1.8f, {0.257f, 0.42f}},
@@ -694,14 +698,12 @@ hipError_t launch_matmul_rows(MatmulRows a, bool fp32, hipStream_t stream) {
   const Way* best = nullptr;
   float least = 0.0f;
   for (const Way& w : kWays) {
-    if (w.launch == launch_few && a.rows > 16) continue;
+    if (w.launch == launch_few && a.rows > w.bm) continue;
     const long tiles = (long)((a.n + w.bn - 1) / w.bn) * ((a.rows + w.bm - 1) / w.bm), chip = (long)kComputeUnits * w.most;
     if (tiles * w.threads >= 1l << 32) continue;
     const long rounds = tiles / chip, left = tiles - rounds * chip;
     float us = w.start + (float)rounds * (w.round + (float)stages * w.stage[w.most - 1]);
     if (left) us += w.round + (float)stages * w.stage[(left - 1) / kComputeUnits];
-    // up to eight rows ask for fewer lines (4 rows of 4096 to 16384 channels 16.0 us, 16 rows 20.6)
-    if (w.launch == launch_few && a.rows <= 8) us *= 0.85f;
     if (!best || us < least) {
       best = &w;
       least = us;

@@ -164,6 +164,8 @@ __device__ __forceinline__ double inverse_root(double a) {
 // (rows of more than 8 T P values) are read again.  The row of x and the residual is rounded to bf16 before anything else is formed from it: the norm is that of
 // the stream as it is kept.  Squares of bf16 numbers are exact in fp32 but may pass its range, and are summed in 64 bits.  A value's code is the
 // nearest to h w 127 / top: the norm's own factor r is in the scale alone, top r / 127, so that codes do not depend on the order of the sum.
+// Bound by memory on many rows (8224 of 4096 with the sum and a bf16 result, 270 MB, 43.6 us, 6.2 TB/s; a plain copy has 4.9), by the chain of launch, loads, reduction and stores on few: 4 rows 2.7 us a call in a
+// captured graph.
 template <int T, int P, bool Past>
 __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
   const long row = blockIdx.x;
@@ -235,7 +237,8 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
   }
 }
 
-// Rows through an activation, times other rows, to bf16 and to 8 bits.  Laid out as the norm.
+// Rows through an activation, times other rows, to bf16 and to 8 bits.  Laid out as the norm, and bound as it is: 2500 gated rows of 8192 (102 MB) 20.0 us, 5.1
+// TB/s; 64 of them 4.5.
 template <int T, int P, bool Past>
 __global__ __launch_bounds__(T) void quantise_rows_kernel(const QuantiseRows a) {
   const long row = blockIdx.x;
