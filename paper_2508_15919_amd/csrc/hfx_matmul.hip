@@ -364,9 +364,9 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
 // 16 rows meet all banks.  The operands of 32 values are read while the matrix instructions of the 32 before them run.  The workgroup meets once a
 // stage, ahead of the last of these, when all of the stage has been read: its places are then free for the copies of the stages RM and RN behind it.  These go on into the next tile, so
 // that its first stages arrive while the results of this one leave.
-// Bound by the clock that power leaves the matrix cores: 8224 rows of 4096 to 6144 channels 195 to 204 us, 2.0 to 2.1 POP/s (a library's product 227), the matrix cores busy in 51 % of the cycles of a clock of 1.9 to 2.0
-// GHz; 8192 of 8192 to 8192 434 us, 2.54 POP/s.  Nothing but these instructions, on operands in registers, runs at 3.4 POP/s with random operands and at 4.5 with zeros.  (Tiles whose copies end with them, in one ring for both
-// operands: 219 us.)
+// Bound by the clock that power leaves the matrix cores, with the LDS close behind: 8192 rows of 4096 to 6144 channels 172 to 176 us, 2.35 to 2.4 POP/s (a library's product of 8224 rows 227), the matrix cores busy in 61 %
+// of the cycles of a clock of 1.85 GHz; 8192 of 8192 to 8192 434 to 450 us.  Nothing but these instructions, on operands in registers, runs at 3.4 POP/s with random operands and at 4.5 with zeros.  Four wavefronts of 128 by
+// 128, which read a third less from the LDS, take 183 and 464 us.  (Tiles whose copies end with them, in one ring for both operands: 8224 rows 219 us; with both, and no second launch, 195 to 205.)
 template <int BN, int BM, int WN, int WM, int RN, int RM, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * 64) void matmul_large_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
   constexpr int kWaves = BN / WN * (BM / WM), TN = WN / 32, TM = WM / 32;
