@@ -668,7 +668,7 @@ static hipError_t launch_large(const MatmulRows& a, bool fp32, hipStream_t strea
 //   256  1024  8192     128x64    6.3   64x64    6.9        777   1024  8192   128x128, two to a unit 14.6   256x128 14.8
 //   777  8192  4096    128x128   39.4  128x64   47.7        1500  8192  4096  128x192   58.0   256x128  60.5
 //   1024 4096  6144    256x128   34.2  128x128, two to a unit 36.1
-//   8224 4096  6144    256x160  204.3  256x256 209.4        4128  4096 16384  256x192  251.4   256x256 263.4        8192  8192  8192  256x256  434     256x192 494
+//   2500 8192  4096    256x160   83.3  256x192   88.2       4128 1024  8192  256x192   44.3  128x128   48.5       2048 4096  16384 256x256  127.5  256x128  145.8
 // (channels x rows of a tile).  A product fills the chip with the largest tiles that leave little of a last round empty: the larger ones ask for fewer lines.
 struct Way {
   Launch launch;

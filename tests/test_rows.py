@@ -503,6 +503,46 @@ def test_a_layers_calls_on_a_stream_and_in_a_graph():
         assert bool(torch.isfinite(eager["out"]).all()) and float(eager["out"].float().std()) > 0.01
 
 
+@pytest.mark.gpu
+def test_calls_on_two_streams_at_once_and_a_product_of_two_launches_in_a_graph():
+    """Nothing that calls share: each stream's results are those of its calls alone, also while a graph of a product that takes two launches is replayed."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(17)
+
+    def random_codes(rows, k):
+        return torch.randint(-127, 128, (rows, k), dtype=torch.int8, device="cuda", generator=gen), torch.rand(rows, device="cuda", generator=gen) + 0.1
+    rows, n, k = 4128, 16384, 1024
+    large, (large_codes, large_scales) = hb.make_weight_q8(*random_codes(n, k)), random_codes(rows, k)
+    small, norm = hb.make_weight_q8(*random_codes(900, 2048)), hb.make_norm(torch.rand(2048, generator=gen, device="cuda").bfloat16(), 1e-6)
+    x = torch.randn((50, 2048), generator=gen, device="cuda").bfloat16()
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = [torch.empty((rows, n), dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+
+    def chain(stream):
+        with torch.cuda.stream(stream):
+            codes, scales, out = torch.empty((50, 2048), dtype=torch.int8, device="cuda"), torch.empty(50, device="cuda"), torch.empty((50, 900), device="cuda")
+        hb.hfx_rms_norm(norm, 50, x, 2048, None, 0, None, None, codes, scales, stream)
+        hb.hfx_matmul_rows(small, 50, codes, 2048, scales, out, 900, True, stream)
+        return out
+    want = chain(torch.cuda.current_stream())
+    hb.hfx_matmul_rows(large, rows, large_codes, k, large_scales, outs[0], n, False, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=first):
+        hb.hfx_matmul_rows(large, rows, large_codes, k, large_scales, outs[1], n, False, torch.cuda.current_stream())
+    for turn in range(3):
+        outs[1].zero_()
+        outs[2].zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(first):
+            graph.replay()
+        got = [chain(second) for _ in range(8)]
+        hb.hfx_matmul_rows(large, rows, large_codes, k, large_scales, outs[2], n, False, second)
+        got += [chain(first), chain(second)]
+        torch.cuda.synchronize()
+        assert torch.equal(outs[1], outs[0]) and torch.equal(outs[2], outs[0]) and all(torch.equal(o, want) for o in got)
+
+
 # ------------------------------------------------------------------ refusals, on the host
 class Fake:
     """A norm or weight without memory: its numbers are addresses."""
