@@ -150,7 +150,8 @@ __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned of
 // once a stage, ahead of the last of these, when all of the stage has been read: its place is then free for the copies of the stage S behind it.
 // Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 85 GB/s for each, 256 rows of 4096 to 6144 channels 17.2 us where weights come from memory and
 // 12.8 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels: two lines 10.1 us, one 11.2, in a ring of
-// the same bytes 13.1), and eight wavefronts of 32 by 32 serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels 15.3 and 15.6 us).
+// the same bytes 13.1; alone on its unit 128 by 64 too, 256 rows of 4096 to 6144 17.0 and 17.8,
+// 200 15.5 and 17.0), and eight wavefronts of 32 by 32 serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels 15.3 and 15.6 us).
 // Turned: the whole stages are taken in a ring of their own, for each eighth column of tiles (a die's next one) from three stages further on: rows that lie a multiple of 4096 bytes apart
 // have the same stage in the same few channels of the L2, where all the die's workgroups would ask for it at once.
 template <int BN, int BM, int WN, int WM, int K, int S, int U, bool Turned, bool Fp32>
@@ -680,6 +681,7 @@ static const Way kWays[] = {
     {launch_tiles<32, 32, 32, 32, 4, 4, 2>, 32, 32, 256, 2, 2.1f, 0.9f, {0.11f, 0.215f}},
     {launch_tiles<32, 64, 32, 32, 2, 4, 2>, 32, 64, 256, 1, 1.8f, 1.2f, {0.17f}},
     {launch_tiles<64, 64, 32, 32, 1, 4, 1>, 64, 64, 256, 2, 1.2f, 1.8f, {0.257f, 0.42f}},
+    {launch_tiles<128, 64, 32, 32, 1, 3, 2>, 128, 64, 512, 1, 0.4f, 2.6f, {0.392f}},
     {launch_tiles<128, 64, 32, 32, 1, 3, 1>, 128, 64, 512, 2, 0.4f, 2.6f, {0.413f, 0.695f}},
     {launch_tiles<128, 128, 64, 32, 1, 2, 1>, 128, 128, 512, 2, 0.2f, 3.9f, {0.725f, 1.055f}},
     {launch_tiles<128, 128, 64, 32, 1, 4, 1>, 128, 128, 512, 1, 0.4f, 3.6f, {0.553f}},

@@ -382,7 +382,8 @@ FILLING = [(771, 8208, 4099), (1491, 4112, 4100), (4100, 400, 4100), (4100, 384,
            (1324, 272, 9280), (2471, 416, 4910), (929, 3856, 6111), (4654, 400, 10263), (665, 4384, 9861), (639, 3984, 6414), (1043, 3984, 2648), (4255, 3984, 877), (3345, 1504, 4599),
            (4543, 16, 6456), (3153, 16, 7319), (1039, 16, 2186), (4410, 272, 208), (567, 144, 394),
            (64, 4112, 6144), (37, 4240, 6001), (128, 496, 4000), (33, 16, 6144), (60, 144, 6144), (100, 272, 4000), (64, 8336, 4090), (24, 8208, 4097), (128, 4128, 6144),
-           (4128, 1024, 16384), (6200, 1040, 9001), (8224, 1040, 8203), (4500, 1040, 8200), (4128, 2064, 16387), (4100, 1024, 16384), (4104, 4112, 4100)]
+           (4128, 1024, 16384), (6200, 1040, 9001), (8224, 1040, 8203), (4500, 1040, 8200), (4128, 2064, 16387), (4100, 1024, 16384), (4104, 4112, 4100),
+           (250, 4112, 6100), (200, 4240, 6144), (500, 8208, 4090), (400, 144, 4000), (1000, 400, 3900), (900, 656, 2500), (130, 528, 16001)]
 
 
 @pytest.mark.gpu
