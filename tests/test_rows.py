@@ -91,7 +91,7 @@ def check_norm(got, want):
 @pytest.mark.gpu
 @pytest.mark.parametrize("with_residual", [True, False])
 @pytest.mark.parametrize("rows,cols,extra", [(1, 16, 0), (3, 48, 8), (70, 512, 0), (5, 1024, 24), (4, 1040, 0), (33, 2048, 8), (2, 4096, 0), (3, 8192, 0), (2, 8208, 8),
-                                             (1, 32768, 0), (2, 40016, 16), (1, 131056, 0)])
+                                             (1, 32768, 0), (2, 40016, 16), (1, 131056, 0), (1300, 4112, 8), (300, 16400, 0)])
 def test_norm(rows, cols, extra, with_residual):
     import torch
     g = np.random.default_rng(rows * 131 + cols)
@@ -226,7 +226,7 @@ def run_rows(torch, activation, x, times, extra=0, want_out=True, behind=2):
     return [None if t is None else t[:rows].cpu().double().numpy() for t in (out, codes, scales)]
 
 
-SIZES = [(1, 16, 0), (3, 80, 8), (40, 1024, 0), (5, 1376, 8), (2, 8192, 0), (3, 14336, 0), (2, 33008, 8), (1, 131056, 0)]
+SIZES = [(1, 16, 0), (3, 80, 8), (40, 1024, 0), (5, 1376, 8), (2, 8192, 0), (3, 14336, 0), (2, 33008, 8), (1, 131056, 0), (300, 6160, 8), (2100, 4112, 0)]
 
 
 @pytest.mark.gpu
