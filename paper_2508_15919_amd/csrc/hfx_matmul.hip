@@ -148,8 +148,8 @@ __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned of
 // 16-byte pieces are permuted by bits 1 to 3 of its number, so that 16 lanes that read the same piece of 16 rows meet all banks.  (WN channels by WM rows, and of a
 // stage one part of K, belong to a wavefront.)  The operands of 32 values are read while the matrix instructions of the 32 before them run; the workgroup meets
 // once a stage, ahead of the last of these, when all of the stage has been read: its place is then free for the copies of the stage S behind it.
-// Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 85 GB/s for each, 256 rows of 4096 to 6144 channels 17.2 us where weights come from memory and
-// 12.8 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels: two lines 10.1 us, one 11.2, in a ring of
+// Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 85 GB/s for each, 256 rows of 4096 to 6144 channels 17.0 us where weights come from memory and
+// 12.4 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels: two lines 10.1 us, one 11.2, in a ring of
 // the same bytes 13.1; alone on its unit 128 by 64 too, 256 rows of 4096 to 6144 17.0 and 17.8,
 // 200 15.5 and 17.0), and eight wavefronts of 32 by 32 serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels 15.3 and 15.6 us).
 // Turned: the whole stages are taken in a ring of their own, for each eighth column of tiles (a die's next one) from three stages further on: rows that lie a multiple of 4096 bytes apart
