@@ -124,30 +124,32 @@ __device__ __forceinline__ uint2 to_codes(const float* v, float factor) {
   return make_uint2(w[0], w[1]);
 }
 
-// v / (1 + e^-v), as v t / (1 + t) below zero and v / (1 + t) above, t = e^-|v|.  For |v| <= 80, where t is a normal number: t = 2^p (1 + q ln 2) with p the product of -|v| and log2 e rounded
-// and q what it lost, the quotient by a reciprocal and one correction (an IEEE division and expf take three times the instructions, and rows of 8192 gated values were bound by them: 2500 of
-// them 27 us).
+// v / (1 + e^-v), as v t / (1 + t) below zero and v / (1 + t) above, t = e^-|v|: t = 2^p (1 + q ln 2) with p the product of -|v| and log2 e rounded and q what it lost, the quotient by a
+// reciprocal and one correction (an IEEE division and expf take three times the instructions, and rows of 8192 gated values were bound by them: 2500 of them 27 us).  Past 80, where 1 + t is
+// 1 and t leaves the range of normal numbers, 2^(p + 64) takes the place of 2^p, of a p that ends at -200 log2 e, and the product with v the rest.  Which form a value takes goes by itself alone;
+// Far: there are such values among the wavefront's.
+template <bool Far>
+__device__ __forceinline__ float silu_of(float v) {
+#pragma clang fp contract(off)
+  constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
+  const bool far = Far && !(fabsf(v) <= 80.0f);
+  const float a = Far ? fmaxf(-fabsf(v), -200.0f) : -fabsf(v), p = a * kLog2e, q = __builtin_fmaf(a, kLog2eRest, __builtin_fmaf(a, kLog2e, -p));
+  float t = __builtin_amdgcn_exp2f(far ? p + 64.0f : p);
+  t = __builtin_fmaf(t, q * kLn2, t);
+  const float n = v < 0.0f ? (far ? v * t * 0x1p-64f : v * t) : v, d = 1.0f + t, r = __builtin_amdgcn_rcpf(d), y = n * r;
+  return far ? n : __builtin_fmaf(__builtin_fmaf(-d, y, n), r, y);
+}
 __device__ __forceinline__ void silu(float* v) {
   float most = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
   if (__builtin_expect(__any(!(most <= 80.0f)), 0)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float t = expf(-fabsf(v[e]));
-      v[e] = (v[e] < 0.0f ? v[e] * t : v[e]) / (1.0f + t);
-    }
+    for (int e = 0; e < 8; ++e) v[e] = silu_of<true>(v[e]);
     return;
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
-    const float a = -fabsf(v[e]), p = a * kLog2e, q = __builtin_fmaf(a, kLog2eRest, __builtin_fmaf(a, kLog2e, -p));
-    float t = __builtin_amdgcn_exp2f(p);
-    t = __builtin_fmaf(t, q * kLn2, t);
-    const float n = v[e] < 0.0f ? v[e] * t : v[e], d = 1.0f + t, r = __builtin_amdgcn_rcpf(d), y = n * r;
-    v[e] = __builtin_fmaf(__builtin_fmaf(-d, y, n), r, y);
-  }
+  for (int e = 0; e < 8; ++e) v[e] = silu_of<false>(v[e]);
 }
 
 // a^(-1/2), by the hardware's estimate and two steps of Newton's method (a square root and divisions in 64 bits are chains of forty dependent operations).

@@ -297,6 +297,68 @@ def test_rows_in_place():
     assert torch.equal(a, want) and torch.equal(b, want)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("beside", [90.0, -1000.0, float("inf"), float("nan")])
+def test_silu_of_a_value_does_not_depend_on_those_beside_it(beside):
+    """One value in 512 far out, or not finite: the results of the others keep their bits."""
+    import torch
+    rows, cols, stream = 2048, 4096, torch.cuda.current_stream()
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.empty((rows, cols), device="cuda").normal_(0.0, 16.0, generator=gen).clamp_(-80.0, 80.0).bfloat16()
+    times = torch.empty((rows, cols), device="cuda").normal_(generator=gen).bfloat16()
+    outs = []
+    for value in (0.0, beside):
+        x[:, 77::512] = value
+        outs.append(torch.empty_like(x))
+        hb.hfx_quantise_rows(hb.HFX_ACT_SILU, rows, cols, x, cols, times, cols, outs[-1], None, None, stream)
+        outs[-1][:, 77::512] = 0.0
+    assert int((outs[0].view(torch.int16) != outs[1].view(torch.int16)).sum()) == 0
+
+
+@pytest.mark.gpu
+def test_silu_of_every_number():
+    """One number to a row, so that its result is seen through the scale, times 2^60 where it is small.  The value 2^-21, as above; the scale's division 2^-24."""
+    import torch
+    x = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    x = x[torch.isfinite(x)]
+    for part, up in ((x.abs() <= 1.0, 2.0 ** 60), ((x.abs() > 1.0) & (x.abs() <= 80.0), 2.0 ** 60), ((x.abs() > 80.0) & (x.abs() <= 110.0), 2.0 ** 60), (x.abs() > 110.0, 1.0)):
+        n = int(part.sum())
+        rows = torch.zeros((n, 16), dtype=torch.bfloat16, device="cuda")
+        rows[:, 3] = x[part].cuda()
+        out, codes, scales = torch.empty_like(rows), torch.empty((n, 16), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+        hb.hfx_quantise_rows(hb.HFX_ACT_SILU, n, 16, rows, 16, torch.full_like(rows, up), 16, out, codes, scales, torch.cuda.current_stream())
+        v = x[part].double().numpy()
+        with np.errstate(over="ignore"):
+            v = v / (1.0 + np.exp(-v))
+        top = np.maximum(np.abs(v) * up, 2.0 ** -100)
+        # (results below 2^-126 are whole numbers of 2^-149, before the product with `up`: half of one)
+        assert (np.abs(scales.cpu().double().numpy() * 127.0 - top) <= (2.0 ** -21 + 2.0 ** -24) * top + 2.0 ** -150 * up).all()
+        far = v * up
+        assert (np.abs(out[:, 3].cpu().double().numpy() - far) <= (HALF_BF16 + 2.0 ** -20) * np.abs(far) + 2.0 ** -150 * up + 2.0 ** -133).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [4112, 8192])
+def test_a_row_does_not_depend_on_the_number_of_rows(cols):
+    import torch
+    stream = torch.cuda.current_stream()
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x, times = torch.empty((2, 700, cols), device="cuda").normal_(0.0, 3.0, generator=gen).bfloat16()
+    x[:, 9::700] = 100.0
+    norm = hb.make_norm(times[0], 1e-6)
+
+    def call(rows):
+        codes, scales = torch.empty((2, rows, cols), dtype=torch.int8, device="cuda"), torch.empty((2, rows), device="cuda")
+        total = torch.empty_like(x[:rows])
+        hb.hfx_quantise_rows(hb.HFX_ACT_SILU, rows, cols, x, cols, times, cols, None, codes[0], scales[0], stream)
+        hb.hfx_rms_norm(norm, rows, x, cols, times, cols, total, None, codes[1], scales[1], stream)
+        return codes, scales
+    codes, scales = call(700)
+    for rows in (1, 256, 257):
+        few_codes, few_scales = call(rows)
+        assert torch.equal(few_codes, codes[:, :rows]) and torch.equal(few_scales, scales[:, :rows])
+
+
 # ------------------------------------------------------------------ products
 def product_oracle(codes, scales, weight, weight_scales, bias, fp32):
     """With the operator's roundings; the sums by a product in 64 bits, which holds them exactly."""
