@@ -643,12 +643,15 @@ static hipError_t launch_tiles_as(const MatmulRows& a, bool fp32, hipStream_t st
   return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, S, U, Turned, true> : matmul_tile_kernel<BN, BM, WN, WM, K, S, U, Turned, false>,
                 dim3((unsigned)tiles_n * (unsigned)tiles_m), BN / WN * (BM / WM) * K * 64, stream, a, tiles_n, tiles_m);
 }
+// Stages in turns, plain and so: 64 rows of 8192 to 4096 channels by 32x32 13.7 and 9.4 us, 96 of 16384 35.3 and 30.8, 32 of 4096 to 16384 by 64x64, from memory, 18.2 and 15.2.  Elsewhere they cost
+// more than they give: 256 rows of 8192 to 4096 by 64x64 16.2 and 18.4, 64 of 5120 to 5120 by 32x32 8.8 and 9.4, 37 of 8192 to 1280 (80 tiles) 8.1 and 8.4.
+static bool takes_turns(int bn, int bm, int rows, int n, long weight_stride) {
+  return bn == bm && bn <= 64 && rows <= 128 && weight_stride % 4096 == 0 && (long)((n + bn - 1) / bn) * ((rows + bm - 1) / bm) >= kComputeUnits;
+}
 template <int BN, int BM, int WN, int WM, int K, int S, int U>
 static hipError_t launch_tiles(const MatmulRows& a, bool fp32, hipStream_t stream) {
-  // Stages in turns, plain and so: 64 rows of 8192 to 4096 channels by 32x32 13.7 and 9.4 us, 96 of 16384 35.3 and 30.8, 32 of 4096 to 16384 by 64x64, from memory, 18.2 and 15.2.  Elsewhere they cost
-  // more than they give: 256 rows of 8192 to 4096 by 64x64 16.2 and 18.4, 64 of 5120 to 5120 by 32x32 8.8 and 9.4, 37 of 8192 to 1280 (80 tiles) 8.1 and 8.4.
   if constexpr (BN == BM && BN <= 64)
-    if (a.rows <= 128 && a.weight_stride % 4096 == 0 && (long)((a.n + BN - 1) / BN) * ((a.rows + BM - 1) / BM) >= kComputeUnits) return launch_tiles_as<BN, BM, WN, WM, K, S, U, true>(a, fp32, stream);
+    if (takes_turns(BN, BM, a.rows, a.n, a.weight_stride)) return launch_tiles_as<BN, BM, WN, WM, K, S, U, true>(a, fp32, stream);
   return launch_tiles_as<BN, BM, WN, WM, K, S, U, false>(a, fp32, stream);
 }
 // Workgroups of a large kernel: one for each compute unit.  Where the sum has fewer stages than a ring each takes one tile, because the copies go on into the next tile and not past it.
@@ -713,62 +716,79 @@ static Choice best_way(int rows, int n, int stages) {
   return best;
 }
 
+// The launches of a product: the first takes `rows` rows and `n` channels, a second one (way[1]) the rows or the channels that are left.
+// A large product whose last round would be nearly empty: two launches, one of whole rounds or of whole tiles, one of the rows or channels that are left, if the times say that this takes a twentieth less
+// (8224 rows of 4096 to 6144 channels 205 -> 180 us, 4128 of 8192 to 4096 148 -> 128, 10000 of 5120 to 5120 251 -> 227; of 130 products from 60 us up none took more than 1.03 times as long.  With a fiftieth, and
+// from 25 us up, some took 1.1 times: 1056 of 4096 to 4096 25.5 -> 28.0).
+struct Launches {
+  const Way* way[2];
+  int rows, n;
+};
+static Launches launches_of(int all_rows, int all_n, int stages) {
+  const Choice whole = best_way(all_rows, all_n, stages);
+  Launches l = {{whole.way, nullptr}, all_rows, all_n};
+  if (whole.us <= 60.0f) return l;
+  float least = 0.95f * whole.us;
+  auto consider = [&](const Way& w, int m, int c) {
+    if (m <= 0 || c <= 0 || (m >= all_rows && c >= all_n)) return;
+    const float us = time_of(w, m, c, stages);
+    if (us >= least) return;
+    const Choice rest = m < all_rows ? best_way(all_rows - m, all_n, stages) : best_way(all_rows, all_n - c, stages);
+    if (us + rest.us >= least) return;
+    least = us + rest.us;
+    l = {{&w, rest.way}, m, c};
+  };
+  for (const Way& w : kWays) {
+    if (w.most != 1) continue;
+    const int tiles_n = (all_n + w.bn - 1) / w.bn, tiles_m = (all_rows + w.bm - 1) / w.bm;
+    const long full = (long)tiles_n * tiles_m / kComputeUnits * kComputeUnits;
+    consider(w, all_rows / w.bm * w.bm, all_n);
+    consider(w, (int)(full / tiles_n) * w.bm, all_n);
+    consider(w, all_rows, all_n / w.bn * w.bn);
+    consider(w, all_rows, (int)(full / tiles_m) * w.bn);
+  }
+  return l;
+}
+
 hipError_t launch_matmul_rows(MatmulRows a, bool fp32, hipStream_t stream) {
   // Results of more than 64 MB go past the caches, where they push out what the tiles share: 4128 rows to 16384 channels 268 -> 255 us, 8192 rows over 1024 values to 8192
   // channels 109 -> 89 (21 MB of results: 80.6 and 79.8).
   a.past = !fp32 && a.out_stride % 8 == 0 && 2l * a.rows * a.n > (64l << 20);
-  const int stages = (a.k + 127) / 128;
-  const Choice whole = best_way(a.rows, a.n, stages);
-  // A large product whose last round would be nearly empty: two launches, one of whole rounds or of whole tiles, one of the rows or channels that are left, if the times say that this takes a twentieth less
-  // (8224 rows of 4096 to 6144 channels 205 -> 180 us, 4128 of 8192 to 4096 148 -> 128, 10000 of 5120 to 5120 251 -> 227; of 130 products from 60 us up none took more than 1.03 times as long.  With a fiftieth, and
-  // from 25 us up, some took 1.1 times: 1056 of 4096 to 4096 25.5 -> 28.0).
-  if (whole.us > 60.0f) {
-    Choice one = whole, other = {};
-    int rows = a.rows, n = a.n;
-    float least = 0.95f * whole.us;
-    auto consider = [&](const Way& w, int m, int c) {
-      if (m <= 0 || c <= 0 || (m >= a.rows && c >= a.n)) return;
-      const float us = time_of(w, m, c, stages);
-      if (us >= least) return;
-      const Choice rest = m < a.rows ? best_way(a.rows - m, a.n, stages) : best_way(a.rows, a.n - c, stages);
-      if (us + rest.us >= least) return;
-      least = us + rest.us;
-      one = {&w, us};
-      other = rest;
-      rows = m;
-      n = c;
-    };
-    for (const Way& w : kWays) {
-      if (w.most != 1) continue;
-      const int tiles_n = (a.n + w.bn - 1) / w.bn, tiles_m = (a.rows + w.bm - 1) / w.bm;
-      const long full = (long)tiles_n * tiles_m / kComputeUnits * kComputeUnits;
-      consider(w, a.rows / w.bm * w.bm, a.n);
-      consider(w, (int)(full / tiles_n) * w.bm, a.n);
-      consider(w, a.rows, a.n / w.bn * w.bn);
-      consider(w, a.rows, (int)(full / tiles_m) * w.bn);
+  const Launches l = launches_of(a.rows, a.n, (a.k + 127) / 128);
+  MatmulRows rest = a;
+  if (l.way[1]) {
+    const int element = fp32 ? 4 : 2;
+    if (l.rows < a.rows) {
+      rest.rows -= l.rows;
+      rest.codes += l.rows * a.codes_stride;
+      rest.scales += l.rows;
+      rest.out = static_cast<char*>(a.out) + l.rows * a.out_stride * element;
+    } else {
+      rest.n -= l.n;
+      rest.weight += l.n * a.weight_stride;
+      rest.weight_scales += l.n;
+      if (a.bias) rest.bias += l.n;
+      rest.out = static_cast<char*>(a.out) + (long)l.n * element;
     }
-    if (other.way) {
-      MatmulRows rest = a;
-      const int element = fp32 ? 4 : 2;
-      if (rows < a.rows) {
-        rest.rows -= rows;
-        rest.codes += rows * a.codes_stride;
-        rest.scales += rows;
-        rest.out = static_cast<char*>(a.out) + rows * a.out_stride * element;
-      } else {
-        rest.n -= n;
-        rest.weight += n * a.weight_stride;
-        rest.weight_scales += n;
-        if (a.bias) rest.bias += n;
-        rest.out = static_cast<char*>(a.out) + (long)n * element;
-      }
-      a.rows = rows;
-      a.n = n;
-      const hipError_t e = one.way->launch(a, fp32, stream);
-      return e != hipSuccess ? e : other.way->launch(rest, fp32, stream);
-    }
+    a.rows = l.rows;
+    a.n = l.n;
   }
-  return whole.way->launch(a, fp32, stream);
+  const hipError_t e = l.way[0]->launch(a, fp32, stream);
+  return e != hipSuccess || !l.way[1] ? e : l.way[1]->launch(rest, fp32, stream);
 }
 
 }  // namespace hfx
+
+// For tests, which see to it that they reach every kernel: how many there are (rows 0), or the launches of a product, their numbers in kWays in ways[] (100 more where stages are taken in turns).
+extern "C" int hfx_internal_matmul_ways(int rows, int n, int k, int64_t weight_stride, int* ways) {
+  using namespace hfx;
+  if (rows == 0) return sizeof(kWays) / sizeof(kWays[0]);
+  const Launches l = launches_of(rows, n, (k + 127) / 128);
+  int count = 0;
+  for (const Way* w : l.way) {
+    if (!w) break;
+    const int m = count == 0 ? l.rows : l.rows < rows ? rows - l.rows : rows, c = count == 0 ? l.n : l.rows < rows ? n : n - l.n;
+    ways[count++] = (int)(w - kWays) + (takes_turns(w->bn, w->bm, m, c, (long)weight_stride) ? 100 : 0);
+  }
+  return count;
+}

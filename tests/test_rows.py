@@ -10,6 +10,8 @@ Tolerances, from the arithmetic:
    the division and the product with the factor 2^-24 each: 2^-22 + 4 * 2^-24 = 2^-21 of the value.  A code is then within half a step, plus 127 times 2^-21 twice (of the value and of the
    row's largest) and the rounding of factor and product (2^-24 each): 0.5 + 1.4e-4 steps.
 """
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -465,6 +467,51 @@ def test_products_that_fill_the_chip(rows, k, n):
         hb.hfx_matmul_rows(hb.make_weight_q8(weight, weight_scales, bias if with_bias else None), rows, codes, k, scales, out, n, fp32, torch.cuda.current_stream())
         assert bool((out[rows:] == 7.0).all())
         assert torch.equal(out[:rows], want.to(out.dtype))
+
+
+# (rows, k, elements from one of the weight's rows to the next, n): tiles that take the stages of the sum in turns, whole chips of them and several layers, with whole and partial
+# stages and only those; the few rows that the kernel for them takes, and one more.
+APART = [(64, 4096, 4096, 16384), (33, 4096, 4096, 16383), (50, 4016, 4096, 16384), (48, 272, 4096, 16370), (40, 112, 4096, 16384), (64, 1168, 8192, 16333), (64, 8192, 8192, 4096), (40, 2000, 4096, 4090),
+         (17, 4096, 4096, 8200), (100, 384, 4096, 4096), (1, 8192, 8192, 4096), (7, 512, 512, 640), (8, 512, 512, 640), (9, 512, 512, 640), (8, 4112, 4128, 4099), (8, 8208, 8208, 2050), (9, 4096, 4096, 4096),
+         (100, 4096, 4096, 8190), (150, 1040, 1040, 4096), (200, 400, 416, 4090), (128, 2064, 2064, 6100)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,k,stride,n", APART)
+def test_products_of_few_rows_and_many_channels(rows, k, stride, n):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows + n + k)
+    codes, weight = (torch.randint(-128, 128, (m, k), dtype=torch.int8, device="cuda", generator=gen) for m in (rows, n))
+    weight = strided(torch, weight, stride - k)[:, :k]
+    scales, weight_scales = (torch.rand(m, device="cuda", generator=gen) + 0.01 for m in (rows, n))
+    bias = torch.empty(n, dtype=torch.bfloat16, device="cuda").normal_(0.0, 1000.0, generator=gen)
+    sums = (codes.double() @ weight.double().T).float()         # exact in 64 bits, rounded once
+    for fp32 in (False, True):
+        for with_bias in (False, True):
+            want = sums * scales[:, None] * weight_scales
+            if with_bias:
+                want = want + bias.float()
+            out = torch.full((rows + 2, n + 3), 7.0, dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda")
+            hb.hfx_matmul_rows(hb.make_weight_q8(weight, weight_scales, bias if with_bias else None), rows, codes, k, scales, out, n + 3, fp32, torch.cuda.current_stream())
+            assert bool((out[rows:] == 7.0).all()) and bool((out[:, n:] == 7.0).all())
+            assert torch.equal(out[:rows, :n], want.to(out.dtype))
+
+
+def test_every_kernel_is_reached():
+    """The sizes of the two tests above come to every kernel that a product can take, with the stages of the sum in order and, where there is such a form, in turns."""
+    choose, ways = hb.load().hfx_internal_matmul_ways, (ctypes.c_int * 2)()
+    choose.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.POINTER(ctypes.c_int)]
+    reached = {}
+    for rows, k, stride, n in [(rows, k, k, n) for rows, k, n in FILLING] + APART:
+        launches = choose(rows, n, k, stride, ways)
+        assert launches in (1, 2)
+        for way in ways[:launches]:
+            reached.setdefault(way, []).append((rows, k, stride, n))
+    ways_there_are = choose(0, 0, 0, 0, ways)
+    assert set(range(ways_there_are)) <= set(reached), sorted(set(range(ways_there_are)) - set(reached))
+    assert {101, 103} == {way for way in reached if way >= 100}                          # 32 by 32 and 64 by 64
+    assert all(len(sizes) >= 3 for sizes in reached.values()), {way: sizes for way, sizes in reached.items() if len(sizes) < 3}
+    assert {choose(rows, 640, 512, 512, ways) and ways[0] for rows in (1, 7, 8)} == {0} and choose(9, 640, 512, 512, ways) == 1 and ways[0] == 1
 
 
 @pytest.mark.gpu
