@@ -361,6 +361,29 @@ def test_a_row_does_not_depend_on_the_number_of_rows(cols):
         assert torch.equal(few_codes, codes[:, :rows]) and torch.equal(few_scales, scales[:, :rows])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(9601, 512), (4801, 1024), (2407, 2048), (1203, 4096)])
+def test_rows_past_the_caches(rows, cols):
+    """Calls of more than 32 MB of each thread count: the same bits as in calls of a tenth of the rows."""
+    import torch
+    stream = torch.cuda.current_stream()
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x, y = torch.empty((2, rows, cols), device="cuda").normal_(0.0, 2.0, generator=gen).bfloat16()
+    norm = hb.make_norm(y[0] + 1.0, 1e-6)
+
+    def call(first, count):
+        total, out, normed = torch.empty((3, count, cols), dtype=torch.bfloat16, device="cuda")
+        codes, scales = torch.empty((2, count, cols), dtype=torch.int8, device="cuda"), torch.empty((2, count), device="cuda")
+        hb.hfx_rms_norm(norm, count, x[first:], cols, y[first:], cols, total, normed, codes[0], scales[0], stream)
+        hb.hfx_quantise_rows(hb.HFX_ACT_SILU, count, cols, x[first:], cols, y[first:], cols, out, codes[1], scales[1], stream)
+        return total, out, normed, *codes, *scales
+    whole, part = call(0, rows), -(-rows // 10)
+    parts = [call(first, min(part, rows - first)) for first in range(0, rows, part)]
+    for i, got in enumerate(whole):
+        assert torch.equal(got, torch.cat([p[i] for p in parts])), i
+    assert torch.equal(whole[0], (x.float() + y.float()).bfloat16())
+
+
 # ------------------------------------------------------------------ products
 def product_oracle(codes, scales, weight, weight_scales, bias, fp32):
     """With the operator's roundings; the sums by a product in 64 bits, which holds them exactly."""
