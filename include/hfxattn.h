@@ -396,8 +396,8 @@ typedef struct {
  *   sum          [device] bf16 [rows][cols]: takes h.  May be x or residual itself if that is packed
  *   out          [device] bf16 [rows][cols]: takes the result; NULL: not wanted
  *   codes, scales [device] int8 [rows][cols] and fp32 [rows]: the result in 8 bits; both or none, none only with out.  The code of a
- *                value is formed from h * weight, exact in fp32 unless that overflows (it then counts as not finite), the factor 127 / top and their product rounded to
- *                fp32; the scale is that of the row of h * weight, times r.
+ *                value is formed from h * weight, exact in fp32 unless that overflows (it then counts as not finite) or falls below 2^-126 (its code is 0 either way), the
+ *                factor 127 / top and their product rounded to fp32; the scale is that of the row of h * weight, times r.
  * Buffers are 16-byte aligned (scales: 4) and overlap in no other way.  Asynchronous on `stream`; allocates nothing.
  * Errors: HFX_ERR_NULL, HFX_ERR_SHAPE (rows < 0; cols, eps or a stride not as above; in place and not packed), HFX_ERR_ALIGN (also: a stride that is no
  * multiple of 8), HFX_ERR_DEVICE.
