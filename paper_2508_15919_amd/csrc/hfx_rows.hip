@@ -292,7 +292,9 @@ __global__ __launch_bounds__(T) void quantise_rows_kernel(const QuantiseRows a) 
 
 // Threads and pieces for rows of `cols` values: one piece to a thread up to 4096, two up to 16384, four and from there on a second reading.  (8224 rows of 4096: 512 threads of one piece
 // 48.9 us, 256 of two 52.9, 128 of four 54.6, 1024 of one 65.2; four rows 3.2, 3.7, 4.9 and 3.3.  8224 rows of 1024: 128 of one 17.1, 64 of two 17.3, 256 of one 19.9.  2500 gated rows of 8192: 512 of two
-// 22.0, 1024 of one 26.8, 256 of four 23.5.)  Up to 256 gated rows, each on a unit of its own, take 1024 of one: 64 of 8192 3.3 us, with 512 of two 3.6 (the norm's 3.7 and 3.5).
+// 22.0, 1024 of one 26.8, 256 of four 23.5.)  Up to 256 rows on
+// their way to 8 bits, each on a unit of its own, take 1024 of one from 4112 to 8192 values, with an activation, a factor, both or neither: with 512 of two 64 rows of 8192 3.60 and 3.29 us (gated), 2.46 and
+// 2.33 (plain), of 4112 3.16 and 2.91, 2.34 and 2.16; 256 of 8192 3.80 and 3.57, 2.66 and 2.59.  384 plain rows of 8192 2.93 and 3.10, gated 5.50 and 5.44.  The norm's rows do not: 64 of 8192 3.5 and 3.7.
 // Rows of more than 32 MB in all go past the caches where nobody reads them soon: what comes in, and the sum, which the next norm reads (1024 rows of 4096, 29 MB in 8 bits, with a reader of the
 // sum behind it 15.3 -> 13.1 us; 8224 rows alone 46.7 -> 44.3; 512 rows 8.9 -> 9.3).  What the next call reads, codes and results, stays in reach.
 template <class A, class Pick>
@@ -310,7 +312,7 @@ static hipError_t launch_rows(const A& a, int rows, long bytes, hipStream_t stre
   if (a.cols <= 2048) return run(std::integral_constant<int, 256>(), one);
   if (a.cols <= 4096) return run(std::integral_constant<int, 512>(), one);
   if constexpr (std::is_same_v<A, QuantiseRows>)
-    if (rows <= 256 && a.cols > 4096 && a.cols <= 8192) return run(std::integral_constant<int, 1024>(), one);
+    if (rows <= 256 && a.cols <= 8192) return run(std::integral_constant<int, 1024>(), one);
   if (a.cols <= 8192) return run(std::integral_constant<int, 512>(), two);
   if (a.cols <= 16384) return run(std::integral_constant<int, 1024>(), two);
   return run(std::integral_constant<int, 1024>(), four);
