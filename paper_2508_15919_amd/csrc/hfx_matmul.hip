@@ -61,9 +61,10 @@ __device__ __forceinline__ void store_line(const MatmulRows& a, int m, int n, co
 // 16 channels by up to 8 rows to a workgroup, the sum cut into steps of 128 values that its 16 wavefronts take in turn; both operands go straight to registers, two steps ahead.  A
 // lane has 32 bytes in a row of a step, which two matrix instructions take one half each (any order of the values will do that is the same in both operands), so that
 // four lanes ask for a whole line.  Rows that are not there are the last one again, which costs no further lines
-// (16 rows of 4096 to 16384 channels 20.6 us where 4 take 16.0: 9 and more go by tiles of 32 rows, 16.3).
-// Bound by the weight's way from memory: one row of 4096 to 16384 channels (67 MB) 14.9 us, 5.3 TB/s behind the 2.1 us of a launch.  Four rows to 6144
-// channels 8.8 us, with eight wavefronts four steps ahead 9.3.
+// (16 rows of 4096 to 16384 channels 20.6 us where 4 take 16.0: 9 and more go by tiles of 32 rows, 14.2).
+// Bound by the weight's way to the compute units, behind the 2.1 us of a launch: 4 rows of 8192 to 4096 channels (34 MB) 9.5 us from memory and 8.6 from the last level's cache, where tiles of 32 by 32 take 12.8 and
+// 12.2; one row of 16384 to 4096 (67 MB) 16.0 and 14.3, 20.6 and 17.0; one of 4096 to 4096 6.5 and 5.5, 7.4 and 5.8.  More channels go by the tiles (4 rows of 4096 to 6144 here 9.3 us, from memory, and by those
+// 8.0).  Eight wavefronts four steps ahead, in place of sixteen two, took 1.06 times as long.
 template <bool Fp32>
 __global__ __launch_bounds__(1024) void matmul_few_kernel(const MatmulRows a) {
   constexpr int kWaves = 16, kAhead = 2;
@@ -148,11 +149,12 @@ __device__ __forceinline__ void copy_words_to_lds(const float* base, unsigned of
 // 16-byte pieces are permuted by bits 1 to 3 of its number, so that 16 lanes that read the same piece of 16 rows meet all banks.  (WN channels by WM rows, and of a
 // stage one part of K, belong to a wavefront.)  The operands of 32 values are read while the matrix instructions of the 32 before them run; the workgroup meets
 // once a stage, ahead of the last of these, when all of the stage has been read: its place is then free for the copies of the stage S behind it.
-// Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 85 GB/s for each, 256 rows of 4096 to 6144 channels 17.0 us where weights come from memory and
-// 12.4 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels: two lines 10.1 us, one 11.2, in a ring of
-// the same bytes 13.1; alone on its unit 128 by 64 too, 256 rows of 4096 to 6144 17.0 and 17.8,
-// 200 15.5 and 17.0), and eight wavefronts of 32 by 32 serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels 15.3 and 15.6 us).
-// Turned: the whole stages are taken in a ring of their own, for each eighth column of tiles (a die's next one) from three stages further on: rows that lie a multiple of 4096 bytes apart
+// Bound by the way of the tiles' lines to a compute unit, most of which another one asks for too: 45 to 95 GB/s for each, 256 rows of 4096 to 6144 channels 17.1 us where weights come from memory and
+// 12.7 where the last level's cache has them (34 MB in all, 6.9 us at a large copy's rate).  Small tiles want long stages (37 rows of 8192 to 1280 channels, from memory and from that cache: two lines 9.4 and 7.9 us, one
+// 13.6 and 10.6, in a ring of the same bytes 11.2 and 11.0; alone on its unit 128 by 64 too: 256 rows of 4096 to 6144 17.2 and 17.8 from memory, 200 15.6 and 17.0, the same from the cache), and eight wavefronts of 32 by 32
+// serve 128 by 64 better than four of 64 by 32 (128 rows of 4096 to 16384 channels, from memory, 22.4 and 22.8 us).
+// Tiles are taken in plain order, the channels' first: those of the same channels in other rows meet on a die, which then has their part of the weight once, where there is a multiple of eight tiles of channels.
+// Turned: the whole stages are taken in a ring of their own, for each eighth column of tiles (with the first rows a die's next one) from three stages further on: rows that lie a multiple of 4096 bytes apart
 // have the same stage in the same few channels of the L2, where all the die's workgroups would ask for it at once.
 template <int BN, int BM, int WN, int WM, int K, int S, int U, bool Turned, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
@@ -365,8 +367,8 @@ __global__ __launch_bounds__(BN / WN * (BM / WM) * K * 64) void matmul_tile_kern
 // 16 rows meet all banks.  The operands of 32 values are read while the matrix instructions of the 32 before them run.  The workgroup meets once a
 // stage, ahead of the last of these, when all of the stage has been read: its places are then free for the copies of the stages RM and RN behind it.  These go on into the next tile, so
 // that its first stages arrive while the results of this one leave.
-// Bound by the clock that power leaves the matrix cores, with the LDS close behind: 8192 rows of 4096 to 6144 channels 172 to 176 us, 2.35 to 2.4 POP/s (a library's product of 8224 rows 227), the matrix cores busy in 61 %
-// of the cycles of a clock of 1.85 GHz; 8192 of 8192 to 8192 434 to 450 us.  Nothing but these instructions, on operands in registers, runs at 3.4 POP/s with random operands and at 4.5 with zeros.  Four wavefronts of 128 by
+// Bound by the clock that power leaves the matrix cores, with the LDS close behind: 8192 rows of 4096 to 6144 channels 172 to 176 us, 2.35 to 2.4 POP/s (a library's product 184; of 8224 rows 207, here 181), the matrix cores busy in 61 %
+// of the cycles of a clock of 1.85 GHz; 8192 of 8192 to 8192 434 to 450 us.  Nothing but these instructions, on operands in registers, runs at 3.2 to 3.4 POP/s with random operands and at 4.5 with zeros.  Four wavefronts of 128 by
 // 128, which read a third less from the LDS, take 183 and 464 us.  (Tiles whose copies end with them, in one ring for both operands: 8224 rows 219 us; with both, and no second launch, 195 to 205.)
 template <int BN, int BM, int WN, int WM, int RN, int RM, bool Fp32>
 __global__ __launch_bounds__(BN / WN * (BM / WM) * 64) void matmul_large_kernel(const MatmulRows a, int tiles_n, int tiles_m) {
@@ -643,8 +645,11 @@ static hipError_t launch_tiles_as(const MatmulRows& a, bool fp32, hipStream_t st
   return launch(fp32 ? matmul_tile_kernel<BN, BM, WN, WM, K, S, U, Turned, true> : matmul_tile_kernel<BN, BM, WN, WM, K, S, U, Turned, false>,
                 dim3((unsigned)tiles_n * (unsigned)tiles_m), BN / WN * (BM / WM) * K * 64, stream, a, tiles_n, tiles_m);
 }
-// Stages in turns, plain and so: 64 rows of 8192 to 4096 channels by 32x32 13.7 and 9.4 us, 96 of 16384 35.3 and 30.8, 32 of 4096 to 16384 by 64x64, from memory, 18.2 and 15.2.  Elsewhere they cost
-// more than they give: 256 rows of 8192 to 4096 by 64x64 16.2 and 18.4, 64 of 5120 to 5120 by 32x32 8.8 and 9.4, 37 of 8192 to 1280 (80 tiles) 8.1 and 8.4.
+// Where the stages are taken in turns, plain and so, over 184 products that come here (1 to 128 rows, sums of 4096 to 16384 values, 2048 to 20480 channels), from memory and from the last level's cache: 32x32 on
+// average 0.91 and 0.88 times the time, 64x64 0.90 and 0.94.  In us, from the cache (from memory): 64 rows of 8192 to 4096 channels by 32x32 13.5 and 9.2 (13.4 and 13.2), 16 of 4096 to 16384 13.7 and 11.8 (15.9 and 14.2);
+// by 64x64 64 of 4096 to 16384 12.8 and 12.6 (18.4 and 16.3), 33 of 16384 to 16384 65.5 and 46.9.  The worst, two tiles of rows by 64x64: 112 of 4096 to 8192 10.2 and 11.4 (13.8 and 14.2).  What does not come here: 256 rows of 8192 to
+// 4096 by 64x64 16.2 and 18.4, 64 of 5120 to 5120 by 32x32 8.8 and 9.4, 37 of 8192 to 1280 (80 tiles) 8.1 and 8.4; 32x64, which has no such form though it would pay (96 of 16384 to 4096 27.2 and 20.7, from memory 31.1 and 24.7;
+// 96 of 8192 to 4096 15.1 and 11.8, 16.6 and 14.6).
 static bool takes_turns(int bn, int bm, int rows, int n, long weight_stride) {
   return bn == bm && bn <= 64 && rows <= 128 && weight_stride % 4096 == 0 && (long)((n + bn - 1) / bn) * ((rows + bm - 1) / bm) >= kComputeUnits;
 }
@@ -667,6 +672,7 @@ static hipError_t launch_large(const MatmulRows& a, bool fp32, hipStream_t strea
 // change from call to call): the kernel that it names takes 1.006 times the fastest one's time on average, more than 1.1 times in one (777 rows of 8192 to 1280 channels, 260 tiles of 64 by 64, whose
 // last four cost less than a second layer of tiles: 29 and 21 us).  Why there are several, in us
 // (rows, k, channels; that kernel, then the next best one among the others):
+// (buffers of 600 MB in turn, 24 at most: those of 37 rows stay in the last level's cache)
 //   4    8192  4096        few    9.6   32x32   12.7        37    8192  1280   32x32    8.0   32x64    9.7
 //   64   4096  6144      32x64   10.9   32x32   11.6        128   4096  6144   64x64   13.1   32x64   16.0
 //   256  1024  8192     128x64    6.3   64x64    6.9        777   1024  8192   128x128, two to a unit 14.6   256x128 14.8

@@ -239,8 +239,8 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNorm a) {
   }
 }
 
-// Rows through an activation, times other rows, to bf16 and to 8 bits.  Laid out as the norm, and bound as it is: 2500 gated rows of 8192 (102 MB) 20.0 us, 5.1
-// TB/s; 64 of them 4.5.
+// Rows through an activation, times other rows, to bf16 and to 8 bits.  Laid out as the norm, and bound as it is: 2500 gated rows of 8192 (102 MB) 20.2 us, 5.1
+// TB/s; 64 of them 3.3 to 3.4 us a call in a captured graph.
 template <int T, int P, bool Past>
 __global__ __launch_bounds__(T) void quantise_rows_kernel(const QuantiseRows a) {
   const long row = blockIdx.x;
